@@ -53,6 +53,11 @@ extern "C" {
 #define NGSGD_TANH 0
 #define NGSGD_PNORM 1
 
+/* Element types of the operators that take 16-bit data. */
+#define NGSGD_FLOAT32 0
+#define NGSGD_BFLOAT16 1
+#define NGSGD_FLOAT16 2
+
 #define NGSGD_MAX_LAYERS 16
 #define NGSGD_MAX_RANK 96    /* the R x R update runs in one workgroup's LDS */
 
@@ -180,6 +185,99 @@ int ngsgd_precondition_simple(float* dev_M, int32_t N, int32_t D, int32_t ld, fl
 int ngsgd_precondition_simple_static(float* dev_M, int32_t N, int32_t D, int32_t ld, float alpha,
                                      float epsilon, float* dev_gamma, float* dev_rownorm2,
                                      void* hip_stream);
+
+/* ---- layer norm ------------------------------------------------------------------------------- */
+
+/* y = xhat * weight + bias,  xhat = (x - mean) * rstd,  for each of the N rows of D numbers, with the row's mean
+ * and rstd = (variance + epsilon)^(-1/2) (variance with divisor D, from the differences to the mean).
+ *   type           of x and y (NGSGD_FLOAT32, NGSGD_BFLOAT16 or NGSGD_FLOAT16)
+ *   weight_type    of weight and bias: `type` or NGSGD_FLOAT32
+ *   dev_weight, dev_bias (optional, D numbers each): without them ones and zeros
+ *   dev_mean, dev_rstd (optional, N floats each) receive what the backward pass needs
+ * Statistics and sums are in fp32, outputs are rounded once.  Leading dimensions count elements, at least D and otherwise free:
+ * rows need no alignment beyond an element's (rows on multiples of 16 bytes are faster).  dev_y may be dev_x with
+ * the same leading dimension; other overlaps are not allowed.  N may be 0.  Rows do not mix: an infinity or NaN
+ * stays in its row.  epsilon is finite and not negative; with 0 a row of equal numbers gives NaN. */
+int ngsgd_layernorm_forward(const void* dev_x, int64_t ldx, int32_t type, const void* dev_weight,
+                            const void* dev_bias, int32_t weight_type, int64_t N, int32_t D, float epsilon,
+                            void* dev_y, int64_t ldy, float* dev_mean, float* dev_rstd, void* hip_stream);
+
+/* Device workspace that ngsgd_layernorm_backward needs for the weight's and the bias' gradient of up to max_rows
+ * rows; it holds nothing between calls. */
+int ngsgd_layernorm_workspace_bytes(int64_t max_rows, int32_t D, size_t* out_bytes);
+
+/* Gradients of the above for the derivative dy of a scalar, with the mean and rstd of the forward pass:
+ *   dev_dx       (optional, N x D) = rstd * (g - mean(g) - xhat * mean(g * xhat)),  g = dy * weight
+ *   dev_dweight  (optional, D, weight_type) = sum over the rows of dy * xhat
+ *   dev_dbias    (optional, D, weight_type) = sum over the rows of dy
+ * At least one of them.  The sums over the rows are in fp32 in an order that depends on the sizes alone: a call repeated
+ * gives the same bits.  dev_dx may be dev_dy with the same leading dimension; other overlaps are not allowed.
+ * With N = 0 the sums are zero.  dev_workspace (256-byte aligned) is only needed with dev_dweight or dev_dbias. */
+int ngsgd_layernorm_backward(const void* dev_dy, int64_t lddy, const void* dev_x, int64_t ldx, int32_t type,
+                             const void* dev_weight, int32_t weight_type, const float* dev_mean,
+                             const float* dev_rstd, int64_t N, int32_t D, void* dev_dx, int64_t lddx,
+                             void* dev_dweight, void* dev_dbias, void* dev_workspace, size_t workspace_bytes,
+                             void* hip_stream);
+
+/* ---- AdamW over many tensors ------------------------------------------------------------------- */
+
+typedef struct ngsgd_adamw ngsgd_adamw;  /* the moments and step count of a list of tensors */
+
+/* Host memory, copied by ngsgd_adamw_create. */
+typedef struct {
+  int32_t n_tensors;
+  void* const* dev_params;    /* each tensor dense; NULL only where its size is 0           */
+  const int64_t* sizes;       /* elements; no two tensors may share memory                  */
+  const float* weight_decay;  /* of each tensor; NULL: 0                                    */
+  const float* rate;          /* factor of each tensor on the learning rate; NULL: 1        */
+  int32_t param_type;         /* NGSGD_FLOAT32, _BFLOAT16 or _FLOAT16                       */
+  int32_t grad_type;          /* that of the parameters, NGSGD_FLOAT32, or any with fp32 parameters */
+  int32_t state_bits;         /* 32: moments in fp32; 8: codes with an exponent for every 256 elements */
+  int32_t master;             /* 1: parameters in 16 bits are rounded from fp32 copies that are kept */
+  double beta1, beta2;        /* in [0, 1)                                                  */
+  float epsilon;
+} ngsgd_adamw_config;
+
+int ngsgd_adamw_workspace_bytes(const ngsgd_adamw_config* cfg, size_t* out_bytes);
+
+/* Zero moments, step count 0, fp32 copies from the parameters.  The parameters stay where they are until
+ * ngsgd_adamw_destroy.  Synchronises the device (so not under capture). */
+int ngsgd_adamw_create(const ngsgd_adamw_config* cfg, void* dev_workspace, size_t workspace_bytes,
+                       ngsgd_adamw** out);
+int ngsgd_adamw_destroy(ngsgd_adamw* h);
+
+/* One step, t = 1, 2, ...:
+ *   g = grad_scale * gradient;  m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2
+ *   p = p (1 - lr * weight_decay) - lr * (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + epsilon)
+ * in fp32, from the fp32 copy of p if there is one.
+ *   dev_grads   (host array) the gradient of each tensor, dense, of grad_type; a tensor whose gradient is NULL is
+ *               left as it is, while the step counts
+ *   dev_lr, dev_grad_scale (optional, 1 float each) are multiplied to lr and grad_scale: a schedule or the
+ *               factor of a clipped norm that only the device knows
+ * The step count lives on the device, so a captured step counts on at each replay (with the gradients' addresses,
+ * lr and grad_scale of its capture).  Up to 448 tensors take one launch.
+ * Moments in 8 bits: m as a sign, 4 bits of exponent and 3 behind the point, sqrt(v) as 5 and 3 bits, below an exponent that 256
+ * elements share; p is updated from this step's moments before they are coded.  They are rounded down
+ * after a share of a step has been added, frac(i A + t B) of the element's place i in the flat arrays and t (A, B = 0x9E3779B1,
+ * 0x6A09E667 over 2^32, the upper 20 bits), so that over the steps changes much smaller than a code's step
+ * add up.  An infinity or NaN makes its own element NaN, not its block. */
+int ngsgd_adamw_step(ngsgd_adamw* h, const void* const* dev_grads, float lr, const float* dev_lr,
+                     float grad_scale, const float* dev_grad_scale, void* hip_stream);
+
+/* The flat arrays: their length, and their addresses in the workspace (NULL for moments in 8 bits, or without fp32
+ * copies).  Tensor k's elements start behind those of the tensors before it, each rounded up to a multiple of 256. */
+int ngsgd_adamw_arrays(const ngsgd_adamw* h, int64_t* elements, float** dev_m, float** dev_v, float** dev_master);
+
+/* The moments as values, to flat arrays in fp32 or bf16 (which holds those of 8-bit codes exactly, but for a v below
+ * 2^-126; 16-byte aligned), and the step count.  Any of the three may be NULL. */
+int ngsgd_adamw_get_state(const ngsgd_adamw* h, void* dev_m, void* dev_v, int32_t type, int64_t* dev_t,
+                          void* hip_stream);
+
+/* Installs moments (flat, 16-byte aligned; NULL: zeros; in 8 bits rounded to the nearest code, which gives back what
+ * ngsgd_adamw_get_state gave) and the step count t >= 0.  fp32 copies are taken from dev_master (flat), with the parameters
+ * rounded from it, or with NULL from the parameters. */
+int ngsgd_adamw_set_state(ngsgd_adamw* h, const float* dev_m, const float* dev_v, const float* dev_master,
+                          int64_t t, void* hip_stream);
 
 /* ---- one replica of the network -------------------------------------------------------------- */
 

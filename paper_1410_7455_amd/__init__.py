@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from contextlib import nullcontext
 from ctypes import POINTER, byref, c_char_p, c_double, c_float, c_int, c_int32, c_int64, c_size_t, c_void_p
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -22,6 +23,9 @@ NGSGD_ENOMEM = -2
 NGSGD_EHIP = -3
 NGSGD_TANH = 0
 NGSGD_PNORM = 1
+NGSGD_FLOAT32 = 0
+NGSGD_BFLOAT16 = 1
+NGSGD_FLOAT16 = 2
 NGSGD_SIDE_INPUT = 0
 NGSGD_SIDE_OUTPUT = 1
 NGSGD_MAX_RANK = 96
@@ -49,6 +53,14 @@ class ngsgd_config(ctypes.Structure):
     ]
 
 
+class ngsgd_adamw_config(ctypes.Structure):
+    _fields_ = [
+        ("n_tensors", c_int32), ("dev_params", POINTER(c_void_p)), ("sizes", POINTER(c_int64)),
+        ("weight_decay", POINTER(c_float)), ("rate", POINTER(c_float)), ("param_type", c_int32), ("grad_type", c_int32),
+        ("state_bits", c_int32), ("master", c_int32), ("beta1", c_double), ("beta2", c_double), ("epsilon", c_float),
+    ]
+
+
 # name -> (restype, argtypes); one entry per symbol declared in include/ngsgd.h
 _SIGNATURES = {
     "ngsgd_precond_workspace_bytes": (c_int, [c_int32, c_int32, c_int32, POINTER(c_size_t)]),
@@ -65,6 +77,19 @@ _SIGNATURES = {
                                           c_void_p, c_void_p, c_void_p]),
     "ngsgd_precondition_simple_static": (c_int, [c_void_p, c_int32, c_int32, c_int32, c_float, c_float, c_void_p,
                                                  c_void_p, c_void_p]),
+    "ngsgd_layernorm_forward": (c_int, [c_void_p, c_int64, c_int32, c_void_p, c_void_p, c_int32, c_int64, c_int32, c_float,
+                                        c_void_p, c_int64, c_void_p, c_void_p, c_void_p]),
+    "ngsgd_layernorm_workspace_bytes": (c_int, [c_int64, c_int32, POINTER(c_size_t)]),
+    "ngsgd_layernorm_backward": (c_int, [c_void_p, c_int64, c_void_p, c_int64, c_int32, c_void_p, c_int32, c_void_p, c_void_p,
+                                         c_int64, c_int32, c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_size_t,
+                                         c_void_p]),
+    "ngsgd_adamw_workspace_bytes": (c_int, [POINTER(ngsgd_adamw_config), POINTER(c_size_t)]),
+    "ngsgd_adamw_create": (c_int, [POINTER(ngsgd_adamw_config), c_void_p, c_size_t, POINTER(c_void_p)]),
+    "ngsgd_adamw_destroy": (c_int, [c_void_p]),
+    "ngsgd_adamw_step": (c_int, [c_void_p, POINTER(c_void_p), c_float, c_void_p, c_float, c_void_p, c_void_p]),
+    "ngsgd_adamw_arrays": (c_int, [c_void_p, POINTER(c_int64), POINTER(c_void_p), POINTER(c_void_p), POINTER(c_void_p)]),
+    "ngsgd_adamw_get_state": (c_int, [c_void_p, c_void_p, c_void_p, c_int32, c_void_p, c_void_p]),
+    "ngsgd_adamw_set_state": (c_int, [c_void_p, c_void_p, c_void_p, c_void_p, c_int64, c_void_p]),
     "ngsgd_workspace_bytes": (c_int, [POINTER(ngsgd_config), POINTER(c_size_t)]),
     "ngsgd_create": (c_int, [POINTER(ngsgd_config), c_void_p, c_size_t, POINTER(c_void_p)]),
     "ngsgd_destroy": (c_int, [c_void_p]),
@@ -224,6 +249,236 @@ def precondition_simple_static(M, alpha=4.0, epsilon=1e-20, gamma=None, rownorm2
                                                            epsilon, _ptr(gamma), _ptr(rownorm2),
                                                            _stream_ptr(stream)),
            "ngsgd_precondition_simple_static")
+
+
+def _type_of(dtype):
+    """NGSGD_FLOAT32 / _BFLOAT16 / _FLOAT16 of a torch dtype."""
+    name = str(dtype)
+    codes = {"torch.float32": NGSGD_FLOAT32, "torch.bfloat16": NGSGD_BFLOAT16, "torch.float16": NGSGD_FLOAT16}
+    if name not in codes:
+        raise ValueError(f"{name}: the types are float32, bfloat16 and float16")
+    return codes[name]
+
+
+def _require(condition, message):
+    """Argument checks that keep a kernel inside its buffers: they hold where assertions are switched off too."""
+    if not condition:
+        raise ValueError(message)
+
+
+def _check_tensor(t, name, dtype=None, numel=None):
+    """A dense tensor on the current device."""
+    import torch
+    _require(t.is_cuda and t.device.index == torch.cuda.current_device(), f"{name} is not on the current device")
+    _require(t.is_contiguous(), f"{name} is not dense")
+    _require(dtype is None or t.dtype == dtype, f"{name} is {t.dtype}, not {dtype}")
+    _require(numel is None or t.numel() == numel, f"{name} has {t.numel()} elements, not {numel}")
+
+
+def _allocate_on(stream):
+    """Outputs are allocated on the stream that writes them."""
+    import torch
+    return nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
+class LayerNorm:
+    """ngsgd_layernorm_forward / ngsgd_layernorm_backward: stateless, the workspace of the gradients is kept for reuse.
+
+    Inputs are float32, bfloat16 or float16, (..., dim) with up to max_rows rows; rows are dense (the last stride is 1) and,
+    as a matrix, may lie any distance apart.  Weight and bias (optional) have the input's type or float32, the same for both.  Calls on
+    one object are issued in order on one stream: the workspace is shared."""
+
+    def __init__(self, max_rows, dim, epsilon=1e-5):
+        import torch
+        self.lib = load_library()
+        self.max_rows, self.dim, self.epsilon = max_rows, dim, epsilon
+        nbytes = c_size_t(0)
+        _check(self.lib.ngsgd_layernorm_workspace_bytes(max_rows, dim, byref(nbytes)), "ngsgd_layernorm_workspace_bytes")
+        self.workspace_bytes = nbytes.value
+        self.workspace = torch.empty(nbytes.value, dtype=torch.uint8, device="cuda")
+
+    def _rows(self, t, name, like=None):
+        """(rows x dim view of t, leading dimension)"""
+        import torch
+        _require(t.is_cuda and t.device.index == torch.cuda.current_device(), f"{name} is not on the current device")
+        _require(t.dim() >= 1 and t.shape[-1] == self.dim, f"{name} does not end in {self.dim} columns")
+        _require(t.stride(-1) == 1 or self.dim == 1, f"{name}: rows are not dense")
+        _require(like is None or (t.dtype == like.dtype and t.shape == like.shape), f"{name} has another type or shape than x")
+        if t.dim() != 2:
+            t = t.view(t.numel() // self.dim, self.dim)
+        _require(t.shape[0] <= self.max_rows, f"{name} has more than {self.max_rows} rows")
+        return t, (t.stride(0) if t.shape[0] > 1 else self.dim)
+
+    def _vectors(self, x, *named):
+        """NGSGD_* type of the given weights (that of the first one present; float32 if there is none)."""
+        present = [(name, v) for name, v in named if v is not None]
+        if not present:
+            return NGSGD_FLOAT32
+        dtype = present[0][1].dtype
+        _require(dtype == x.dtype or str(dtype) == "torch.float32", f"{present[0][0]} is {dtype} for {x.dtype} rows")
+        for name, v in present:
+            _check_tensor(v, name, dtype, self.dim)
+        return _type_of(dtype)
+
+    def forward(self, x, weight=None, bias=None, out=None, mean=None, rstd=None, stream=None):
+        """(y, mean, rstd); y into `out` if given (which may be x), the rows' float32 mean and rstd into `mean` and `rstd`."""
+        import torch
+        rows, ldx = self._rows(x, "x")
+        weight_type = self._vectors(x, ("weight", weight), ("bias", bias))
+        with _allocate_on(stream):
+            out = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+            mean = torch.empty(rows.shape[0], dtype=torch.float32, device=x.device) if mean is None else mean
+            rstd = torch.empty(rows.shape[0], dtype=torch.float32, device=x.device) if rstd is None else rstd
+        out_rows, ldy = self._rows(out, "out", like=x)
+        _check_tensor(mean, "mean", torch.float32, rows.shape[0])
+        _check_tensor(rstd, "rstd", torch.float32, rows.shape[0])
+        _check(self.lib.ngsgd_layernorm_forward(_ptr(rows), ldx, _type_of(x.dtype), _ptr(weight), _ptr(bias), weight_type,
+                                                rows.shape[0], self.dim, self.epsilon, _ptr(out_rows), ldy, _ptr(mean),
+                                                _ptr(rstd), _stream_ptr(stream)), "ngsgd_layernorm_forward")
+        return out, mean, rstd
+
+    def backward(self, dy, x, mean, rstd, weight=None, needs=(True, True, True), dx=None, dweight=None, dbias=None,
+                 stream=None):
+        """(dx, dweight, dbias) for the derivative dy of y and the mean and rstd of the forward pass; None where `needs`
+        says so.  dx may be dy.  dweight and dbias are of the weight's type (float32 without a weight)."""
+        import torch
+        rows, ldx = self._rows(x, "x")
+        dy_rows, lddy = self._rows(dy, "dy", like=x)
+        _check_tensor(mean, "mean", torch.float32, rows.shape[0])
+        _check_tensor(rstd, "rstd", torch.float32, rows.shape[0])
+        weight_type = self._vectors(x, ("weight", weight), ("dweight", dweight), ("dbias", dbias))
+        vector_dtype = next((v.dtype for v in (weight, dweight, dbias) if v is not None), torch.float32)
+        with _allocate_on(stream):
+            dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if dx is None and needs[0] else dx
+            dweight = torch.empty(self.dim, dtype=vector_dtype, device=x.device) if dweight is None and needs[1] else dweight
+            dbias = torch.empty(self.dim, dtype=vector_dtype, device=x.device) if dbias is None and needs[2] else dbias
+        dx_rows, lddx = (None, self.dim) if dx is None else self._rows(dx, "dx", like=x)
+        _check(self.lib.ngsgd_layernorm_backward(_ptr(dy_rows), lddy, _ptr(rows), ldx, _type_of(x.dtype), _ptr(weight),
+                                                 weight_type, _ptr(mean), _ptr(rstd), rows.shape[0], self.dim, _ptr(dx_rows),
+                                                 lddx, _ptr(dweight), _ptr(dbias), _ptr(self.workspace),
+                                                 self.workspace_bytes, _stream_ptr(stream)), "ngsgd_layernorm_backward")
+        return dx, dweight, dbias
+
+
+class AdamW:
+    """ngsgd_adamw_*: one AdamW step over many tensors of one type per call, on the current device.
+
+    The parameters are dense tensors, updated in place where they lie.  weight_decay and rate (a factor on the learning rate) are
+    numbers or one number per tensor.  state_bits is 32 or 8; master keeps fp32 copies of parameters in 16 bits.  Calls on
+    one object are issued in order on one stream."""
+
+    def __init__(self, params, betas=(0.9, 0.999), epsilon=1e-8, weight_decay=0.0, rate=1.0, grad_dtype=None, state_bits=32,
+                 master=False):
+        import torch
+        self.handle = None
+        self.lib = load_library()
+        self.params = list(params)
+        n = len(self.params)
+        _require(n > 0, "no parameters")
+        dtype = self.params[0].dtype
+        for i, p in enumerate(self.params):
+            _check_tensor(p, f"parameter {i}", dtype)
+        self.grad_dtype = dtype if grad_dtype is None else grad_dtype
+        self.sizes = [p.numel() for p in self.params]
+        self.offsets, at = [], 0
+        for size in self.sizes:
+            self.offsets.append(at)
+            at += -(-size // 256) * 256
+
+        def per_tensor(value, name):
+            values = list(value) if isinstance(value, (list, tuple)) else [float(value)] * n
+            _require(len(values) == n, f"{len(values)} numbers in {name} for {n} tensors")
+            return (c_float * n)(*values)
+
+        cfg = ngsgd_adamw_config(n, (c_void_p * n)(*[p.data_ptr() for p in self.params]), (c_int64 * n)(*self.sizes),
+                                 per_tensor(weight_decay, "weight_decay"), per_tensor(rate, "rate"), _type_of(dtype),
+                                 _type_of(self.grad_dtype), state_bits, 1 if master else 0, betas[0], betas[1], epsilon)
+        nbytes = c_size_t(0)
+        _check(self.lib.ngsgd_adamw_workspace_bytes(byref(cfg), byref(nbytes)), "ngsgd_adamw_workspace_bytes")
+        self.workspace_bytes = nbytes.value
+        self.workspace = torch.empty(nbytes.value, dtype=torch.uint8, device="cuda")
+        h = c_void_p(0)
+        _check(self.lib.ngsgd_adamw_create(byref(cfg), _ptr(self.workspace), nbytes.value, byref(h)), "ngsgd_adamw_create")
+        self.handle = h
+        elements, m, v, fp32 = c_int64(0), c_void_p(0), c_void_p(0), c_void_p(0)
+        _check(self.lib.ngsgd_adamw_arrays(h, byref(elements), byref(m), byref(v), byref(fp32)), "ngsgd_adamw_arrays")
+        self.elements = elements.value
+
+        def view(address):
+            if not address.value:
+                return None
+            start = address.value - self.workspace.data_ptr()
+            return self.workspace[start:start + 4 * self.elements].view(torch.float32)
+
+        self._m, self._v = view(m), view(v)
+        self.master = view(fp32)          # flat, None without fp32 copies
+        self._grads = (c_void_p * n)()
+
+    def close(self):
+        if self.handle is not None:
+            self.lib.ngsgd_adamw_destroy(self.handle)
+        self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def step(self, grads, lr, grad_scale=None, stream=None):
+        """One step.  grads: a dense tensor of grad_dtype for each parameter, or None to leave that one as it is.  lr and grad_scale are
+        numbers or float32 tensors of one element on the device."""
+        import torch
+        _require(len(grads) == len(self.params), f"{len(grads)} gradients for {len(self.params)} tensors")
+        array, dtype, device = self._grads, self.grad_dtype, self.params[0].device
+        _require(device.index == torch.cuda.current_device(), "the parameters are not on the current device")
+        for i, g in enumerate(grads):
+            if g is None or self.sizes[i] == 0:
+                array[i] = None
+                continue
+            if g.dtype != dtype or g.numel() != self.sizes[i] or g.device != device or not g.is_contiguous():
+                raise ValueError(f"gradient {i}: {g.dtype}, {g.numel()} elements on {g.device}, for {dtype}, {self.sizes[i]} on "
+                                 f"{device}, dense")
+            array[i] = g.data_ptr()
+        factors = []
+        for name, value in (("lr", lr), ("grad_scale", grad_scale)):
+            if isinstance(value, torch.Tensor):
+                _check_tensor(value, name, torch.float32, 1)
+                factors += [1.0, c_void_p(value.data_ptr())]
+            else:
+                factors += [1.0 if value is None else float(value), c_void_p(0)]
+        _check(self.lib.ngsgd_adamw_step(self.handle, array, *factors, _stream_ptr(stream)), "ngsgd_adamw_step")
+
+    def state(self, dtype=None, stream=None):
+        """(m, v), flat; tensor k's are [offsets[k] : offsets[k] + sizes[k]].  With 32 bits the arrays themselves (or copies in
+        bfloat16, if asked for); with 8 bits the values of the codes, in float32 or in bfloat16, which holds them exactly."""
+        import torch
+        dtype = torch.float32 if dtype is None else dtype
+        if self._m is not None and dtype == torch.float32:
+            return self._m, self._v
+        with _allocate_on(stream):
+            m, v = (torch.empty(self.elements, dtype=dtype, device=self.workspace.device) for _ in range(2))
+        _check(self.lib.ngsgd_adamw_get_state(self.handle, _ptr(m), _ptr(v), _type_of(dtype), c_void_p(0), _stream_ptr(stream)),
+               "ngsgd_adamw_get_state")
+        return m, v
+
+    def set_state(self, m, v, t, master=None, stream=None):
+        """Installs flat float32 moments (None: zeros) and the step count; the fp32 copies from `master` (flat), which is rounded to the
+        parameters too, or from the parameters."""
+        import torch
+        for name, a in (("m", m), ("v", v), ("master", master)):
+            if a is not None:
+                _check_tensor(a, name, torch.float32, self.elements)
+        _check(self.lib.ngsgd_adamw_set_state(self.handle, _ptr(m), _ptr(v), _ptr(master), int(t), _stream_ptr(stream)),
+               "ngsgd_adamw_set_state")
+
+    def steps(self):
+        """The step count; waits for the stream."""
+        import torch
+        t = torch.empty(1, dtype=torch.int64, device=self.workspace.device)
+        _check(self.lib.ngsgd_adamw_get_state(self.handle, c_void_p(0), c_void_p(0), NGSGD_FLOAT32, _ptr(t), _stream_ptr()),
+               "ngsgd_adamw_get_state")
+        return int(t.item())
 
 
 class Network:

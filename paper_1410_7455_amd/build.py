@@ -8,7 +8,7 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 LIB_PATH = os.path.join(HERE, "libngsgd.so")
-SOURCES = [os.path.join(HERE, "csrc", "ngsgd.hip")]
+SOURCES = [os.path.join(HERE, "csrc", name) for name in ("ngsgd.hip", "layer_norm.hip", "adamw.hip")]
 
 HIPCC_FLAGS = [
     "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-shared",

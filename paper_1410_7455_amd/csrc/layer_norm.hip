@@ -1,0 +1,107 @@
+// C ABI of layer norm: argument checks and launches.  Declarations and contracts are in include/ngsgd.h.
+#include "layer_norm.h"
+
+#include <algorithm>
+#include <cmath>
+
+#include "host.h"
+
+using namespace ngsgd;
+
+namespace {
+
+constexpr int kNormGrid = 2048;     // workgroups that walk over the rows
+constexpr int kNormGroups = 512;    // most groups of rows that are summed on their own
+
+inline int type_bytes(const int type) { return type == NGSGD_FLOAT32 ? 4 : 2; }
+inline bool known_type(const int type) { return type == NGSGD_FLOAT32 || type == NGSGD_BFLOAT16 || type == NGSGD_FLOAT16; }
+inline bool on_element(const void* p, const int type) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(type_bytes(type) - 1)) == 0; }
+
+int norm_groups(const int64_t N) { return (int)std::min<int64_t>(kNormGroups, std::max<int64_t>(1, (N + 7) / 8)); }
+
+// f(element, weight element) for the types of a call
+template <typename F>
+int with_types(const int type, const int weight_type, F f) {
+  if (type == NGSGD_FLOAT32) return f(float(), float());
+  if (type == NGSGD_BFLOAT16) return weight_type == NGSGD_FLOAT32 ? f(bf16(), float()) : f(bf16(), bf16());
+  return weight_type == NGSGD_FLOAT32 ? f(fp16(), float()) : f(fp16(), fp16());
+}
+
+int check_types(const int type, const int weight_type, const int64_t N, const int32_t D) {
+  if (!known_type(type) || !known_type(weight_type) || (weight_type != type && weight_type != NGSGD_FLOAT32)) return NGSGD_EINVAL;
+  return N < 0 || D < 1 ? NGSGD_EINVAL : NGSGD_OK;
+}
+// A matrix argument: present, rows that do not overlap, whole elements.
+bool good_matrix(const void* p, const int64_t ld, const int type, const int64_t N, const int32_t D) {
+  if (N == 0) return true;
+  return p != nullptr && on_element(p, type) && (ld >= D || N == 1) && ld >= 0 && ld <= INT64_MAX / 8 / N;
+}
+
+}  // namespace
+
+extern "C" int ngsgd_layernorm_forward(const void* dev_x, int64_t ldx, int32_t type, const void* dev_weight, const void* dev_bias,
+                                       int32_t weight_type, int64_t N, int32_t D, float epsilon, void* dev_y, int64_t ldy, float* dev_mean,
+                                       float* dev_rstd, void* hip_stream) {
+  NG_TRY(check_types(type, weight_type, N, D));
+  if (!(epsilon >= 0.f) || !std::isfinite(epsilon)) return NGSGD_EINVAL;
+  if (!good_matrix(dev_x, ldx, type, N, D) || !good_matrix(dev_y, ldy, type, N, D)) return NGSGD_EINVAL;
+  if (!on_element(dev_weight, weight_type) || !on_element(dev_bias, weight_type)) return NGSGD_EINVAL;
+  if (!on_element(dev_mean, NGSGD_FLOAT32) || !on_element(dev_rstd, NGSGD_FLOAT32)) return NGSGD_EINVAL;
+  if (N == 0) return NGSGD_OK;
+  const LayerNormForward a{dev_x, ldx, dev_weight, dev_bias, dev_y, ldy, dev_mean, dev_rstd, N, D, epsilon};
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  return with_types(type, weight_type, [&](auto t, auto w) -> int {
+    hipLaunchKernelGGL((layernorm_forward_wide_kernel<decltype(t), decltype(w)>), dim3((unsigned)std::min<int64_t>(N, kNormGrid)),
+                       dim3(kNormThreads), 0, s, a);
+    LAUNCH_CHECK();
+    return NGSGD_OK;
+  });
+}
+
+extern "C" int ngsgd_layernorm_workspace_bytes(int64_t max_rows, int32_t D, size_t* out_bytes) {
+  if (out_bytes == nullptr || max_rows < 0 || D < 1) return NGSGD_EINVAL;
+  Carver c(nullptr);
+  (void)c.take<float>((size_t)norm_groups(max_rows) * 2 * D);
+  *out_bytes = align_up(c.off, 256);
+  return NGSGD_OK;
+}
+
+extern "C" int ngsgd_layernorm_backward(const void* dev_dy, int64_t lddy, const void* dev_x, int64_t ldx, int32_t type, const void* dev_weight,
+                                        int32_t weight_type, const float* dev_mean, const float* dev_rstd, int64_t N, int32_t D, void* dev_dx,
+                                        int64_t lddx, void* dev_dweight, void* dev_dbias, void* dev_workspace, size_t workspace_bytes,
+                                        void* hip_stream) {
+  NG_TRY(check_types(type, weight_type, N, D));
+  const bool sums = dev_dweight != nullptr || dev_dbias != nullptr;
+  if (!good_matrix(dev_dy, lddy, type, N, D) || !good_matrix(dev_x, ldx, type, N, D)) return NGSGD_EINVAL;
+  if (dev_dx != nullptr && !good_matrix(dev_dx, lddx, type, N, D)) return NGSGD_EINVAL;
+  if (dev_dx == nullptr && !sums) return NGSGD_EINVAL;
+  if (N > 0 && (dev_mean == nullptr || dev_rstd == nullptr)) return NGSGD_EINVAL;
+  if (!on_element(dev_mean, NGSGD_FLOAT32) || !on_element(dev_rstd, NGSGD_FLOAT32)) return NGSGD_EINVAL;
+  if (!on_element(dev_weight, weight_type) || !on_element(dev_dweight, weight_type) || !on_element(dev_dbias, weight_type)) return NGSGD_EINVAL;
+  if (sums) {
+    if (dev_workspace == nullptr || (reinterpret_cast<uintptr_t>(dev_workspace) & 255u)) return NGSGD_EINVAL;
+    size_t need = 0;
+    NG_TRY(ngsgd_layernorm_workspace_bytes(N, D, &need));
+    if (workspace_bytes < need) return NGSGD_ENOMEM;
+  }
+  LayerNormBackward a{dev_dy, lddy, dev_x, ldx, dev_weight, dev_mean, dev_rstd, dev_dx, lddx, dev_dweight, dev_dbias, N, D,
+                      static_cast<float*>(dev_workspace), norm_groups(N)};
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  return with_types(type, weight_type, [&](auto t, auto w) -> int {
+    using T = decltype(t);
+    using W = decltype(w);
+    const unsigned columns = ((unsigned)D + kNormThreads - 1) / kNormThreads;
+    // the sums first: the gradient may overwrite dy or x
+    if (sums) {
+      hipLaunchKernelGGL(layernorm_backward_columns_kernel<T>, dim3(columns, a.groups), dim3(kNormThreads), 0, s, a);
+      LAUNCH_CHECK();
+      hipLaunchKernelGGL(layernorm_backward_sum_kernel<W>, dim3(columns, 2), dim3(kNormThreads), 0, s, a);
+      LAUNCH_CHECK();
+    }
+    if (a.dx != nullptr && N > 0) {
+      hipLaunchKernelGGL((layernorm_backward_rows_kernel<T, W>), dim3((unsigned)std::min<int64_t>(N, kNormGrid)), dim3(kNormThreads), 0, s, a);
+      LAUNCH_CHECK();
+    }
+    return NGSGD_OK;
+  });
+}
