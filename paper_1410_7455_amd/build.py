@@ -4,6 +4,7 @@ from __future__ import annotations
 import os
 import shutil
 import subprocess
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -11,7 +12,7 @@ LIB_PATH = os.path.join(HERE, "libngsgd.so")
 SOURCES = [os.path.join(HERE, "csrc", name) for name in ("ngsgd.hip", "layer_norm.hip", "adamw.hip")]
 
 HIPCC_FLAGS = [
-    "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-shared",
+    "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC",
     # no packed fp32 instructions: some of their forms have given wrong results on this hardware
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wno-unused-result",
@@ -26,15 +27,30 @@ def find_hipcc() -> str:
 
 
 def build(verbose: bool = False) -> str:
-    cmd = [find_hipcc(), *HIPCC_FLAGS, "-I", os.path.join(ROOT, "include"), "-I", os.path.join(HERE, "csrc"),
-           "-o", LIB_PATH, *SOURCES]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    proc = subprocess.run(cmd, capture_output=True, text=True)
-    if proc.returncode != 0:
-        raise RuntimeError("hipcc failed:\n" + proc.stdout + proc.stderr)
-    if verbose and proc.stderr.strip():
-        print(proc.stderr)
+    """Compiles every source (side by side) and links them; raises with the compiler's output if one fails."""
+    hipcc = find_hipcc()
+    objects = os.path.join(HERE, "_build")
+    os.makedirs(objects, exist_ok=True)
+    include = ["-I", os.path.join(ROOT, "include"), "-I", os.path.join(HERE, "csrc")]
+
+    def run(cmd):
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        return subprocess.run(cmd, capture_output=True, text=True)
+
+    def compile_one(source):
+        return run([hipcc, *HIPCC_FLAGS, *include, "-c", "-o", os.path.join(objects, os.path.basename(source) + ".o"), source])
+
+    with ThreadPoolExecutor(max_workers=min(len(SOURCES), os.cpu_count() or 1)) as pool:
+        results = list(pool.map(compile_one, SOURCES))
+    if all(r.returncode == 0 for r in results):
+        results.append(run([hipcc, "-shared", "-fPIC", "--offload-arch=gfx950", "-o", LIB_PATH,
+                            *(os.path.join(objects, os.path.basename(s) + ".o") for s in SOURCES)]))
+    for proc in results:
+        if proc.returncode != 0:
+            raise RuntimeError("hipcc failed:\n" + proc.stdout + proc.stderr)
+        if verbose and proc.stderr.strip():
+            print(proc.stderr)
     return LIB_PATH
 
 

@@ -10,7 +10,7 @@ using bf16 = __bf16;
 using fp16 = _Float16;
 
 template <typename T, int V>
-struct alignas(sizeof(T) * V) Pack {
+struct alignas(sizeof(T) * V < 16 ? sizeof(T) * V : 16) Pack {
   T v[V];
 };
 
@@ -25,11 +25,14 @@ template <int CTRL>
 __device__ __forceinline__ float dpp_add_f32(const float v) {
   return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
 }
-__device__ __forceinline__ float wave_sum_f32(float v) {
+__device__ __forceinline__ float row16_sum_f32(float v) {
   v = dpp_add_f32<0xB1>(v);    // quad_perm [1,0,3,2]
   v = dpp_add_f32<0x4E>(v);    // quad_perm [2,3,0,1]
   v = dpp_add_f32<0x141>(v);   // row_half_mirror
-  v = dpp_add_f32<0x140>(v);   // row_mirror
+  return dpp_add_f32<0x140>(v);   // row_mirror
+}
+__device__ __forceinline__ float wave_sum_f32(float v) {
+  v = row16_sum_f32(v);
   v += __shfl_xor(v, 16);
   return v + __shfl_xor(v, 32);
 }

@@ -8,6 +8,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "elements.h"
 
 namespace ngsgd {
@@ -44,8 +46,231 @@ struct LayerNormBackward {
   int groups;
 };
 
+// ---- rows that a group of threads holds in registers ------------------------------------------------
+// TPR threads share a row and E of its columns each, as E / VEC pieces of VEC neighbours; a workgroup of NT threads walks over the rows,
+// NT / TPR at a time.  A thread keeps its columns of the weight, the bias and (backward) of the sums over the rows in registers,
+// and requests its next row before it works on the one that it has.
+template <typename T, int VEC_, int E_, int TPR_, int NT_>
+struct RowShape {
+  static constexpr int VEC = VEC_, E = E_, TPR = TPR_, NT = NT_, K = E / VEC, ROWS = NT / TPR;
+  static_assert(E % VEC == 0 && NT % TPR == 0 && (TPR == NT || TPR <= 64), "a row belongs to a workgroup or within a wavefront");
+  __device__ static int member() { return threadIdx.x % TPR; }
+  __device__ static int row() { return threadIdx.x / TPR; }
+  __device__ static int column(const int k) { return (k * TPR + member()) * VEC; }
+};
+
+// A thread's columns of a row as they lie in memory, two 16-bit elements to a register where pieces are loaded whole.
+template <typename S, typename T>
+struct RowPart {
+  static constexpr bool kWords = S::VEC > 1 && sizeof(T) == 2;
+  using Word = std::conditional_t<kWords, uint32_t, T>;
+  static constexpr int PER = kWords ? 2 : 1;   // elements in a word
+  Word v[S::E / PER];
+
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < S::E / PER; ++i) v[i] = Word(0);
+  }
+  // Zeros behind column D.
+  __device__ __forceinline__ void load(const T* p, const int D) {
+#pragma unroll
+    for (int k = 0; k < S::K; ++k) {
+      const int c = S::column(k);
+      if constexpr (S::VEC > 1) {
+        constexpr int WORDS = S::VEC / PER;
+        if (c + S::VEC <= D) {
+          const Pack<Word, WORDS> q = *reinterpret_cast<const Pack<Word, WORDS>*>(p + c);
+#pragma unroll
+          for (int j = 0; j < WORDS; ++j) v[k * WORDS + j] = q.v[j];
+        } else {
+          Pack<T, S::VEC> q;
+#pragma unroll
+          for (int j = 0; j < S::VEC; ++j) q.v[j] = c + j < D ? p[c + j] : T(0.f);
+          const Pack<Word, WORDS> w = __builtin_bit_cast(Pack<Word, WORDS>, q);
+#pragma unroll
+          for (int j = 0; j < WORDS; ++j) v[k * WORDS + j] = w.v[j];
+        }
+      } else {
+        v[k] = c < D ? p[c] : T(0.f);
+      }
+    }
+  }
+  __device__ __forceinline__ float get(const int e) const {
+    if constexpr (kWords)
+      return to_float(__builtin_bit_cast(T, (uint16_t)(e & 1 ? v[e / 2] >> 16 : v[e / 2])));
+    else
+      return to_float(v[e]);
+  }
+};
+template <typename S, typename T>
+__device__ __forceinline__ void store_row(const float (&v)[S::E], T* p, const int D) {
+#pragma unroll
+  for (int k = 0; k < S::K; ++k) {
+    const int c = S::column(k);
+    if (S::VEC > 1 && c + S::VEC <= D) {
+      Pack<T, S::VEC> o;
+#pragma unroll
+      for (int j = 0; j < S::VEC; ++j) o.v[j] = from_float<T>(v[k * S::VEC + j]);
+      *reinterpret_cast<Pack<T, S::VEC>*>(p + c) = o;
+    } else {
+#pragma unroll
+      for (int j = 0; j < S::VEC; ++j)
+        if (c + j < D) p[c + j] = from_float<T>(v[k * S::VEC + j]);
+    }
+  }
+}
+template <typename S>
+using RowScratch = float[2][2][S::TPR <= 64 ? 1 : S::TPR / 64];
+
+// Sums over the threads of a row.
+template <typename S>
+__device__ __forceinline__ float row_sum(float v, RowScratch<S>& red, const int parity) {
+  if constexpr (S::TPR == 16)
+    return row16_sum_f32(v);
+  else
+    return block_sum_f32<S::TPR / 64>(v, red, parity);
+}
+template <typename S>
+__device__ __forceinline__ void row_sum_pair(float& a, float& b, RowScratch<S>& red, const int parity) {
+  if constexpr (S::TPR == 16) {
+    a = row16_sum_f32(a);
+    b = row16_sum_f32(b);
+  } else {
+    block_sum_pair_f32<S::TPR / 64>(a, b, red, parity);
+  }
+}
+
+template <typename T, typename W, typename S>
+__global__ __launch_bounds__(S::NT) void layernorm_forward_kernel(const LayerNormForward a) {
+  __shared__ RowScratch<S> red;
+  constexpr int E = S::E;
+  RowPart<S, W> w, b;
+  if (a.w != nullptr) w.load(static_cast<const W*>(a.w), a.D);
+  if (a.b != nullptr) b.load(static_cast<const W*>(a.b), a.D);
+  const int64_t step = (int64_t)gridDim.x * S::ROWS;
+  int64_t row = (int64_t)blockIdx.x * S::ROWS + S::row();
+  RowPart<S, T> next;
+  next.clear();
+  if (row < a.N) next.load(static_cast<const T*>(a.x) + row * a.ldx, a.D);
+  for (int64_t first = (int64_t)blockIdx.x * S::ROWS; first < a.N; first += step, row += step) {   // (uniform in the workgroup)
+    float x[E];
+    float s = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      x[e] = next.get(e);
+      s += x[e];
+    }
+    if (row + step < a.N) next.load(static_cast<const T*>(a.x) + (row + step) * a.ldx, a.D);
+    const float mean = row_sum<S>(s, red, 0) / (float)a.D;
+    float q = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      x[e] = S::column(e / S::VEC) + e % S::VEC < a.D ? x[e] - mean : 0.f;
+      q += x[e] * x[e];
+    }
+    const float rstd = 1.f / sqrtf(row_sum<S>(q, red, 1) / (float)a.D + a.eps);
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      x[e] *= rstd;
+      if (a.w != nullptr) x[e] *= w.get(e);
+      if (a.b != nullptr) x[e] += b.get(e);
+    }
+    if (row < a.N) {
+      store_row<S>(x, static_cast<T*>(a.y) + row * a.ldy, a.D);
+      if (S::member() == 0) {
+        if (a.mean != nullptr) a.mean[row] = mean;
+        if (a.rstd != nullptr) a.rstd[row] = rstd;
+      }
+    }
+  }
+}
+
+// What a thread needs of a row; zeros behind the last one.
+template <typename S, typename T>
+struct BackwardRow {
+  RowPart<S, T> x, dy;
+  float mean, rstd;
+  __device__ __forceinline__ void load(const LayerNormBackward& a, const int64_t r) {
+    if (r < a.N) {
+      x.load(static_cast<const T*>(a.x) + r * a.ldx, a.D);
+      dy.load(static_cast<const T*>(a.dy) + r * a.lddy, a.D);
+      mean = a.mean[r];
+      rstd = a.rstd[r];
+    } else {
+      x.clear();
+      dy.clear();
+      mean = rstd = 0.f;
+    }
+  }
+};
+
+// Sums of a workgroup's rows go to part[workgroup][dw, db][D].
+template <typename T, typename W, typename S>
+__global__ __launch_bounds__(S::NT) void layernorm_backward_kernel(const LayerNormBackward a) {
+  __shared__ RowScratch<S> red;
+  __shared__ float sums[S::ROWS > 1 ? S::NT * S::E : 1];
+  constexpr int E = S::E;
+  RowPart<S, W> w;
+  if (a.w != nullptr) w.load(static_cast<const W*>(a.w), a.D);
+  float dw[E], db[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) dw[e] = db[e] = 0.f;
+  const int64_t step = (int64_t)gridDim.x * S::ROWS;
+  int64_t row = (int64_t)blockIdx.x * S::ROWS + S::row();
+  BackwardRow<S, T> next;
+  next.load(a, row);
+  int parity = 0;
+  for (int64_t first = (int64_t)blockIdx.x * S::ROWS; first < a.N; first += step, row += step, parity ^= 1) {   // (uniform in the workgroup)
+    float xhat[E], g[E];
+    const float rstd = next.rstd;
+    float c1 = 0.f, c2 = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      xhat[e] = (next.x.get(e) - next.mean) * rstd;
+      g[e] = next.dy.get(e);
+      dw[e] += g[e] * xhat[e];
+      db[e] += g[e];
+      if (a.w != nullptr) g[e] *= w.get(e);
+      c1 += g[e];
+      c2 += g[e] * xhat[e];
+    }
+    next.load(a, row + step);
+    if (a.dx != nullptr) {
+      row_sum_pair<S>(c1, c2, red, parity);
+      c1 /= (float)a.D;
+      c2 /= (float)a.D;
+#pragma unroll
+      for (int e = 0; e < E; ++e) g[e] = rstd * (g[e] - c1 - xhat[e] * c2);
+      if (row < a.N) store_row<S>(g, static_cast<T*>(a.dx) + row * a.lddx, a.D);
+    }
+  }
+  if (a.part == nullptr) return;
+  float* const part = a.part + (size_t)blockIdx.x * 2 * a.D;
+  if (S::ROWS == 1) {
+    store_row<S>(dw, part, a.D);
+    store_row<S>(db, part + a.D, a.D);
+    return;
+  }
+  // the rows that the workgroup worked on side by side, in order
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < E; ++e) sums[(S::row() * S::TPR + S::member()) * E + e] = which == 0 ? dw[e] : db[e];
+    __syncthreads();
+    for (int i = threadIdx.x; i < S::TPR * E; i += S::NT) {
+      float v = 0.f;
+#pragma unroll
+      for (int r = 0; r < S::ROWS; ++r) v += sums[r * S::TPR * E + i];
+      const int e = i % E, c = ((e / S::VEC) * S::TPR + i / E) * S::VEC + e % S::VEC;
+      if (c < a.D) part[(size_t)which * a.D + c] = v;
+    }
+  }
+}
+
 // ---- rows of any width, read from memory in every pass ---------------------------------------------
 constexpr int kNormThreads = 256;
+constexpr int kRegisterColumns = 16384;   // the widest rows of the kernels above
 
 template <typename T, typename W>
 __global__ __launch_bounds__(kNormThreads) void layernorm_forward_wide_kernel(const LayerNormForward a) {

@@ -10,14 +10,58 @@ using namespace ngsgd;
 
 namespace {
 
-constexpr int kNormGrid = 2048;     // workgroups that walk over the rows
+constexpr int kNormGrid = 2048;     // workgroups that walk over rows wider than registers hold
 constexpr int kNormGroups = 512;    // most groups of rows that are summed on their own
 
 inline int type_bytes(const int type) { return type == NGSGD_FLOAT32 ? 4 : 2; }
 inline bool known_type(const int type) { return type == NGSGD_FLOAT32 || type == NGSGD_BFLOAT16 || type == NGSGD_FLOAT16; }
 inline bool on_element(const void* p, const int type) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(type_bytes(type) - 1)) == 0; }
 
-int norm_groups(const int64_t N) { return (int)std::min<int64_t>(kNormGroups, std::max<int64_t>(1, (N + 7) / 8)); }
+// The threads of a row by its width: as few as hold it with 8 or 16 columns each.
+struct RowPlan {
+  int tpr, e, nt;   // tpr 0: from memory
+  int rows() const { return nt / tpr; }
+};
+RowPlan row_plan(const int D) {
+  if (D <= 128) return {16, 8, 256};
+  if (D <= 512) return {64, 8, 256};
+  if (D <= 1024) return {64, 16, 256};
+  if (D <= 2048) return {256, 8, 256};
+  if (D <= 4096) return {256, 16, 256};
+  if (D <= 8192) return {512, 16, 512};
+  return D <= kRegisterColumns ? RowPlan{1024, 16, 1024} : RowPlan{0, 0, kNormThreads};
+}
+// Groups of rows whose sums are formed on their own: the workgroups of the backward pass.
+int norm_groups(const int64_t N, const int D) {
+  const RowPlan p = row_plan(D);
+  if (p.tpr == 0) return (int)std::min<int64_t>(kNormGroups, std::max<int64_t>(1, (N + 7) / 8));
+  const int64_t rows = 4 * p.rows();
+  return (int)std::min<int64_t>(std::max(256, kNormGroups * 256 / p.nt), std::max<int64_t>(1, (N + rows - 1) / rows));
+}
+unsigned forward_grid(const int64_t N, const RowPlan& p) {
+  return (unsigned)std::min<int64_t>(256 * 1536 / p.nt, (N + p.rows() - 1) / p.rows());
+}
+
+// f(shape) for rows of this width; pieces of 16 bytes, or of an element where an address or a leading dimension is not a multiple of that
+template <typename T, int VEC, typename F>
+void with_row_shape(const RowPlan& p, F f) {
+  if (p.tpr == 16) return f(RowShape<T, VEC, 8, 16, 256>());
+  if (p.tpr == 64 && p.e == 8) return f(RowShape<T, VEC, 8, 64, 256>());
+  if (p.tpr == 64) return f(RowShape<T, VEC, 16, 64, 256>());
+  if (p.tpr == 256 && p.e == 8) return f(RowShape<T, VEC, 8, 256, 256>());
+  if (p.tpr == 256) return f(RowShape<T, VEC, 16, 256, 256>());
+  if (p.tpr == 512) return f(RowShape<T, VEC, 16, 512, 512>());
+  f(RowShape<T, VEC, 16, 1024, 1024>());
+}
+template <typename T>
+bool rows_aligned(const void* p, const int64_t ld, const int64_t N) {
+  return aligned16(p) && (N == 1 || ld % (int64_t)(16 / sizeof(T)) == 0);
+}
+template <typename T, typename F>
+void with_row_shape(const RowPlan& p, const bool aligned, F f) {
+  if (aligned) return with_row_shape<T, 16 / sizeof(T)>(p, f);
+  with_row_shape<T, 1>(p, f);
+}
 
 // f(element, weight element) for the types of a call
 template <typename F>
@@ -51,8 +95,17 @@ extern "C" int ngsgd_layernorm_forward(const void* dev_x, int64_t ldx, int32_t t
   const LayerNormForward a{dev_x, ldx, dev_weight, dev_bias, dev_y, ldy, dev_mean, dev_rstd, N, D, epsilon};
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   return with_types(type, weight_type, [&](auto t, auto w) -> int {
-    hipLaunchKernelGGL((layernorm_forward_wide_kernel<decltype(t), decltype(w)>), dim3((unsigned)std::min<int64_t>(N, kNormGrid)),
-                       dim3(kNormThreads), 0, s, a);
+    using T = decltype(t);
+    using W = decltype(w);
+    const RowPlan plan = row_plan(D);
+    if (plan.tpr == 0) {
+      hipLaunchKernelGGL((layernorm_forward_wide_kernel<T, W>), dim3((unsigned)std::min<int64_t>(N, kNormGrid)), dim3(kNormThreads), 0, s, a);
+    } else {
+      const bool aligned = rows_aligned<T>(a.x, a.ldx, N) && rows_aligned<T>(a.y, a.ldy, N) && aligned16(a.w) && aligned16(a.b);
+      with_row_shape<T>(plan, aligned, [&](auto shape) {
+        hipLaunchKernelGGL((layernorm_forward_kernel<T, W, decltype(shape)>), dim3(forward_grid(N, plan)), dim3(plan.nt), 0, s, a);
+      });
+    }
     LAUNCH_CHECK();
     return NGSGD_OK;
   });
@@ -61,7 +114,7 @@ extern "C" int ngsgd_layernorm_forward(const void* dev_x, int64_t ldx, int32_t t
 extern "C" int ngsgd_layernorm_workspace_bytes(int64_t max_rows, int32_t D, size_t* out_bytes) {
   if (out_bytes == nullptr || max_rows < 0 || D < 1) return NGSGD_EINVAL;
   Carver c(nullptr);
-  (void)c.take<float>((size_t)norm_groups(max_rows) * 2 * D);
+  (void)c.take<float>((size_t)norm_groups(max_rows, D) * 2 * D);
   *out_bytes = align_up(c.off, 256);
   return NGSGD_OK;
 }
@@ -84,22 +137,34 @@ extern "C" int ngsgd_layernorm_backward(const void* dev_dy, int64_t lddy, const 
     NG_TRY(ngsgd_layernorm_workspace_bytes(N, D, &need));
     if (workspace_bytes < need) return NGSGD_ENOMEM;
   }
+  const RowPlan plan = row_plan(D);
   LayerNormBackward a{dev_dy, lddy, dev_x, ldx, dev_weight, dev_mean, dev_rstd, dev_dx, lddx, dev_dweight, dev_dbias, N, D,
-                      static_cast<float*>(dev_workspace), norm_groups(N)};
+                      sums ? static_cast<float*>(dev_workspace) : nullptr, N > 0 ? norm_groups(N, D) : 0};
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   return with_types(type, weight_type, [&](auto t, auto w) -> int {
     using T = decltype(t);
     using W = decltype(w);
     const unsigned columns = ((unsigned)D + kNormThreads - 1) / kNormThreads;
-    // the sums first: the gradient may overwrite dy or x
-    if (sums) {
-      hipLaunchKernelGGL(layernorm_backward_columns_kernel<T>, dim3(columns, a.groups), dim3(kNormThreads), 0, s, a);
+    if (N > 0 && plan.tpr != 0) {
+      const bool aligned = rows_aligned<T>(a.x, a.ldx, N) && rows_aligned<T>(a.dy, a.lddy, N) && rows_aligned<T>(a.dx, a.lddx, N) &&
+                           aligned16(a.w) && (D % 4 == 0 || a.part == nullptr);   // (a row of part is D floats)
+      with_row_shape<T>(plan, aligned, [&](auto shape) {
+        hipLaunchKernelGGL((layernorm_backward_kernel<T, W, decltype(shape)>), dim3(a.groups), dim3(plan.nt), 0, s, a);
+      });
       LAUNCH_CHECK();
-      hipLaunchKernelGGL(layernorm_backward_sum_kernel<W>, dim3(columns, 2), dim3(kNormThreads), 0, s, a);
-      LAUNCH_CHECK();
+    } else if (N > 0) {
+      // the sums first: the gradient may overwrite dy
+      if (sums) {
+        hipLaunchKernelGGL(layernorm_backward_columns_kernel<T>, dim3(columns, a.groups), dim3(kNormThreads), 0, s, a);
+        LAUNCH_CHECK();
+      }
+      if (a.dx != nullptr) {
+        hipLaunchKernelGGL((layernorm_backward_rows_kernel<T, W>), dim3((unsigned)std::min<int64_t>(N, kNormGrid)), dim3(kNormThreads), 0, s, a);
+        LAUNCH_CHECK();
+      }
     }
-    if (a.dx != nullptr && N > 0) {
-      hipLaunchKernelGGL((layernorm_backward_rows_kernel<T, W>), dim3((unsigned)std::min<int64_t>(N, kNormGrid)), dim3(kNormThreads), 0, s, a);
+    if (sums) {
+      hipLaunchKernelGGL(layernorm_backward_sum_kernel<W>, dim3(columns, 2), dim3(kNormThreads), 0, s, a);
       LAUNCH_CHECK();
     }
     return NGSGD_OK;
