@@ -164,7 +164,7 @@ extern "C" int ngsgd_layernorm_backward(const void* dev_dy, int64_t lddy, const 
       }
     }
     if (sums) {
-      hipLaunchKernelGGL(layernorm_backward_sum_kernel<W>, dim3(columns, 2), dim3(kNormThreads), 0, s, a);
+      hipLaunchKernelGGL(layernorm_backward_sum_kernel<W>, dim3((unsigned)((2 * (int64_t)D + kSumColumns - 1) / kSumColumns)), dim3(kSumThreads), 0, s, a);
       LAUNCH_CHECK();
     }
     return NGSGD_OK;
