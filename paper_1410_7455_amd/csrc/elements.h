@@ -9,8 +9,10 @@ namespace ngsgd {
 using bf16 = __bf16;
 using fp16 = _Float16;
 
+// V neighbours in memory, on any element's boundary: the target's vector loads and stores take addresses that are multiples of
+// nothing, so one path serves every leading dimension and every start of a matrix.
 template <typename T, int V>
-struct alignas(sizeof(T) * V < 16 ? sizeof(T) * V : 16) Pack {
+struct __attribute__((packed, aligned(sizeof(T)))) Pack {
   T v[V];
 };
 
@@ -31,41 +33,36 @@ __device__ __forceinline__ float row16_sum_f32(float v) {
   v = dpp_add_f32<0x141>(v);   // row_half_mirror
   return dpp_add_f32<0x140>(v);   // row_mirror
 }
-__device__ __forceinline__ float wave_sum_f32(float v) {
-  v = row16_sum_f32(v);
-  v += __shfl_xor(v, 16);
-  return v + __shfl_xor(v, 32);
+// The two halves of 32 lanes, or of each half the two of 16, with their lanes exchanged: one instruction gives both addends.
+__device__ __forceinline__ float half16_add_f32(const float v) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+  return __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
 }
+__device__ __forceinline__ float half32_add_f32(const float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+  return __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
+}
+__device__ __forceinline__ float wave_sum_f32(const float v) { return half32_add_f32(half16_add_f32(row16_sum_f32(v))); }
 
-// Two sums over a workgroup of WAVES wavefronts at the price of one barrier: `red` is used in turn by parity, so that a wavefront that is
-// ahead writes into the other half.
-template <int WAVES>
-__device__ __forceinline__ void block_sum_pair_f32(float& a, float& b, float (*red)[2][WAVES], const int parity) {
+// Sums over a workgroup of up to 16 wavefronts at the price of one barrier: `red` is used in turn by parity, so that a wavefront that is
+// ahead writes into the other half.  A lane reads one wavefront's sums, and the 16 lanes of a row add them.
+constexpr int kMaxWaves = 16;
+using BlockScratch = Pack<float, 2>[2][kMaxWaves];
+
+__device__ __forceinline__ void block_sum_pair_f32(float& a, float& b, BlockScratch& red, const int parity) {
   a = wave_sum_f32(a);
   b = wave_sum_f32(b);
-  if (WAVES == 1) return;
-  if ((threadIdx.x & 63) == 0) {
-    red[parity][0][threadIdx.x >> 6] = a;
-    red[parity][1][threadIdx.x >> 6] = b;
-  }
+  if ((threadIdx.x & 63) == 0) red[parity][threadIdx.x >> 6] = Pack<float, 2>{{a, b}};
   __syncthreads();
-  a = red[parity][0][0];
-  b = red[parity][1][0];
-#pragma unroll
-  for (int w = 1; w < WAVES; ++w) {
-    a += red[parity][0][w];
-    b += red[parity][1][w];
-  }
+  const int wave = threadIdx.x & 15;
+  const Pack<float, 2> of = red[parity][wave];
+  const bool here = wave < (int)(blockDim.x >> 6);
+  a = row16_sum_f32(here ? of.v[0] : 0.f);
+  b = row16_sum_f32(here ? of.v[1] : 0.f);
 }
-template <int WAVES>
-__device__ __forceinline__ float block_sum_f32(float a, float (*red)[2][WAVES], const int parity) {
-  a = wave_sum_f32(a);
-  if (WAVES == 1) return a;
-  if ((threadIdx.x & 63) == 0) red[parity][0][threadIdx.x >> 6] = a;
-  __syncthreads();
-  a = red[parity][0][0];
-#pragma unroll
-  for (int w = 1; w < WAVES; ++w) a += red[parity][0][w];
+__device__ __forceinline__ float block_sum_f32(float a, BlockScratch& red, const int parity) {
+  float none = 0.f;
+  block_sum_pair_f32(a, none, red, parity);
   return a;
 }
 

@@ -26,6 +26,7 @@ struct LayerNormForward {
   int64_t N;
   int D;
   float eps;
+  int pad_to;        // above D: y[D] = 1 and zeros up to this column (the bias input of a layer behind)
 };
 
 struct LayerNormBackward {
@@ -42,131 +43,155 @@ struct LayerNormBackward {
   void* db;          // optional
   int64_t N;
   int D;
-  float* part;       // [groups][2][D] sums over a group of rows
+  float* part;       // [groups][2][D] sums over a group of rows; nullptr: none
   int groups;
+  int n_slabs;       // dy is the sum of so many matrices (partial products), slab_stride elements apart
+  int64_t slab_stride;
 };
 
 // ---- rows that a group of threads holds in registers ------------------------------------------------
-// TPR threads share a row and E of its columns each, as E / VEC pieces of VEC neighbours; a workgroup of NT threads walks over the rows,
-// NT / TPR at a time.  A thread keeps its columns of the weight, the bias and (backward) of the sums over the rows in registers,
-// and requests its next row before it works on the one that it has.
-template <typename T, int VEC_, int E_, int TPR_, int NT_>
+// TPR threads share a row, a part of a wavefront (16, 32 or 64) or the whole workgroup (0), which then has as many
+// wavefronts as the width asks for.  A thread holds E columns, as pieces of 16 bytes; the workgroup walks over the rows.  Its columns of
+// the weight, the bias and (backward) of the sums over the rows stay in registers, and rows to come are requested before the one
+// that is there is worked on: SLOTS rows are in flight or in hand.  Rows shorter than 16 bytes have pieces of an element.
+template <int VEC_, int E_, int TPR_, int MAX_THREADS, int SLOTS_>
 struct RowShape {
-  static constexpr int VEC = VEC_, E = E_, TPR = TPR_, NT = NT_, K = E / VEC, ROWS = NT / TPR;
-  static_assert(E % VEC == 0 && NT % TPR == 0 && (TPR == NT || TPR <= 64), "a row belongs to a workgroup or within a wavefront");
-  __device__ static int member() { return threadIdx.x % TPR; }
-  __device__ static int row() { return threadIdx.x / TPR; }
-  __device__ static int column(const int k) { return (k * TPR + member()) * VEC; }
+  static constexpr int VEC = VEC_, E = E_, K = E / VEC, TPR = TPR_, NT = MAX_THREADS, SLOTS = SLOTS_;
+  static constexpr int ROWS = TPR == 0 ? 1 : NT / TPR;   // rows that a workgroup works on side by side
+  static_assert(E % VEC == 0 && NT % 64 == 0 && NT <= 64 * kMaxWaves, "whole pieces, whole wavefronts");
+  __device__ static int threads() { return TPR == 0 ? (int)blockDim.x : TPR; }
+  __device__ static int member() { return TPR == 0 ? (int)threadIdx.x : (int)threadIdx.x % TPR; }
+  __device__ static int row() { return TPR == 0 ? 0 : (int)threadIdx.x / TPR; }
+  __device__ static int column(const int k) { return (k * threads() + member()) * VEC; }
 };
 
-// A thread's columns of a row as they lie in memory, two 16-bit elements to a register where pieces are loaded whole.
+// Where a thread's pieces lie.  A row's last piece is moved back to end at column D, so that it is loaded and stored whole like the others: its
+// first columns are the end of the piece before it, which count there (loading it by elements, and waiting for them in one wavefront
+// and so at the barrier in all, took 90 us for 8192 x 5000 bf16 backward where 8192 x 5120 took 51).  D >= VEC.
+template <typename S>
+struct RowColumns {
+  int D, at[S::K];
+  __device__ __forceinline__ explicit RowColumns(const int D_) : D(D_) {
+#pragma unroll
+    for (int k = 0; k < S::K; ++k) at[k] = min(S::column(k), D - S::VEC);
+  }
+  __device__ __forceinline__ bool here(const int k) const { return S::column(k) < D; }
+  // element e of the thread counts: it is a column of the row, and of no other piece
+  __device__ __forceinline__ bool counts(const int e) const {
+    const int k = e / S::VEC, c = at[k] + e % S::VEC;
+    return c >= S::column(k) && c < D;
+  }
+};
+
+// A thread's columns of a row as they lie in memory (two 16-bit elements to a register).
 template <typename S, typename T>
 struct RowPart {
-  static constexpr bool kWords = S::VEC > 1 && sizeof(T) == 2;
-  using Word = std::conditional_t<kWords, uint32_t, T>;
-  static constexpr int PER = kWords ? 2 : 1;   // elements in a word
-  Word v[S::E / PER];
+  static constexpr int PER = S::VEC > 1 ? 4 / sizeof(T) : 1, WORDS = S::VEC / PER;   // elements of a register, registers of a piece
+  struct __attribute__((packed, aligned(sizeof(T)))) Words {
+    uint32_t v[WORDS];
+  };
+  uint32_t v[S::E / PER];
 
   __device__ __forceinline__ void clear() {
 #pragma unroll
-    for (int i = 0; i < S::E / PER; ++i) v[i] = Word(0);
+    for (int i = 0; i < S::E / PER; ++i) v[i] = 0u;
   }
-  // Zeros behind column D.
-  __device__ __forceinline__ void load(const T* p, const int D) {
+  // What is behind the row's end keeps its value (nothing but the loads may write to v: it would wait for them).
+  __device__ __forceinline__ void load(const T* p, const RowColumns<S>& cols) {
 #pragma unroll
     for (int k = 0; k < S::K; ++k) {
-      const int c = S::column(k);
-      if constexpr (S::VEC > 1) {
-        constexpr int WORDS = S::VEC / PER;
-        if (c + S::VEC <= D) {
-          const Pack<Word, WORDS> q = *reinterpret_cast<const Pack<Word, WORDS>*>(p + c);
-#pragma unroll
-          for (int j = 0; j < WORDS; ++j) v[k * WORDS + j] = q.v[j];
-        } else {
-          Pack<T, S::VEC> q;
-#pragma unroll
-          for (int j = 0; j < S::VEC; ++j) q.v[j] = c + j < D ? p[c + j] : T(0.f);
-          const Pack<Word, WORDS> w = __builtin_bit_cast(Pack<Word, WORDS>, q);
-#pragma unroll
-          for (int j = 0; j < WORDS; ++j) v[k * WORDS + j] = w.v[j];
-        }
+      if (!cols.here(k)) continue;
+      if constexpr (S::VEC * sizeof(T) < 4) {
+        v[k] = __builtin_bit_cast(uint16_t, p[cols.at[k]]);
       } else {
-        v[k] = c < D ? p[c] : T(0.f);
+        const Words q = *reinterpret_cast<const Words*>(p + cols.at[k]);
+#pragma unroll
+        for (int j = 0; j < WORDS; ++j) v[k * WORDS + j] = q.v[j];
       }
     }
   }
   __device__ __forceinline__ float get(const int e) const {
-    if constexpr (kWords)
-      return to_float(__builtin_bit_cast(T, (uint16_t)(e & 1 ? v[e / 2] >> 16 : v[e / 2])));
+    if constexpr (sizeof(T) == 2)
+      return to_float(__builtin_bit_cast(T, (uint16_t)(PER == 2 && e & 1 ? v[e / PER] >> 16 : v[e / PER])));
     else
-      return to_float(v[e]);
+      return __builtin_bit_cast(float, v[e]);
   }
 };
-template <typename S, typename T>
-__device__ __forceinline__ void store_row(const float (&v)[S::E], T* p, const int D) {
+// Both pieces that hold a column write the same number to it; with ONCE only the one where it counts.
+template <typename S, bool ONCE, typename T>
+__device__ __forceinline__ void store_row(const float (&v)[S::E], T* p, const RowColumns<S>& cols) {
 #pragma unroll
   for (int k = 0; k < S::K; ++k) {
-    const int c = S::column(k);
-    if (S::VEC > 1 && c + S::VEC <= D) {
+    if (!cols.here(k)) continue;
+    if (!ONCE || cols.at[k] == S::column(k)) {
       Pack<T, S::VEC> o;
 #pragma unroll
       for (int j = 0; j < S::VEC; ++j) o.v[j] = from_float<T>(v[k * S::VEC + j]);
-      *reinterpret_cast<Pack<T, S::VEC>*>(p + c) = o;
+      *reinterpret_cast<Pack<T, S::VEC>*>(p + cols.at[k]) = o;
     } else {
 #pragma unroll
       for (int j = 0; j < S::VEC; ++j)
-        if (c + j < D) p[c + j] = from_float<T>(v[k * S::VEC + j]);
+        if (cols.counts(k * S::VEC + j)) p[cols.at[k] + j] = from_float<T>(v[k * S::VEC + j]);
+    }
+  }
+}
+
+// Sums over the threads of a row.
+template <typename S>
+__device__ __forceinline__ void row_sum_pair(float& a, float& b, BlockScratch& red, const int parity) {
+  if constexpr (S::TPR == 0) {
+    block_sum_pair_f32(a, b, red, parity);
+  } else {
+    a = row16_sum_f32(a);
+    b = row16_sum_f32(b);
+    if constexpr (S::TPR >= 32) {
+      a = half16_add_f32(a);
+      b = half16_add_f32(b);
+    }
+    if constexpr (S::TPR == 64) {
+      a = half32_add_f32(a);
+      b = half32_add_f32(b);
     }
   }
 }
 template <typename S>
-using RowScratch = float[2][2][S::TPR <= 64 ? 1 : S::TPR / 64];
-
-// Sums over the threads of a row.
-template <typename S>
-__device__ __forceinline__ float row_sum(float v, RowScratch<S>& red, const int parity) {
-  if constexpr (S::TPR == 16)
-    return row16_sum_f32(v);
-  else
-    return block_sum_f32<S::TPR / 64>(v, red, parity);
-}
-template <typename S>
-__device__ __forceinline__ void row_sum_pair(float& a, float& b, RowScratch<S>& red, const int parity) {
-  if constexpr (S::TPR == 16) {
-    a = row16_sum_f32(a);
-    b = row16_sum_f32(b);
-  } else {
-    block_sum_pair_f32<S::TPR / 64>(a, b, red, parity);
-  }
+__device__ __forceinline__ float row_sum(float v, BlockScratch& red, const int parity) {
+  float none = 0.f;
+  row_sum_pair<S>(v, none, red, parity);
+  return v;
 }
 
+// Bound by memory.
 template <typename T, typename W, typename S>
 __global__ __launch_bounds__(S::NT) void layernorm_forward_kernel(const LayerNormForward a) {
-  __shared__ RowScratch<S> red;
+  __shared__ BlockScratch red;
   constexpr int E = S::E;
+  const RowColumns<S> cols(a.D);
   RowPart<S, W> w, b;
-  if (a.w != nullptr) w.load(static_cast<const W*>(a.w), a.D);
-  if (a.b != nullptr) b.load(static_cast<const W*>(a.b), a.D);
+  w.clear();
+  b.clear();
+  if (a.w != nullptr) w.load(static_cast<const W*>(a.w), cols);
+  if (a.b != nullptr) b.load(static_cast<const W*>(a.b), cols);
   const int64_t step = (int64_t)gridDim.x * S::ROWS;
   int64_t row = (int64_t)blockIdx.x * S::ROWS + S::row();
   RowPart<S, T> next;
   next.clear();
-  if (row < a.N) next.load(static_cast<const T*>(a.x) + row * a.ldx, a.D);
+  if (row < a.N) next.load(static_cast<const T*>(a.x) + row * a.ldx, cols);
   for (int64_t first = (int64_t)blockIdx.x * S::ROWS; first < a.N; first += step, row += step) {   // (uniform in the workgroup)
     float x[E];
     float s = 0.f;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       x[e] = next.get(e);
-      s += x[e];
+      s += cols.counts(e) ? x[e] : 0.f;
     }
-    if (row + step < a.N) next.load(static_cast<const T*>(a.x) + (row + step) * a.ldx, a.D);
+    if (row + step < a.N) next.load(static_cast<const T*>(a.x) + (row + step) * a.ldx, cols);
     const float mean = row_sum<S>(s, red, 0) / (float)a.D;
     float q = 0.f;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      x[e] = S::column(e / S::VEC) + e % S::VEC < a.D ? x[e] - mean : 0.f;
-      q += x[e] * x[e];
+      x[e] -= mean;
+      q += cols.counts(e) ? x[e] * x[e] : 0.f;
     }
     const float rstd = 1.f / sqrtf(row_sum<S>(q, red, 1) / (float)a.D + a.eps);
 #pragma unroll
@@ -176,7 +201,9 @@ __global__ __launch_bounds__(S::NT) void layernorm_forward_kernel(const LayerNor
       if (a.b != nullptr) x[e] += b.get(e);
     }
     if (row < a.N) {
-      store_row<S>(x, static_cast<T*>(a.y) + row * a.ldy, a.D);
+      T* const y = static_cast<T*>(a.y) + row * a.ldy;
+      store_row<S, false>(x, y, cols);
+      for (int c = a.D + S::member(); c < a.pad_to; c += S::threads()) y[c] = from_float<T>(c == a.D ? 1.f : 0.f);
       if (S::member() == 0) {
         if (a.mean != nullptr) a.mean[row] = mean;
         if (a.rstd != nullptr) a.rstd[row] = rstd;
@@ -186,69 +213,99 @@ __global__ __launch_bounds__(S::NT) void layernorm_forward_kernel(const LayerNor
 }
 
 // What a thread needs of a row; zeros behind the last one.
-template <typename S, typename T>
+template <typename S, typename T, bool SLABS>
 struct BackwardRow {
   RowPart<S, T> x, dy;
   float mean, rstd;
-  __device__ __forceinline__ void load(const LayerNormBackward& a, const int64_t r) {
+  __device__ __forceinline__ float xhat(const int e) const { return (x.get(e) - mean) * rstd; }
+  __device__ __forceinline__ void load(const LayerNormBackward& a, const RowColumns<S>& cols, const int64_t r) {
+    float m = 0.f, s = 0.f;
     if (r < a.N) {
-      x.load(static_cast<const T*>(a.x) + r * a.ldx, a.D);
-      dy.load(static_cast<const T*>(a.dy) + r * a.lddy, a.D);
-      mean = a.mean[r];
-      rstd = a.rstd[r];
+      const T* const p = static_cast<const T*>(a.dy) + r * a.lddy;
+      x.load(static_cast<const T*>(a.x) + r * a.ldx, cols);
+      dy.load(p, cols);
+      if constexpr (SLABS) {   // (fp32) in a fixed order
+        for (int k = 1; k < a.n_slabs; ++k) {
+          RowPart<S, T> more;
+          more.clear();
+          more.load(p + k * a.slab_stride, cols);
+#pragma unroll
+          for (int e = 0; e < S::E; ++e) dy.v[e] = __builtin_bit_cast(uint32_t, dy.get(e) + more.get(e));
+        }
+      }
+      m = a.mean[r];
+      s = a.rstd[r];
     } else {
       x.clear();
       dy.clear();
-      mean = rstd = 0.f;
     }
+    mean = m;   // (assigned in the branches, one in another order than the other, the structure ends up in memory)
+    rstd = s;
   }
 };
 
-// Sums of a workgroup's rows go to part[workgroup][dw, db][D].
-template <typename T, typename W, typename S>
+// Sums of a workgroup's rows go to part[workgroup][dw, db][D].  Bound by memory, as long as enough rows are in flight: 16384 x 8192 bf16 takes
+// 168 us with one row to come and 151 with two (5.3 TB/s, the rate of a large copy); the gradient is formed from x and dy again behind the
+// row's sums, so that registers hold rows to come instead of xhat and g.
+template <typename T, typename W, typename S, bool SLABS>
 __global__ __launch_bounds__(S::NT) void layernorm_backward_kernel(const LayerNormBackward a) {
-  __shared__ RowScratch<S> red;
+  __shared__ BlockScratch red;
   __shared__ float sums[S::ROWS > 1 ? S::NT * S::E : 1];
-  constexpr int E = S::E;
+  constexpr int E = S::E, SLOTS = S::SLOTS;
+  const RowColumns<S> cols(a.D);
   RowPart<S, W> w;
-  if (a.w != nullptr) w.load(static_cast<const W*>(a.w), a.D);
+  w.clear();
+  if (a.w != nullptr) w.load(static_cast<const W*>(a.w), cols);
   float dw[E], db[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) dw[e] = db[e] = 0.f;
   const int64_t step = (int64_t)gridDim.x * S::ROWS;
   int64_t row = (int64_t)blockIdx.x * S::ROWS + S::row();
-  BackwardRow<S, T> next;
-  next.load(a, row);
+  BackwardRow<S, T, SLABS> rows[SLOTS];
+#pragma unroll
+  for (int k = 0; k < SLOTS; ++k) {
+    rows[k].x.clear();
+    rows[k].dy.clear();
+    rows[k].load(a, cols, row + k * step);
+  }
   int parity = 0;
-  for (int64_t first = (int64_t)blockIdx.x * S::ROWS; first < a.N; first += step, row += step, parity ^= 1) {   // (uniform in the workgroup)
-    float xhat[E], g[E];
-    const float rstd = next.rstd;
-    float c1 = 0.f, c2 = 0.f;
+  for (int64_t first = (int64_t)blockIdx.x * S::ROWS; first < a.N; first += SLOTS * step) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      xhat[e] = (next.x.get(e) - next.mean) * rstd;
-      g[e] = next.dy.get(e);
-      dw[e] += g[e] * xhat[e];
-      db[e] += g[e];
-      if (a.w != nullptr) g[e] *= w.get(e);
-      c1 += g[e];
-      c2 += g[e] * xhat[e];
-    }
-    next.load(a, row + step);
-    if (a.dx != nullptr) {
-      row_sum_pair<S>(c1, c2, red, parity);
-      c1 /= (float)a.D;
-      c2 /= (float)a.D;
+    for (int k = 0; k < SLOTS; ++k) {
+      if (first + k * step < a.N) {   // (uniform in the workgroup)
+        const BackwardRow<S, T, SLABS>& r = rows[k];
+        float c1 = 0.f, c2 = 0.f;
 #pragma unroll
-      for (int e = 0; e < E; ++e) g[e] = rstd * (g[e] - c1 - xhat[e] * c2);
-      if (row < a.N) store_row<S>(g, static_cast<T*>(a.dx) + row * a.lddx, a.D);
+        for (int e = 0; e < E; ++e) {
+          const float xhat = r.xhat(e), dy = cols.counts(e) ? r.dy.get(e) : 0.f, g = a.w != nullptr ? dy * w.get(e) : dy;
+          dw[e] += dy * xhat;
+          db[e] += dy;
+          c1 += g;
+          c2 += g * xhat;
+        }
+        if (a.dx != nullptr) {
+          row_sum_pair<S>(c1, c2, red, parity);
+          c1 /= (float)a.D;
+          c2 /= (float)a.D;
+          float dx[E];
+#pragma unroll
+          for (int e = 0; e < E; ++e) {
+            const float dy = r.dy.get(e), g = a.w != nullptr ? dy * w.get(e) : dy;
+            dx[e] = r.rstd * (g - c1 - r.xhat(e) * c2);
+          }
+          if (row < a.N) store_row<S, false>(dx, static_cast<T*>(a.dx) + row * a.lddx, cols);
+        }
+        rows[k].load(a, cols, row + SLOTS * step);
+        parity ^= 1;
+        row += step;
+      }
     }
   }
   if (a.part == nullptr) return;
   float* const part = a.part + (size_t)blockIdx.x * 2 * a.D;
   if (S::ROWS == 1) {
-    store_row<S>(dw, part, a.D);
-    store_row<S>(db, part + a.D, a.D);
+    store_row<S, true>(dw, part, cols);
+    store_row<S, true>(db, part + a.D, cols);
     return;
   }
   // the rows that the workgroup worked on side by side, in order
@@ -256,45 +313,60 @@ __global__ __launch_bounds__(S::NT) void layernorm_backward_kernel(const LayerNo
   for (int which = 0; which < 2; ++which) {
     __syncthreads();
 #pragma unroll
-    for (int e = 0; e < E; ++e) sums[(S::row() * S::TPR + S::member()) * E + e] = which == 0 ? dw[e] : db[e];
+    for (int e = 0; e < E; ++e) sums[threadIdx.x * E + e] = which == 0 ? dw[e] : db[e];
     __syncthreads();
-    for (int i = threadIdx.x; i < S::TPR * E; i += S::NT) {
-      float v = 0.f;
+    if (S::row() != 0) continue;
+    float v[E];
 #pragma unroll
-      for (int r = 0; r < S::ROWS; ++r) v += sums[r * S::TPR * E + i];
-      const int e = i % E, c = ((e / S::VEC) * S::TPR + i / E) * S::VEC + e % S::VEC;
-      if (c < a.D) part[(size_t)which * a.D + c] = v;
+    for (int e = 0; e < E; ++e) {
+      v[e] = 0.f;
+#pragma unroll
+      for (int r = 0; r < S::ROWS; ++r) v[e] += sums[(r * S::threads() + S::member()) * E + e];
+    }
+    store_row<S, true>(v, part + (size_t)which * a.D, cols);
+  }
+}
+
+// ---- rows of any width, read from memory in every pass -------------------------------------------------
+constexpr int kWideThreads = 1024;
+constexpr int kRegisterColumns = 16384;   // the widest rows of the kernels above
+
+// f(column, value) for a thread's elements of a row
+template <typename T, typename F>
+__device__ __forceinline__ void for_row(const T* p, const int D, F f) {
+  constexpr int VEC = 16 / sizeof(T);
+  for (int64_t c = (int64_t)threadIdx.x * VEC; c < D; c += kWideThreads * VEC) {
+    if (c + VEC <= D) {
+      const Pack<T, VEC> q = *reinterpret_cast<const Pack<T, VEC>*>(p + c);
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) f((int)c + j, to_float(q.v[j]));
+    } else {
+      for (int64_t i = c; i < D; ++i) f((int)i, to_float(p[i]));
     }
   }
 }
 
-// ---- rows of any width, read from memory in every pass ---------------------------------------------
-constexpr int kNormThreads = 256;
-constexpr int kRegisterColumns = 16384;   // the widest rows of the kernels above
-
 template <typename T, typename W>
-__global__ __launch_bounds__(kNormThreads) void layernorm_forward_wide_kernel(const LayerNormForward a) {
-  __shared__ float red[2][2][kNormThreads / 64];
+__global__ __launch_bounds__(kWideThreads) void layernorm_forward_wide_kernel(const LayerNormForward a) {
+  __shared__ BlockScratch red;
   const W* const w = static_cast<const W*>(a.w);
   const W* const b = static_cast<const W*>(a.b);
   for (int64_t row = blockIdx.x; row < a.N; row += gridDim.x) {
     const T* const x = static_cast<const T*>(a.x) + row * a.ldx;
     T* const y = static_cast<T*>(a.y) + row * a.ldy;
     float s = 0.f;
-    for (int c = threadIdx.x; c < a.D; c += kNormThreads) s += to_float(x[c]);
-    const float mean = block_sum_f32<kNormThreads / 64>(s, red, 0) / (float)a.D;
+    for_row(x, a.D, [&](int, float v) { s += v; });
+    const float mean = block_sum_f32(s, red, 0) / (float)a.D;
     float q = 0.f;
-    for (int c = threadIdx.x; c < a.D; c += kNormThreads) {
-      const float d = to_float(x[c]) - mean;
-      q += d * d;
-    }
-    const float rstd = 1.f / sqrtf(block_sum_f32<kNormThreads / 64>(q, red, 1) / (float)a.D + a.eps);
-    for (int c = threadIdx.x; c < a.D; c += kNormThreads) {
-      float v = (to_float(x[c]) - mean) * rstd;
+    for_row(x, a.D, [&](int, float v) { q += (v - mean) * (v - mean); });
+    const float rstd = 1.f / sqrtf(block_sum_f32(q, red, 1) / (float)a.D + a.eps);
+    for_row(x, a.D, [&](int c, float v) {
+      v = (v - mean) * rstd;
       if (w != nullptr) v *= to_float(w[c]);
       if (b != nullptr) v += to_float(b[c]);
       y[c] = from_float<T>(v);
-    }
+    });
+    for (int64_t c = (int64_t)a.D + threadIdx.x; c < a.pad_to; c += kWideThreads) y[c] = from_float<T>(c == a.D ? 1.f : 0.f);
     if (threadIdx.x == 0) {
       if (a.mean != nullptr) a.mean[row] = mean;
       if (a.rstd != nullptr) a.rstd[row] = rstd;
@@ -302,44 +374,52 @@ __global__ __launch_bounds__(kNormThreads) void layernorm_forward_wide_kernel(co
   }
 }
 
-template <typename T, typename W>
-__global__ __launch_bounds__(kNormThreads) void layernorm_backward_rows_kernel(const LayerNormBackward a) {
-  __shared__ float red[2][2][kNormThreads / 64];
+template <typename T, bool SLABS>
+__device__ __forceinline__ float dy_of(const LayerNormBackward& a, const int64_t row, const int64_t c) {
+  const T* const p = static_cast<const T*>(a.dy) + row * a.lddy + c;
+  float v = to_float(p[0]);
+  if constexpr (SLABS)
+    for (int k = 1; k < a.n_slabs; ++k) v += to_float(p[k * a.slab_stride]);
+  return v;
+}
+
+template <typename T, typename W, bool SLABS>
+__global__ __launch_bounds__(kWideThreads) void layernorm_backward_rows_kernel(const LayerNormBackward a) {
+  __shared__ BlockScratch red;
   const W* const w = static_cast<const W*>(a.w);
   int parity = 0;
   for (int64_t row = blockIdx.x; row < a.N; row += gridDim.x, parity ^= 1) {
     const T* const x = static_cast<const T*>(a.x) + row * a.ldx;
-    const T* const dy = static_cast<const T*>(a.dy) + row * a.lddy;
     T* const dx = static_cast<T*>(a.dx) + row * a.lddx;
     const float mean = a.mean[row], rstd = a.rstd[row];
     float c1 = 0.f, c2 = 0.f;
-    for (int c = threadIdx.x; c < a.D; c += kNormThreads) {
-      float g = to_float(dy[c]);
+    for_row(x, a.D, [&](int c, float v) {
+      float g = dy_of<T, SLABS>(a, row, c);
       if (w != nullptr) g *= to_float(w[c]);
       c1 += g;
-      c2 += g * ((to_float(x[c]) - mean) * rstd);
-    }
-    block_sum_pair_f32<kNormThreads / 64>(c1, c2, red, parity);
+      c2 += g * ((v - mean) * rstd);
+    });
+    block_sum_pair_f32(c1, c2, red, parity);
     c1 /= (float)a.D;
     c2 /= (float)a.D;
-    for (int c = threadIdx.x; c < a.D; c += kNormThreads) {
-      float g = to_float(dy[c]);
+    for_row(x, a.D, [&](int c, float v) {
+      float g = dy_of<T, SLABS>(a, row, c);
       if (w != nullptr) g *= to_float(w[c]);
-      const float xhat = (to_float(x[c]) - mean) * rstd;
-      dx[c] = from_float<T>(rstd * (g - c1 - xhat * c2));
-    }
+      dx[c] = from_float<T>(rstd * (g - c1 - ((v - mean) * rstd) * c2));
+    });
   }
 }
 
 // Sums over the rows of a group: grid (columns / 256, groups), a thread per column.
-template <typename T>
-__global__ __launch_bounds__(kNormThreads) void layernorm_backward_columns_kernel(const LayerNormBackward a) {
-  const int64_t c = (int64_t)blockIdx.x * kNormThreads + threadIdx.x;
+constexpr int kColumnThreads = 256;
+template <typename T, bool SLABS>
+__global__ __launch_bounds__(kColumnThreads) void layernorm_backward_columns_kernel(const LayerNormBackward a) {
+  const int64_t c = (int64_t)blockIdx.x * kColumnThreads + threadIdx.x;
   if (c >= a.D) return;
   const int64_t first = a.N * blockIdx.y / a.groups, end = a.N * (blockIdx.y + 1) / a.groups;
   float dw = 0.f, db = 0.f;
   for (int64_t row = first; row < end; ++row) {
-    const float dy = to_float(static_cast<const T*>(a.dy)[row * a.lddy + c]);
+    const float dy = dy_of<T, SLABS>(a, row, c);
     dw += dy * ((to_float(static_cast<const T*>(a.x)[row * a.ldx + c]) - a.mean[row]) * a.rstd[row]);
     db += dy;
   }
