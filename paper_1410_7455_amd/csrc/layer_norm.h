@@ -96,6 +96,11 @@ struct RowPart {
 #pragma unroll
     for (int i = 0; i < S::E / PER; ++i) v[i] = 0u;
   }
+  // Keeps what is formed from these registers in a loop from being formed before it, in registers of its own.
+  __device__ __forceinline__ void stay() {
+#pragma unroll
+    for (int i = 0; i < S::E / PER; ++i) asm("" : "+v"(v[i]));
+  }
   // What is behind the row's end keeps its value (nothing but the loads may write to v: it would wait for them).
   __device__ __forceinline__ void load(const T* p, const RowColumns<S>& cols) {
 #pragma unroll
@@ -252,6 +257,9 @@ __global__ __launch_bounds__(S::NT) void layernorm_backward_kernel(const LayerNo
   __shared__ BlockScratch red;
   __shared__ float sums[S::ROWS > 1 ? S::NT * S::E : 1];
   constexpr int E = S::E, SLOTS = S::SLOTS;
+  // The widest rows in 16 bits just fit in a workgroup of 1024's 128 registers (8192 x 16384 bf16: 162 us; 235 with 17 of them in
+  // memory).  In fp32 they do not, and it is the better for what is formed once (16384 x 16384: 746 us, else 865).
+  constexpr bool TIGHT = SLOTS == 1 && sizeof(T) == 2;
   const RowColumns<S> cols(a.D);
   RowPart<S, W> w;
   w.clear();
@@ -273,7 +281,7 @@ __global__ __launch_bounds__(S::NT) void layernorm_backward_kernel(const LayerNo
 #pragma unroll
     for (int k = 0; k < SLOTS; ++k) {
       if (first + k * step < a.N) {   // (uniform in the workgroup)
-        const BackwardRow<S, T, SLABS>& r = rows[k];
+        BackwardRow<S, T, SLABS>& r = rows[k];
         float c1 = 0.f, c2 = 0.f;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
@@ -287,6 +295,11 @@ __global__ __launch_bounds__(S::NT) void layernorm_backward_kernel(const LayerNo
           row_sum_pair<S>(c1, c2, red, parity);
           c1 /= (float)a.D;
           c2 /= (float)a.D;
+          if constexpr (TIGHT) {   // nothing formed above is kept
+            r.x.stay();
+            r.dy.stay();
+            w.stay();
+          }
           float dx[E];
 #pragma unroll
           for (int e = 0; e < E; ++e) {
