@@ -197,7 +197,7 @@ int ngsgd_precondition_simple_static(float* dev_M, int32_t N, int32_t D, int32_t
  * Statistics and sums are in fp32, outputs are rounded once.  Leading dimensions count elements, at least D and otherwise free:
  * rows need no alignment beyond an element's (rows on multiples of 16 bytes are faster).  dev_y may be dev_x with
  * the same leading dimension; other overlaps are not allowed.  N may be 0.  Rows do not mix: an infinity or NaN
- * stays in its row.  epsilon is finite and not negative; with 0 a row of equal numbers gives NaN. */
+ * stays in its row.  D is at most 2^25.  epsilon is finite and not negative; with 0 a row of equal numbers gives NaN. */
 int ngsgd_layernorm_forward(const void* dev_x, int64_t ldx, int32_t type, const void* dev_weight,
                             const void* dev_bias, int32_t weight_type, int64_t N, int32_t D, float epsilon,
                             void* dev_y, int64_t ldy, float* dev_mean, float* dev_rstd, void* hip_stream);
@@ -235,7 +235,7 @@ typedef struct {
   int32_t state_bits;         /* 32: moments in fp32; 8: codes with an exponent for every 256 elements */
   int32_t master;             /* 1: parameters in 16 bits are rounded from fp32 copies that are kept */
   double beta1, beta2;        /* in [0, 1)                                                  */
-  float epsilon;
+  float epsilon;              /* 0 or a positive normal number                              */
 } ngsgd_adamw_config;
 
 int ngsgd_adamw_workspace_bytes(const ngsgd_adamw_config* cfg, size_t* out_bytes);

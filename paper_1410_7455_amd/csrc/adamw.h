@@ -30,37 +30,43 @@ constexpr int kAdamGrads = 448;         // gradients whose addresses one launch 
 constexpr uint32_t kDitherIndex = 0x9E3779B1u, kDitherStep = 0x6A09E667u;   // 2^32 times the fractions of phi (odd) and sqrt 2
 constexpr uint32_t kDitherHalf = 1u << 19;                                  // to nearest
 
-struct AdamTensor {
-  void* p;
-  int64_t n;
+// A piece of work: up to kAdamChunk elements of a tensor, with all that a workgroup has to know of it (one read from memory before the data's).
+struct AdamChunk {
+  void* p;           // its parameters
   int64_t offset;    // of its moments, a multiple of kAdamBlock
+  int tensor, index; // elements [index kAdamChunk, ...) of the tensor
+  int n;             // how many
   float rate;        // factor on the learning rate
   float decay;
-};
-struct AdamChunk {
-  int tensor;
-  int index;         // elements [index kAdamChunk, ...) of the tensor
+  int unused;
 };
 // On the device, so that a captured step counts on when it is replayed.
 struct AdamScalars {
-  int64_t t;                 // steps so far
-  double b1_power, b2_power; // b1^t, b2^t
-  unsigned done;             // workgroups of the step that have read these
+  int64_t t;                   // steps so far
+  double b1_power, b2_power;   // b1^t, b2^t
+  float m_unbias, root_unbias; // 1 / (1 - b1^t), (1 - b2^t)^(-1/2)
+  unsigned done, unused;       // workgroups of a counting step that have read these
+};
+
+struct AdamExponents {
+  uint8_t m, v;   // E of the block's m and of its roots of v, biased as in fp32
+  uint16_t nan;   // not 0: some code stands for NaN
 };
 
 struct AdamState {
-  const AdamTensor* tensors;
   const AdamChunk* chunks;
   AdamScalars* scalars;
   float* master;             // fp32 copies of the parameters, flat as the moments
   float *m32, *v32;
-  uint8_t *m8, *v8, *m_exp, *v_exp;   // codes, and exponents by block
+  uint8_t *m8, *v8;          // codes
+  AdamExponents* exps;       // by block
 };
 
 struct AdamStep {
   AdamState s;
-  int first_tensor, first_chunk, n_chunks;
-  unsigned last;             // the workgroup that is the step's last one to be done
+  int first_tensor, first_chunk;
+  int part_bits;             // 2^part_bits workgroups share a chunk: 1 or 4
+  int counts;                // the step's only launch, of few workgroups: the last one of them to be done counts the step
   float lr, scale, eps;
   double beta1, beta2;       // (in fp32, 1 - 0.999 would be off by 1e-5 of itself)
   const float* dev_lr;       // optional factors on lr and scale
@@ -69,15 +75,27 @@ struct AdamStep {
 };
 
 // ---- codes -------------------------------------------------------------------------------------------
-__device__ __forceinline__ uint32_t dither_of(const int64_t i, const int64_t t) {
-  return ((uint32_t)i * kDitherIndex + (uint32_t)t * kDitherStep) >> 12;
-}
+__device__ __forceinline__ uint32_t dither_start(const int64_t i, const int64_t t) { return (uint32_t)i * kDitherIndex + (uint32_t)t * kDitherStep; }
+__device__ __forceinline__ uint32_t dither_of(const uint32_t start, const int k) { return (start + (uint32_t)k * kDitherIndex) >> 12; }   // of element i + k
 __device__ __forceinline__ bool finite_bits(const uint32_t magnitude) { return magnitude < 0x7f800000u; }
-__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, off));
-  return v;
+
+// Largest of the 64 lanes, in a scalar register.
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp_max_u32(const uint32_t v) {
+  return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true));
 }
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
+  v = dpp_max_u32<0xB1>(v);    // quad_perm [1,0,3,2]
+  v = dpp_max_u32<0x4E>(v);    // quad_perm [2,3,0,1]
+  v = dpp_max_u32<0x141>(v);   // row_half_mirror
+  v = dpp_max_u32<0x140>(v);   // row_mirror
+  const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = max((uint32_t)a[0], (uint32_t)a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return __builtin_amdgcn_readfirstlane(max((uint32_t)b[0], (uint32_t)b[1]));
+}
+__device__ __forceinline__ bool any_lane(const bool b) { return __builtin_amdgcn_ballot_w64(b) != 0; }
+
 // E (biased as in fp32) of a block with this largest finite magnitude; not below what the least code can be written with.
 __device__ __forceinline__ uint32_t exponent_of(const uint32_t top, const uint32_t lowest) { return max((top + 0xFFFFFu) >> 23, lowest); }
 constexpr uint32_t kLowestM = 16, kLowestV = 32;
@@ -85,35 +103,24 @@ constexpr uint32_t kLowestM = 16, kLowestV = 32;
 __device__ __forceinline__ int base_m(const uint32_t e) { return (int)(e + 1) * 8 - 128; }
 __device__ __forceinline__ int base_v(const uint32_t e) { return (int)(e + 1) * 8 - 255; }
 
-__device__ __forceinline__ uint8_t code_m(const float m, const uint32_t e, const uint32_t dither) {
+__device__ __forceinline__ uint32_t code_m(const float m, const int base, const uint32_t dither) {
   const uint32_t bits = __builtin_bit_cast(uint32_t, m), a = bits & 0x7fffffffu;
   if (!finite_bits(a)) return 0x80;
-  const int base = base_m(e);
   const float magnitude = __builtin_bit_cast(float, a), least = __builtin_bit_cast(float, (uint32_t)(base + 1) << 20);
   int code = min(max((int)((a + dither) >> 20) - base, 1), 127);
   if (magnitude < least) code = magnitude > least * ((float)dither * 0x1p-20f) ? 1 : 0;
-  return (uint8_t)(code == 0 ? 0 : code | (bits >> 31 << 7));
+  return code == 0 ? 0u : (uint32_t)code | (bits >> 31 << 7);
 }
-__device__ __forceinline__ float value_m(const uint32_t code, const uint32_t e) {
-  if (code == 0x80u) return __builtin_nanf("");
-  const uint32_t magnitude = (code & 0x7fu) == 0 ? 0u : ((code & 0x7fu) + base_m(e)) << 20;
-  return __builtin_bit_cast(float, magnitude | (code >> 7 << 31));
-}
-__device__ __forceinline__ uint8_t code_root(const float r, const uint32_t e, const uint32_t dither) {
+__device__ __forceinline__ uint32_t code_root(const float r, const int base, const uint32_t dither) {
   const uint32_t bits = __builtin_bit_cast(uint32_t, r);
-  if (!finite_bits(bits)) return 255;   // (a root is not negative; that of a negative number is NaN)
-  return (uint8_t)(bits == 0 ? 0 : min(max((int)((bits + dither) >> 20) - base_v(e), 1), 254));
-}
-__device__ __forceinline__ float value_v(const uint32_t code, const uint32_t e) {
-  if (code == 255u) return __builtin_nanf("");
-  const float r = code == 0 ? 0.f : __builtin_bit_cast(float, (uint32_t)((int)code + base_v(e)) << 20);
-  return r * r;
+  if (!finite_bits(bits)) return 255u;   // (a root is not negative; that of a negative number is NaN)
+  return bits == 0 ? 0u : (uint32_t)min(max((int)((bits + dither) >> 20) - base, 1), 254);
 }
 
 // Four consecutive elements of a lane; `here` of them exist.
 template <typename T>
-__device__ __forceinline__ void load4(float (&out)[4], const T* p, const int here, const bool aligned) {
-  if (here >= 4 && aligned) {
+__device__ __forceinline__ void load4(float (&out)[4], const T* p, const int here) {
+  if (here >= 4) {
     const Pack<T, 4> v = *reinterpret_cast<const Pack<T, 4>*>(p);
 #pragma unroll
     for (int k = 0; k < 4; ++k) out[k] = to_float(v.v[k]);
@@ -123,8 +130,8 @@ __device__ __forceinline__ void load4(float (&out)[4], const T* p, const int her
   }
 }
 template <typename T>
-__device__ __forceinline__ void store4(const float (&v)[4], T* p, const int here, const bool aligned) {
-  if (here >= 4 && aligned) {
+__device__ __forceinline__ void store4(const float (&v)[4], T* p, const int here) {
+  if (here >= 4) {
     Pack<T, 4> o;
 #pragma unroll
     for (int k = 0; k < 4; ++k) o.v[k] = from_float<T>(v[k]);
@@ -136,112 +143,206 @@ __device__ __forceinline__ void store4(const float (&v)[4], T* p, const int here
   }
 }
 
-// The moments of a lane's four elements of block `block` (both numbered over the flat arrays).
+// The moments of a lane's four elements of block `block` (both numbered over the flat arrays), as they lie in memory.
 template <int BITS>
-__device__ __forceinline__ void load_moments(const AdamState& s, const int64_t block, float (&m)[4], float (&v)[4]) {
-  const int64_t at = block * kAdamBlock + 4 * (threadIdx.x & 63);
-  if (BITS == 32) {
-    load4(m, s.m32 + at, 4, true);
-    load4(v, s.v32 + at, 4, true);
-  } else {
-    const uint32_t mc = *reinterpret_cast<const uint32_t*>(s.m8 + at), vc = *reinterpret_cast<const uint32_t*>(s.v8 + at);
-    const uint32_t me = s.m_exp[block], ve = s.v_exp[block];
+struct Moments {
+  Pack<float, 4> m, v;
+  __device__ __forceinline__ void load(const AdamState& s, const int64_t block) {
+    const int64_t at = block * kAdamBlock + 4 * (threadIdx.x & 63);
+    m = *reinterpret_cast<const Pack<float, 4>*>(s.m32 + at);
+    v = *reinterpret_cast<const Pack<float, 4>*>(s.v32 + at);
+  }
+  __device__ __forceinline__ void get(float (&m_out)[4], float (&v_out)[4]) const {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      m[k] = value_m(mc >> (8 * k) & 0xffu, me);
-      v[k] = value_v(vc >> (8 * k) & 0xffu, ve);
+      m_out[k] = m.v[k];
+      v_out[k] = v.v[k];
     }
   }
-}
-template <int BITS>
-__device__ __forceinline__ void store_moments(const AdamState& s, const int64_t block, const float (&m)[4], const float (&v)[4], const bool nearest,
-                                              const int64_t t) {
+};
+template <>
+struct Moments<8> {
+  uint32_t m, v;
+  AdamExponents exps;
+  __device__ __forceinline__ void load(const AdamState& s, const int64_t block) {
+    const int64_t at = block * kAdamBlock + 4 * (threadIdx.x & 63);
+    m = *reinterpret_cast<const uint32_t*>(s.m8 + at);
+    v = *reinterpret_cast<const uint32_t*>(s.v8 + at);
+    exps = s.exps[block];
+  }
+  __device__ __forceinline__ void get(float (&m_out)[4], float (&v_out)[4]) const {
+    const uint32_t e = __builtin_amdgcn_readfirstlane(__builtin_bit_cast(uint32_t, exps));
+    const uint32_t mb = (uint32_t)base_m(e & 0xffu), vb = (uint32_t)base_v(e >> 8 & 0xffu);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const uint32_t mc = m >> (8 * k) & 0x7fu, vc = v >> (8 * k) & 0xffu, sign = m << (24 - 8 * k) & 0x80000000u;
+      m_out[k] = __builtin_bit_cast(float, (mc == 0 ? 0u : (mc + mb) << 20) | sign);
+      const float r = __builtin_bit_cast(float, vc == 0 ? 0u : (vc + vb) << 20);
+      v_out[k] = r * r;
+    }
+    if (e >> 16 != 0) {   // (uniform)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if ((m >> (8 * k) & 0xffu) == 0x80u) m_out[k] = __builtin_nanf("");
+        if ((v >> (8 * k) & 0xffu) == 0xffu) v_out[k] = __builtin_nanf("");
+      }
+    }
+  }
+};
+
+// Codes of a lane's four elements of block `block`, given m and the roots of v.  `plain`: all are finite.  `start`: see dither_start.
+__device__ __forceinline__ void store_codes(const AdamState& s, const int64_t block, const float (&m)[4], const float (&r)[4], const bool plain,
+                                            const bool nearest, const uint32_t start) {
   const int lane = threadIdx.x & 63;
   const int64_t at = block * kAdamBlock + 4 * lane;
-  if (BITS == 32) {
-    store4(m, s.m32 + at, 4, true);
-    store4(v, s.v32 + at, 4, true);
+  uint32_t a[4], b[4], dither[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    a[k] = __builtin_bit_cast(uint32_t, m[k]) & 0x7fffffffu;
+    b[k] = __builtin_bit_cast(uint32_t, r[k]) & 0x7fffffffu;
+    dither[k] = nearest ? kDitherHalf : dither_of(start, k);
+  }
+  uint32_t mt = max(max(a[0], a[1]), max(a[2], a[3])), rt = max(max(b[0], b[1]), max(b[2], b[3])), nan = 0;
+  if (!plain) {   // (uniform)
+    bool odd = false;
+    mt = rt = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      mt = max(mt, finite_bits(a[k]) ? a[k] : 0u);
+      rt = max(rt, finite_bits(b[k]) ? b[k] : 0u);
+      odd |= !finite_bits(a[k]) || !finite_bits(b[k]);
+    }
+    nan = any_lane(odd) ? 1u : 0u;
+  }
+  const uint32_t me = exponent_of(wave_max_u32(mt), kLowestM), ve = exponent_of(wave_max_u32(rt), kLowestV);
+  const int mb = base_m(me), vb = base_v(ve);
+  const uint32_t m_least = (uint32_t)(mb + 1) << 20, r_least = (uint32_t)(vb + 1) << 20;
+  uint32_t mc = 0, vc = 0;
+  if (plain && !any_lane(min(min(a[0], a[1]), min(a[2], a[3])) < m_least || min(min(b[0], b[1]), min(b[2], b[3])) < r_least)) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {   // what the general form comes to where nothing is below the least code
+      mc |= (min(((a[k] + dither[k]) >> 20) - (uint32_t)mb, 127u) | (__builtin_bit_cast(uint32_t, m[k]) >> 24 & 0x80u)) << (8 * k);
+      vc |= min(((b[k] + dither[k]) >> 20) - (uint32_t)vb, 254u) << (8 * k);
+    }
   } else {
-    float r[4];
-    uint32_t mt = 0, rt = 0;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      r[k] = sqrtf(v[k]);
-      const uint32_t a = __builtin_bit_cast(uint32_t, m[k]) & 0x7fffffffu, b = __builtin_bit_cast(uint32_t, r[k]) & 0x7fffffffu;
-      mt = max(mt, finite_bits(a) ? a : 0u);
-      rt = max(rt, finite_bits(b) ? b : 0u);
-    }
-    const uint32_t me = exponent_of(wave_max_u32(mt), kLowestM), ve = exponent_of(wave_max_u32(rt), kLowestV);
-    uint32_t mc = 0, vc = 0;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const uint32_t dither = nearest ? kDitherHalf : dither_of(at + k, t);
-      mc |= (uint32_t)code_m(m[k], me, dither) << (8 * k);
-      vc |= (uint32_t)code_root(r[k], ve, dither) << (8 * k);
-    }
-    *reinterpret_cast<uint32_t*>(s.m8 + at) = mc;
-    *reinterpret_cast<uint32_t*>(s.v8 + at) = vc;
-    if (lane == 0) {
-      s.m_exp[block] = (uint8_t)me;
-      s.v_exp[block] = (uint8_t)ve;
+      mc |= code_m(m[k], mb, dither[k]) << (8 * k);
+      vc |= code_root(r[k], vb, dither[k]) << (8 * k);
     }
   }
+  *reinterpret_cast<uint32_t*>(s.m8 + at) = mc;
+  *reinterpret_cast<uint32_t*>(s.v8 + at) = vc;
+  if (lane == 0) s.exps[block] = AdamExponents{(uint8_t)me, (uint8_t)ve, (uint16_t)nan};
+}
+
+// Classes of fp32 numbers, as v_cmp_class takes them.
+constexpr int kClassNotFinite = 0x207, kClassZeroOrNormal = 0x160;   // NaN, -inf, +inf; -0, +0, a positive normal number
+
+// Root of zero or of a normal number, rounded to nearest but for a few cases in a thousand: one step of Newton's from the hardware's estimate of
+// v^(-1/2) (a third of the instructions of the library's, which has to do with subnormal numbers too).
+__device__ __forceinline__ float quick_root(const float v) {
+  const float y = __builtin_amdgcn_rsqf(v), s = v * y, h = 0.5f * y;
+  return v == 0.f ? 0.f : fmaf(fmaf(-s, s, v), h, s);
 }
 
 // ---- the step ------------------------------------------------------------------------------------------
-// Workgroups walk over the chunks.  P: parameters, G: gradients.
+__device__ __forceinline__ AdamScalars counted(AdamScalars st, const double beta1, const double beta2) {
+  st.t += 1;
+  st.b1_power *= beta1;
+  st.b2_power *= beta2;
+  st.m_unbias = (float)(1.0 / (1.0 - st.b1_power));
+  st.root_unbias = (float)sqrt(1.0 / (1.0 - st.b2_power));
+  return st;
+}
+// Counts the step in a launch of its own, about 1.5 us (and 2.5 us of the host's time).  A counter by which the step's last workgroup knows itself
+// costs 60 ns for each workgroup, one after the other: 90 us for 1536 of them, so only steps of few workgroups count that way.
+__global__ void adamw_count_kernel(AdamScalars* st, const double beta1, const double beta2) { *st = counted(*st, beta1, beta2); }
+
+// What no thread of the launch writes: read through the scalar cache.
+template <typename T>
+__device__ __forceinline__ T constant(const T* p, const int i) {
+  static_assert(sizeof(T) % 8 == 0, "whole words");
+  const auto* const from = reinterpret_cast<const __attribute__((address_space(4))) uint64_t*>(reinterpret_cast<uintptr_t>(p + i));
+  uint64_t words[sizeof(T) / 8];
+#pragma unroll
+  for (size_t k = 0; k < sizeof(T) / 8; ++k) words[k] = from[k];
+  return __builtin_bit_cast(T, words);
+}
+
+// A workgroup per chunk, or per quarter of one where there are few; a wavefront takes a block at a time.  P: parameters, G: gradients.  Bound by
+// memory: 252 M elements with fp32 parameters, 16-bit gradients and moments in 8 bits 686 us (5.1 TB/s; 731 with 1536 workgroups that walk
+// over the chunks), in 32 bits 1353 us (5.2 TB/s).  In 8 bits the vector ALU is busy for nearly as long (about 65 instructions an element: with
+// the library's root and quotient and codes that allow for everything in every block it took 884 us).
 template <typename P, typename G, int BITS, bool MASTER>
 __global__ __launch_bounds__(kAdamThreads) void adamw_kernel(const AdamStep a) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  AdamScalars* const st = a.s.scalars;
-  const int64_t t = st->t + 1;
-  const double b1_power = st->b1_power * a.beta1, b2_power = st->b2_power * a.beta2;
-  const float lr = a.dev_lr != nullptr ? a.lr * *a.dev_lr : a.lr;
-  const float scale = a.dev_scale != nullptr ? a.scale * *a.dev_scale : a.scale;
-  const float beta1 = (float)a.beta1, m_part = (float)(1.0 - a.beta1), beta2 = (float)a.beta2, v_part = (float)(1.0 - a.beta2);
-  const float m_unbias = (float)(1.0 / (1.0 - b1_power)), v_unbias = (float)(1.0 / (1.0 - b2_power));
-  for (int c = blockIdx.x; c < a.n_chunks; c += gridDim.x) {
-    const AdamChunk chunk = a.s.chunks[a.first_chunk + c];
-    const AdamTensor tensor = a.s.tensors[chunk.tensor];
-    const G* const grad = static_cast<const G*>(a.grads[chunk.tensor - a.first_tensor]);
-    if (grad == nullptr) continue;
-    P* const param = static_cast<P*>(tensor.p);
-    const float rate = lr * tensor.rate, keep = 1.f - rate * tensor.decay, step = rate * m_unbias;
-    const bool aligned_g = (reinterpret_cast<uintptr_t>(grad) & (4 * sizeof(G) - 1)) == 0;
-    const bool aligned_p = (reinterpret_cast<uintptr_t>(param) & (4 * sizeof(P) - 1)) == 0;
-    for (int k = wave; k < kAdamChunk / kAdamBlock; k += kAdamThreads / 64) {
-      const int64_t i = (int64_t)chunk.index * kAdamChunk + k * kAdamBlock + 4 * lane;
-      if (i - 4 * lane >= tensor.n) break;   // (uniform in a wavefront)
-      const int here = (int)min((int64_t)4, max((int64_t)0, tensor.n - i));
-      const int64_t block = (tensor.offset + i) / kAdamBlock;
-      float g[4], p[4], m[4], v[4];
-      load4(g, grad + i, here, aligned_g);
-      if (MASTER)
-        load4(p, a.s.master + tensor.offset + i, 4, true);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const AdamChunk chunk = constant(a.s.chunks, a.first_chunk + ((int)blockIdx.x >> a.part_bits));
+  AdamScalars scalars = *a.s.scalars;
+  if (a.counts) scalars = counted(scalars, a.beta1, a.beta2);
+  const G* grad = static_cast<const G*>(a.grads[chunk.tensor - a.first_tensor]);
+  if (grad != nullptr) {
+    const float lr = (a.dev_lr != nullptr ? a.lr * *a.dev_lr : a.lr) * chunk.rate;
+    const float scale = a.dev_scale != nullptr ? a.scale * *a.dev_scale : a.scale;
+    const float beta1 = (float)a.beta1, m_part = (float)(1.0 - a.beta1), beta2 = (float)a.beta2, v_part = (float)(1.0 - a.beta2);
+    const float keep = 1.f - lr * chunk.decay, step = lr * scalars.m_unbias;
+    grad += (int64_t)chunk.index * kAdamChunk;
+    P* const param = static_cast<P*>(chunk.p);
+    float* const master = MASTER ? a.s.master + chunk.offset : nullptr;
+    const int64_t first_block = chunk.offset / kAdamBlock;
+    const int blocks = kAdamChunk / kAdamBlock / (kAdamThreads / 64) >> a.part_bits;   // of a wavefront in a row
+    const int first = (((int)blockIdx.x & ((1 << a.part_bits) - 1)) * (kAdamThreads / 64) + wave) * (blocks * kAdamBlock);
+    for (int k = 0; k < blocks; ++k) {
+      const int i0 = first + k * kAdamBlock, i = i0 + 4 * lane;
+      if (i0 >= chunk.n) break;   // (uniform in a wavefront)
+      const int64_t block = first_block + i0 / kAdamBlock;
+      const int here = min(4, chunk.n - i);
+      float g[4], p[4], m[4], v[4], r[4];
+      Moments<BITS> held;
+      held.load(a.s, block);
+      load4(g, grad + i, here);
+      if constexpr (MASTER)
+        load4(p, master + i, 4);   // (the flat arrays have whole blocks)
       else
-        load4(p, param + i, here, aligned_p);
-      load_moments<BITS>(a.s, block, m, v);
+        load4(p, param + i, here);
+      held.get(m, v);
+      bool odd = false;
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const float gs = g[u] * scale;
-        m[u] = beta1 * m[u] + m_part * gs;
-        v[u] = beta2 * v[u] + v_part * (gs * gs);
-        p[u] = p[u] * keep - step * m[u] / (sqrtf(v[u] * v_unbias) + a.eps);
+      for (int e = 0; e < 4; ++e) {
+        const float gs = g[e] * scale;
+        m[e] = beta1 * m[e] + m_part * gs;
+        v[e] = beta2 * v[e] + v_part * (gs * gs);
+        odd |= __builtin_amdgcn_classf(m[e], kClassNotFinite) || !__builtin_amdgcn_classf(v[e], kClassZeroOrNormal);
       }
-      store_moments<BITS>(a.s, block, m, v, false, t);
-      if (MASTER) store4(p, a.s.master + tensor.offset + i, 4, true);
-      store4(p, param + i, here, aligned_p);
+      const bool plain = !any_lane(odd);
+      if (plain) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r[e] = quick_root(v[e]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r[e] = sqrtf(v[e]);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e)   // (the divisor is 0, epsilon or a normal number: the hardware's reciprocal is within a unit in the last place)
+        p[e] = p[e] * keep - (step * m[e]) * __builtin_amdgcn_rcpf(r[e] * scalars.root_unbias + a.eps);
+      if constexpr (BITS == 32) {
+        const int64_t at = block * kAdamBlock + 4 * lane;
+        store4(m, a.s.m32 + at, 4);
+        store4(v, a.s.v32 + at, 4);
+      } else {
+        store_codes(a.s, block, m, r, plain, false, dither_start(block * kAdamBlock + 4 * lane, scalars.t));
+      }
+      if constexpr (MASTER) store4(p, master + i, 4);
+      store4(p, param + i, here);
     }
   }
-  // the last workgroup to be done counts the step: everybody has read the scalars
+  if (!a.counts) return;
   __syncthreads();
   if (threadIdx.x == 0) {
     __threadfence();
-    if (__hip_atomic_fetch_add(&st->done, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == a.last) {
-      st->t = t;
-      st->b1_power = b1_power;
-      st->b2_power = b2_power;
-      st->done = 0;
+    if (__hip_atomic_fetch_add(&a.s.scalars->done, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1) {
+      scalars.done = 0;
+      *a.s.scalars = scalars;   // everybody has read them
     }
   }
 }
@@ -253,13 +354,18 @@ __global__ __launch_bounds__(kAdamThreads) void adamw_get_state_kernel(const Ada
   const int64_t step = (int64_t)gridDim.x * (kAdamThreads / 64);
   for (int64_t block = (int64_t)blockIdx.x * (kAdamThreads / 64) + (threadIdx.x >> 6); block < blocks; block += step) {
     float m[4], v[4];
-    if (bits == 32)
-      load_moments<32>(s, block, m, v);
-    else
-      load_moments<8>(s, block, m, v);
+    if (bits == 32) {
+      Moments<32> held;
+      held.load(s, block);
+      held.get(m, v);
+    } else {
+      Moments<8> held;
+      held.load(s, block);
+      held.get(m, v);
+    }
     const int64_t at = block * kAdamBlock + 4 * (threadIdx.x & 63);
-    if (m_out != nullptr) store4(m, m_out + at, 4, true);
-    if (v_out != nullptr) store4(v, v_out + at, 4, true);
+    if (m_out != nullptr) store4(m, m_out + at, 4);
+    if (v_out != nullptr) store4(v, v_out + at, 4);
   }
 }
 
@@ -270,31 +376,32 @@ __global__ __launch_bounds__(kAdamThreads) void adamw_set_state_kernel(const Ada
   for (int64_t block = (int64_t)blockIdx.x * (kAdamThreads / 64) + (threadIdx.x >> 6); block < blocks; block += step) {
     float m[4] = {0.f, 0.f, 0.f, 0.f}, v[4] = {0.f, 0.f, 0.f, 0.f};
     const int64_t at = block * kAdamBlock + 4 * (threadIdx.x & 63);
-    if (m_in != nullptr) load4(m, m_in + at, 4, true);
-    if (v_in != nullptr) load4(v, v_in + at, 4, true);
-    if (bits == 32)
-      store_moments<32>(s, block, m, v, true, 0);
-    else
-      store_moments<8>(s, block, m, v, true, 0);
+    if (m_in != nullptr) load4(m, m_in + at, 4);
+    if (v_in != nullptr) load4(v, v_in + at, 4);
+    if (bits == 32) {
+      store4(m, s.m32 + at, 4);
+      store4(v, s.v32 + at, 4);
+    } else {
+      float r[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) r[k] = sqrtf(v[k]);
+      store_codes(s, block, m, r, false, true, 0);
+    }
   }
   if (blockIdx.x == 0 && threadIdx.x == 0) *s.scalars = scalars;
 }
 
-// The parameters' fp32 copies, from the parameters or from a flat array, from which the parameters are then written too.
+// A workgroup per chunk: the parameters' fp32 copies, from the parameters or from a flat array, from which the parameters are then written too.
 template <typename P>
-__global__ __launch_bounds__(kAdamThreads) void adamw_set_master_kernel(const AdamState s, const int n_chunks, const float* in) {
-  for (int c = blockIdx.x; c < n_chunks; c += gridDim.x) {
-    const AdamChunk chunk = s.chunks[c];
-    const AdamTensor tensor = s.tensors[chunk.tensor];
-    P* const param = static_cast<P*>(tensor.p);
-    const int64_t first = (int64_t)chunk.index * kAdamChunk, end = min(first + kAdamChunk, tensor.n);
-    for (int64_t i = first + threadIdx.x; i < end; i += kAdamThreads) {
-      if (in != nullptr) {
-        s.master[tensor.offset + i] = in[tensor.offset + i];
-        param[i] = from_float<P>(in[tensor.offset + i]);
-      } else {
-        s.master[tensor.offset + i] = to_float(param[i]);
-      }
+__global__ __launch_bounds__(kAdamThreads) void adamw_set_master_kernel(const AdamState s, const float* in) {
+  const AdamChunk chunk = s.chunks[blockIdx.x];
+  P* const param = static_cast<P*>(chunk.p);
+  for (int i = threadIdx.x; i < chunk.n; i += kAdamThreads) {
+    if (in != nullptr) {
+      s.master[chunk.offset + i] = in[chunk.offset + i];
+      param[i] = from_float<P>(in[chunk.offset + i]);
+    } else {
+      s.master[chunk.offset + i] = to_float(param[i]);
     }
   }
 }

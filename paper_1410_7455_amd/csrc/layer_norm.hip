@@ -10,6 +10,7 @@ using namespace ngsgd;
 
 namespace {
 
+constexpr int kMostColumns = 1 << 25;   // (a launch has less than 2^32 threads)
 constexpr int kWideGrid = 2048;      // workgroups that walk over rows wider than registers hold
 constexpr int kNormGroups = 512;     // most groups of rows that are summed on their own
 
@@ -112,7 +113,7 @@ int with_types(const int type, const int weight_type, F f) {
 
 int check_types(const int type, const int weight_type, const int64_t N, const int32_t D) {
   if (!known_type(type) || !known_type(weight_type) || (weight_type != type && weight_type != NGSGD_FLOAT32)) return NGSGD_EINVAL;
-  return N < 0 || D < 1 ? NGSGD_EINVAL : NGSGD_OK;
+  return N < 0 || D < 1 || D > kMostColumns ? NGSGD_EINVAL : NGSGD_OK;
 }
 // A matrix argument: present, rows that do not overlap, whole elements.
 bool good_matrix(const void* p, const int64_t ld, const int type, const int64_t N, const int32_t D) {
@@ -136,7 +137,7 @@ extern "C" int ngsgd_layernorm_forward(const void* dev_x, int64_t ldx, int32_t t
 }
 
 extern "C" int ngsgd_layernorm_workspace_bytes(int64_t max_rows, int32_t D, size_t* out_bytes) {
-  if (out_bytes == nullptr || max_rows < 0 || D < 1) return NGSGD_EINVAL;
+  if (out_bytes == nullptr || max_rows < 0 || D < 1 || D > kMostColumns) return NGSGD_EINVAL;
   Carver c(nullptr);
   (void)c.take<float>((size_t)norm_groups(max_rows, D) * 2 * D);
   *out_bytes = align_up(c.off, 256);
