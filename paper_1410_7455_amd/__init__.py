@@ -251,28 +251,48 @@ def precondition_simple_static(M, alpha=4.0, epsilon=1e-20, gamma=None, rownorm2
            "ngsgd_precondition_simple_static")
 
 
+_TYPES = {}
+
+
 def _type_of(dtype):
     """NGSGD_FLOAT32 / _BFLOAT16 / _FLOAT16 of a torch dtype."""
-    name = str(dtype)
-    codes = {"torch.float32": NGSGD_FLOAT32, "torch.bfloat16": NGSGD_BFLOAT16, "torch.float16": NGSGD_FLOAT16}
-    if name not in codes:
-        raise ValueError(f"{name}: the types are float32, bfloat16 and float16")
-    return codes[name]
+    if not _TYPES:
+        import torch
+        _TYPES.update({torch.float32: NGSGD_FLOAT32, torch.bfloat16: NGSGD_BFLOAT16, torch.float16: NGSGD_FLOAT16})
+    code = _TYPES.get(dtype)
+    if code is None:
+        raise ValueError(f"{dtype}: the types are float32, bfloat16 and float16")
+    return code
 
 
-def _require(condition, message):
-    """Argument checks that keep a kernel inside its buffers: they hold where assertions are switched off too."""
-    if not condition:
-        raise ValueError(message)
+# The argument checks below keep a kernel inside its buffers: they raise where assertions are switched off too.  Messages are only
+# formed when they are needed (the calls are short: a small layer norm takes 2 us on the GPU).
 
-
-def _check_tensor(t, name, dtype=None, numel=None):
-    """A dense tensor on the current device."""
+def _current_device(device):
     import torch
-    _require(t.is_cuda and t.device.index == torch.cuda.current_device(), f"{name} is not on the current device")
-    _require(t.is_contiguous(), f"{name} is not dense")
-    _require(dtype is None or t.dtype == dtype, f"{name} is {t.dtype}, not {dtype}")
-    _require(numel is None or t.numel() == numel, f"{name} has {t.numel()} elements, not {numel}")
+    if device.index != torch.cuda.current_device():
+        raise ValueError(f"made for {device}, which is not the current device")
+
+
+def _check_dense(t, name, device, dtype=None, numel=None):
+    """A dense tensor on the device."""
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, not on {device}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} is not dense")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{name} is {t.dtype}, not {dtype}")
+    if numel is not None and t.numel() != numel:
+        raise ValueError(f"{name} has {t.numel()} elements, not {numel}")
+
+
+def _raw_stream(stream, device):
+    import torch
+    return (torch.cuda.current_stream(device.index) if stream is None else stream).cuda_stream
+
+
+def _address(t):
+    return None if t is None else t.data_ptr()
 
 
 def _allocate_on(stream):
@@ -296,67 +316,88 @@ class LayerNorm:
         _check(self.lib.ngsgd_layernorm_workspace_bytes(max_rows, dim, byref(nbytes)), "ngsgd_layernorm_workspace_bytes")
         self.workspace_bytes = nbytes.value
         self.workspace = torch.empty(nbytes.value, dtype=torch.uint8, device="cuda")
+        self.device = self.workspace.device
 
     def _rows(self, t, name, like=None):
-        """(rows x dim view of t, leading dimension)"""
-        import torch
-        _require(t.is_cuda and t.device.index == torch.cuda.current_device(), f"{name} is not on the current device")
-        _require(t.dim() >= 1 and t.shape[-1] == self.dim, f"{name} does not end in {self.dim} columns")
-        _require(t.stride(-1) == 1 or self.dim == 1, f"{name}: rows are not dense")
-        _require(like is None or (t.dtype == like.dtype and t.shape == like.shape), f"{name} has another type or shape than x")
-        if t.dim() != 2:
-            t = t.view(t.numel() // self.dim, self.dim)
-        _require(t.shape[0] <= self.max_rows, f"{name} has more than {self.max_rows} rows")
-        return t, (t.stride(0) if t.shape[0] > 1 else self.dim)
+        """(number of rows, leading dimension)"""
+        if t.device != self.device:
+            raise ValueError(f"{name} is on {t.device}, not on {self.device}")
+        shape = t.shape
+        if len(shape) < 1 or shape[-1] != self.dim:
+            raise ValueError(f"{name} does not end in {self.dim} columns")
+        if like is not None and (t.dtype != like.dtype or shape != like.shape):
+            raise ValueError(f"{name} has another type or shape than x")
+        if len(shape) != 2:
+            t = t.view(-1, self.dim) if t.numel() else t.new_empty(0, self.dim)
+        rows = t.shape[0]
+        ld, inner = t.stride()
+        if inner != 1 and self.dim != 1:
+            raise ValueError(f"{name}: rows are not dense")
+        if rows > self.max_rows:
+            raise ValueError(f"{name} has more than {self.max_rows} rows")
+        return rows, ld if rows > 1 else self.dim
 
-    def _vectors(self, x, *named):
-        """NGSGD_* type of the given weights (that of the first one present; float32 if there is none)."""
-        present = [(name, v) for name, v in named if v is not None]
-        if not present:
-            return NGSGD_FLOAT32
-        dtype = present[0][1].dtype
-        _require(dtype == x.dtype or str(dtype) == "torch.float32", f"{present[0][0]} is {dtype} for {x.dtype} rows")
-        for name, v in present:
-            _check_tensor(v, name, dtype, self.dim)
-        return _type_of(dtype)
+    def _vector_dtype(self, x, *named):
+        """The type of the given weights (of the first one present; float32 if there is none)."""
+        import torch
+        dtype = None
+        for name, v in named:
+            if v is None:
+                continue
+            if dtype is None:
+                dtype = v.dtype
+                if dtype != x.dtype and dtype != torch.float32:
+                    raise ValueError(f"{name} is {dtype} for {x.dtype} rows")
+            _check_dense(v, name, self.device, dtype, self.dim)
+        return torch.float32 if dtype is None else dtype
 
     def forward(self, x, weight=None, bias=None, out=None, mean=None, rstd=None, stream=None):
         """(y, mean, rstd); y into `out` if given (which may be x), the rows' float32 mean and rstd into `mean` and `rstd`."""
         import torch
+        _current_device(self.device)
         rows, ldx = self._rows(x, "x")
-        weight_type = self._vectors(x, ("weight", weight), ("bias", bias))
-        with _allocate_on(stream):
-            out = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
-            mean = torch.empty(rows.shape[0], dtype=torch.float32, device=x.device) if mean is None else mean
-            rstd = torch.empty(rows.shape[0], dtype=torch.float32, device=x.device) if rstd is None else rstd
-        out_rows, ldy = self._rows(out, "out", like=x)
-        _check_tensor(mean, "mean", torch.float32, rows.shape[0])
-        _check_tensor(rstd, "rstd", torch.float32, rows.shape[0])
-        _check(self.lib.ngsgd_layernorm_forward(_ptr(rows), ldx, _type_of(x.dtype), _ptr(weight), _ptr(bias), weight_type,
-                                                rows.shape[0], self.dim, self.epsilon, _ptr(out_rows), ldy, _ptr(mean),
-                                                _ptr(rstd), _stream_ptr(stream)), "ngsgd_layernorm_forward")
+        weight_type = _type_of(self._vector_dtype(x, ("weight", weight), ("bias", bias)))
+        ldy = self.dim if out is None else self._rows(out, "out", x)[1]
+        for name, v in (("mean", mean), ("rstd", rstd)):
+            if v is not None:
+                _check_dense(v, name, self.device, torch.float32, rows)
+        if out is None or mean is None or rstd is None:
+            with _allocate_on(stream):
+                if out is None:
+                    out = torch.empty_like(x, memory_format=torch.contiguous_format)
+                if mean is None:
+                    mean = torch.empty(rows, dtype=torch.float32, device=self.device)
+                if rstd is None:
+                    rstd = torch.empty(rows, dtype=torch.float32, device=self.device)
+        _check(self.lib.ngsgd_layernorm_forward(x.data_ptr(), ldx, _type_of(x.dtype), _address(weight), _address(bias), weight_type,
+                                                rows, self.dim, self.epsilon, out.data_ptr(), ldy, mean.data_ptr(),
+                                                rstd.data_ptr(), _raw_stream(stream, self.device)), "ngsgd_layernorm_forward")
         return out, mean, rstd
 
     def backward(self, dy, x, mean, rstd, weight=None, needs=(True, True, True), dx=None, dweight=None, dbias=None,
                  stream=None):
         """(dx, dweight, dbias) for the derivative dy of y and the mean and rstd of the forward pass; None where `needs`
-        says so.  dx may be dy.  dweight and dbias are of the weight's type (float32 without a weight)."""
+        says so and none is given.  dx may be dy.  dweight and dbias are of the weight's type (float32 without a weight)."""
         import torch
+        _current_device(self.device)
         rows, ldx = self._rows(x, "x")
-        dy_rows, lddy = self._rows(dy, "dy", like=x)
-        _check_tensor(mean, "mean", torch.float32, rows.shape[0])
-        _check_tensor(rstd, "rstd", torch.float32, rows.shape[0])
-        weight_type = self._vectors(x, ("weight", weight), ("dweight", dweight), ("dbias", dbias))
-        vector_dtype = next((v.dtype for v in (weight, dweight, dbias) if v is not None), torch.float32)
+        _, lddy = self._rows(dy, "dy", x)
+        _check_dense(mean, "mean", self.device, torch.float32, rows)
+        _check_dense(rstd, "rstd", self.device, torch.float32, rows)
+        vector = self._vector_dtype(x, ("weight", weight), ("dweight", dweight), ("dbias", dbias))
+        lddx = self.dim if dx is None else self._rows(dx, "dx", x)[1]
         with _allocate_on(stream):
-            dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if dx is None and needs[0] else dx
-            dweight = torch.empty(self.dim, dtype=vector_dtype, device=x.device) if dweight is None and needs[1] else dweight
-            dbias = torch.empty(self.dim, dtype=vector_dtype, device=x.device) if dbias is None and needs[2] else dbias
-        dx_rows, lddx = (None, self.dim) if dx is None else self._rows(dx, "dx", like=x)
-        _check(self.lib.ngsgd_layernorm_backward(_ptr(dy_rows), lddy, _ptr(rows), ldx, _type_of(x.dtype), _ptr(weight),
-                                                 weight_type, _ptr(mean), _ptr(rstd), rows.shape[0], self.dim, _ptr(dx_rows),
-                                                 lddx, _ptr(dweight), _ptr(dbias), _ptr(self.workspace),
-                                                 self.workspace_bytes, _stream_ptr(stream)), "ngsgd_layernorm_backward")
+            if dx is None and needs[0]:
+                dx = torch.empty_like(x, memory_format=torch.contiguous_format)
+            if dweight is None and needs[1]:
+                dweight = torch.empty(self.dim, dtype=vector, device=self.device)
+            if dbias is None and needs[2]:
+                dbias = torch.empty(self.dim, dtype=vector, device=self.device)
+        _check(self.lib.ngsgd_layernorm_backward(dy.data_ptr(), lddy, x.data_ptr(), ldx, _type_of(x.dtype), _address(weight),
+                                                 _type_of(vector), mean.data_ptr(), rstd.data_ptr(), rows, self.dim,
+                                                 _address(dx), lddx, _address(dweight), _address(dbias),
+                                                 self.workspace.data_ptr(), self.workspace_bytes, _raw_stream(stream, self.device)),
+               "ngsgd_layernorm_backward")
         return dx, dweight, dbias
 
 
@@ -374,10 +415,14 @@ class AdamW:
         self.lib = load_library()
         self.params = list(params)
         n = len(self.params)
-        _require(n > 0, "no parameters")
-        dtype = self.params[0].dtype
+        if n == 0:
+            raise ValueError("no parameters")
+        if not self.params[0].is_cuda:
+            raise ValueError("the parameters are not on the GPU")
+        self.device, dtype = self.params[0].device, self.params[0].dtype
+        _current_device(self.device)
         for i, p in enumerate(self.params):
-            _check_tensor(p, f"parameter {i}", dtype)
+            _check_dense(p, f"parameter {i}", self.device, dtype)
         self.grad_dtype = dtype if grad_dtype is None else grad_dtype
         self.sizes = [p.numel() for p in self.params]
         self.offsets, at = [], 0
@@ -387,7 +432,8 @@ class AdamW:
 
         def per_tensor(value, name):
             values = list(value) if isinstance(value, (list, tuple)) else [float(value)] * n
-            _require(len(values) == n, f"{len(values)} numbers in {name} for {n} tensors")
+            if len(values) != n:
+                raise ValueError(f"{len(values)} numbers in {name} for {n} tensors")
             return (c_float * n)(*values)
 
         cfg = ngsgd_adamw_config(n, (c_void_p * n)(*[p.data_ptr() for p in self.params]), (c_int64 * n)(*self.sizes),
@@ -396,7 +442,7 @@ class AdamW:
         nbytes = c_size_t(0)
         _check(self.lib.ngsgd_adamw_workspace_bytes(byref(cfg), byref(nbytes)), "ngsgd_adamw_workspace_bytes")
         self.workspace_bytes = nbytes.value
-        self.workspace = torch.empty(nbytes.value, dtype=torch.uint8, device="cuda")
+        self.workspace = torch.empty(nbytes.value, dtype=torch.uint8, device=self.device)
         h = c_void_p(0)
         _check(self.lib.ngsgd_adamw_create(byref(cfg), _ptr(self.workspace), nbytes.value, byref(h)), "ngsgd_adamw_create")
         self.handle = h
@@ -429,36 +475,41 @@ class AdamW:
         """One step.  grads: a dense tensor of grad_dtype for each parameter, or None to leave that one as it is.  lr and grad_scale are
         numbers or float32 tensors of one element on the device."""
         import torch
-        _require(len(grads) == len(self.params), f"{len(grads)} gradients for {len(self.params)} tensors")
-        array, dtype, device = self._grads, self.grad_dtype, self.params[0].device
-        _require(device.index == torch.cuda.current_device(), "the parameters are not on the current device")
-        for i, g in enumerate(grads):
-            if g is None or self.sizes[i] == 0:
-                array[i] = None
+        device, dtype, sizes, addresses = self.device, self.grad_dtype, self.sizes, []
+        _current_device(device)
+        if len(grads) != len(sizes):
+            raise ValueError(f"{len(grads)} gradients for {len(sizes)} tensors")
+        for g, size in zip(grads, sizes):
+            if g is None or size == 0:
+                addresses.append(None)
                 continue
-            if g.dtype != dtype or g.numel() != self.sizes[i] or g.device != device or not g.is_contiguous():
-                raise ValueError(f"gradient {i}: {g.dtype}, {g.numel()} elements on {g.device}, for {dtype}, {self.sizes[i]} on "
+            if g.dtype != dtype or g.numel() != size or g.device != device or not g.is_contiguous():
+                raise ValueError(f"gradient {len(addresses)}: {g.dtype}, {g.numel()} elements on {g.device}, for {dtype}, {size} on "
                                  f"{device}, dense")
-            array[i] = g.data_ptr()
+            addresses.append(g.data_ptr())
+        self._grads[:] = addresses
         factors = []
         for name, value in (("lr", lr), ("grad_scale", grad_scale)):
             if isinstance(value, torch.Tensor):
-                _check_tensor(value, name, torch.float32, 1)
-                factors += [1.0, c_void_p(value.data_ptr())]
+                _check_dense(value, name, device, torch.float32, 1)
+                factors += [1.0, value.data_ptr()]
             else:
-                factors += [1.0 if value is None else float(value), c_void_p(0)]
-        _check(self.lib.ngsgd_adamw_step(self.handle, array, *factors, _stream_ptr(stream)), "ngsgd_adamw_step")
+                factors += [1.0 if value is None else value, None]
+        _check(self.lib.ngsgd_adamw_step(self.handle, self._grads, *factors, _raw_stream(stream, self.device)), "ngsgd_adamw_step")
 
     def state(self, dtype=None, stream=None):
         """(m, v), flat; tensor k's are [offsets[k] : offsets[k] + sizes[k]].  With 32 bits the arrays themselves (or copies in
-        bfloat16, if asked for); with 8 bits the values of the codes, in float32 or in bfloat16, which holds them exactly."""
+        bfloat16, if asked for); with 8 bits the values of the codes, in float32 or in bfloat16, which holds them exactly (but for a
+        v below 2^-126)."""
         import torch
         dtype = torch.float32 if dtype is None else dtype
         if self._m is not None and dtype == torch.float32:
             return self._m, self._v
+        _current_device(self.device)
         with _allocate_on(stream):
-            m, v = (torch.empty(self.elements, dtype=dtype, device=self.workspace.device) for _ in range(2))
-        _check(self.lib.ngsgd_adamw_get_state(self.handle, _ptr(m), _ptr(v), _type_of(dtype), c_void_p(0), _stream_ptr(stream)),
+            m = torch.empty(self.elements, dtype=dtype, device=self.device)
+            v = torch.empty(self.elements, dtype=dtype, device=self.device)
+        _check(self.lib.ngsgd_adamw_get_state(self.handle, m.data_ptr(), v.data_ptr(), _type_of(dtype), None, _raw_stream(stream, self.device)),
                "ngsgd_adamw_get_state")
         return m, v
 
@@ -466,17 +517,19 @@ class AdamW:
         """Installs flat float32 moments (None: zeros) and the step count; the fp32 copies from `master` (flat), which is rounded to the
         parameters too, or from the parameters."""
         import torch
+        _current_device(self.device)
         for name, a in (("m", m), ("v", v), ("master", master)):
             if a is not None:
-                _check_tensor(a, name, torch.float32, self.elements)
-        _check(self.lib.ngsgd_adamw_set_state(self.handle, _ptr(m), _ptr(v), _ptr(master), int(t), _stream_ptr(stream)),
+                _check_dense(a, name, self.device, torch.float32, self.elements)
+        _check(self.lib.ngsgd_adamw_set_state(self.handle, _address(m), _address(v), _address(master), int(t), _raw_stream(stream, self.device)),
                "ngsgd_adamw_set_state")
 
     def steps(self):
         """The step count; waits for the stream."""
         import torch
-        t = torch.empty(1, dtype=torch.int64, device=self.workspace.device)
-        _check(self.lib.ngsgd_adamw_get_state(self.handle, c_void_p(0), c_void_p(0), NGSGD_FLOAT32, _ptr(t), _stream_ptr()),
+        _current_device(self.device)
+        t = torch.empty(1, dtype=torch.int64, device=self.device)
+        _check(self.lib.ngsgd_adamw_get_state(self.handle, None, None, NGSGD_FLOAT32, t.data_ptr(), _raw_stream(None, self.device)),
                "ngsgd_adamw_get_state")
         return int(t.item())
 

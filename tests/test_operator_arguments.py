@@ -128,8 +128,10 @@ def test_binding_refuses_tensors_off_the_device():
     with pytest.raises(ValueError):
         ng.AdamW([])
     ln = ng.LayerNorm.__new__(ng.LayerNorm)
-    ln.max_rows, ln.dim, ln.epsilon = 4, 8, 1e-5
+    ln.max_rows, ln.dim, ln.epsilon, ln.device = 4, 8, 1e-5, torch.device("cuda", 0)
     with pytest.raises(ValueError):
-        ln.forward(torch.zeros(2, 8))
+        ln._rows(torch.zeros(2, 8), "x")
+    with pytest.raises(ValueError):
+        ng._check_dense(torch.zeros(8), "weight", ln.device)
     with pytest.raises(ValueError):
         ng._type_of(torch.float64)
