@@ -103,18 +103,26 @@ constexpr uint32_t kLowestM = 16, kLowestV = 32;
 __device__ __forceinline__ int base_m(const uint32_t e) { return (int)(e + 1) * 8 - 128; }
 __device__ __forceinline__ int base_v(const uint32_t e) { return (int)(e + 1) * 8 - 255; }
 
-__device__ __forceinline__ uint32_t code_m(const float m, const int base, const uint32_t dither) {
-  const uint32_t bits = __builtin_bit_cast(uint32_t, m), a = bits & 0x7fffffffu;
-  if (!finite_bits(a)) return 0x80;
-  const float magnitude = __builtin_bit_cast(float, a), least = __builtin_bit_cast(float, (uint32_t)(base + 1) << 20);
-  int code = min(max((int)((a + dither) >> 20) - base, 1), 127);
-  if (magnitude < least) code = magnitude > least * ((float)dither * 0x1p-20f) ? 1 : 0;
-  return code == 0 ? 0u : (uint32_t)code | (bits >> 31 << 7);
+// What is coded is held in 64 bits: with m or the root rounded to 32 first, one code in some 10^6 would lie on the other side of a border.
+// The upper 15 bits of such a number (sign apart) are its binade and eighth: code = those, minus the block's base in the same units.
+constexpr int kBase64 = (1023 - 127) * 8;   // between the two formats' exponents
+__device__ __forceinline__ uint64_t bits_of(const double x) { return __builtin_bit_cast(uint64_t, x); }
+__device__ __forceinline__ uint32_t eighths(const uint64_t magnitude, const uint32_t dither) {
+  return (uint32_t)((magnitude + ((uint64_t)dither << 29)) >> 49);
 }
-__device__ __forceinline__ uint32_t code_root(const float r, const int base, const uint32_t dither) {
-  const uint32_t bits = __builtin_bit_cast(uint32_t, r);
-  if (!finite_bits(bits)) return 255u;   // (a root is not negative; that of a negative number is NaN)
-  return bits == 0 ? 0u : (uint32_t)min(max((int)((bits + dither) >> 20) - base, 1), 254);
+__device__ __forceinline__ double least_of(const int base) { return __builtin_bit_cast(double, (uint64_t)(base + 1 + kBase64) << 49); }
+
+__device__ __forceinline__ uint32_t code_m(const double m, const int base, const uint32_t dither) {
+  const uint64_t bits = bits_of(m), a = bits & ~(1ull << 63);
+  if (!(fabs(m) <= 3.4028234663852886e38)) return 0x80;   // (what fp32 holds)
+  const double least = least_of(base);
+  int code = min(max((int)eighths(a, dither) - base - kBase64, 1), 127);
+  if (fabs(m) < least) code = fabs(m) > least * ((double)dither * 0x1p-20) ? 1 : 0;
+  return code == 0 ? 0u : (uint32_t)code | (uint32_t)(bits >> 63 << 7);
+}
+__device__ __forceinline__ uint32_t code_root(const double r, const int base, const uint32_t dither) {
+  if (!(r <= 3.4028234663852886e38)) return 255u;   // (a root is not negative; that of a negative number is NaN)
+  return r == 0.0 ? 0u : (uint32_t)min(max((int)eighths(bits_of(r), dither) - base - kBase64, 1), 254);
 }
 
 // Four consecutive elements of a lane; `here` of them exist.
@@ -191,15 +199,15 @@ struct Moments<8> {
 };
 
 // Codes of a lane's four elements of block `block`, given m and the roots of v.  `plain`: all are finite.  `start`: see dither_start.
-__device__ __forceinline__ void store_codes(const AdamState& s, const int64_t block, const float (&m)[4], const float (&r)[4], const bool plain,
+__device__ __forceinline__ void store_codes(const AdamState& s, const int64_t block, const double (&m)[4], const double (&r)[4], const bool plain,
                                             const bool nearest, const uint32_t start) {
   const int lane = threadIdx.x & 63;
   const int64_t at = block * kAdamBlock + 4 * lane;
-  uint32_t a[4], b[4], dither[4];
+  uint32_t a[4], b[4], dither[4];   // as fp32
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
-    a[k] = __builtin_bit_cast(uint32_t, m[k]) & 0x7fffffffu;
-    b[k] = __builtin_bit_cast(uint32_t, r[k]) & 0x7fffffffu;
+    a[k] = __builtin_bit_cast(uint32_t, (float)m[k]) & 0x7fffffffu;
+    b[k] = __builtin_bit_cast(uint32_t, (float)r[k]) & 0x7fffffffu;
     dither[k] = nearest ? kDitherHalf : dither_of(start, k);
   }
   uint32_t mt = max(max(a[0], a[1]), max(a[2], a[3])), rt = max(max(b[0], b[1]), max(b[2], b[3])), nan = 0;
@@ -216,13 +224,15 @@ __device__ __forceinline__ void store_codes(const AdamState& s, const int64_t bl
   }
   const uint32_t me = exponent_of(wave_max_u32(mt), kLowestM), ve = exponent_of(wave_max_u32(rt), kLowestV);
   const int mb = base_m(me), vb = base_v(ve);
-  const uint32_t m_least = (uint32_t)(mb + 1) << 20, r_least = (uint32_t)(vb + 1) << 20;
+  // (a code's first number and the one above it: what rounds to the first in fp32 is not below it by more than that)
+  const uint32_t m_least = ((uint32_t)(mb + 1) << 20) + 1, r_least = ((uint32_t)(vb + 1) << 20) + 1;
   uint32_t mc = 0, vc = 0;
   if (plain && !any_lane(min(min(a[0], a[1]), min(a[2], a[3])) < m_least || min(min(b[0], b[1]), min(b[2], b[3])) < r_least)) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {   // what the general form comes to where nothing is below the least code
-      mc |= (min(((a[k] + dither[k]) >> 20) - (uint32_t)mb, 127u) | (__builtin_bit_cast(uint32_t, m[k]) >> 24 & 0x80u)) << (8 * k);
-      vc |= min(((b[k] + dither[k]) >> 20) - (uint32_t)vb, 254u) << (8 * k);
+      const uint64_t bits = bits_of(m[k]);
+      mc |= (min(eighths(bits & ~(1ull << 63), dither[k]) - (uint32_t)(mb + kBase64), 127u) | ((uint32_t)(bits >> 56) & 0x80u)) << (8 * k);
+      vc |= min(eighths(bits_of(r[k]), dither[k]) - (uint32_t)(vb + kBase64), 254u) << (8 * k);
     }
   } else {
 #pragma unroll
@@ -239,11 +249,17 @@ __device__ __forceinline__ void store_codes(const AdamState& s, const int64_t bl
 // Classes of fp32 numbers, as v_cmp_class takes them.
 constexpr int kClassNotFinite = 0x207, kClassZeroOrNormal = 0x160;   // NaN, -inf, +inf; -0, +0, a positive normal number
 
-// Root of zero or of a normal number, rounded to nearest but for a few cases in a thousand: one step of Newton's from the hardware's estimate of
-// v^(-1/2) (a third of the instructions of the library's, which has to do with subnormal numbers too).
+// Root of zero or of a number that is normal in fp32, by one step of Newton's from the hardware's estimate of v^(-1/2) (a third of the
+// instructions of the library's, which has to do with subnormal numbers too): rounded to nearest in fp32 but for a few cases in a thousand, and
+// with the step in 64 bits off by 2^-45 of itself.
 __device__ __forceinline__ float quick_root(const float v) {
   const float y = __builtin_amdgcn_rsqf(v), s = v * y, h = 0.5f * y;
   return v == 0.f ? 0.f : fmaf(fmaf(-s, s, v), h, s);
+}
+__device__ __forceinline__ double quick_root(const double v, const float v32) {
+  const float y = __builtin_amdgcn_rsqf(v32);
+  const double s = (double)(v32 * y);
+  return v32 == 0.f ? 0.0 : fma(fma(-s, s, v), (double)(0.5f * y), s);
 }
 
 // ---- the step ------------------------------------------------------------------------------------------
@@ -271,9 +287,10 @@ __device__ __forceinline__ T constant(const T* p, const int i) {
 }
 
 // A workgroup per chunk, or per quarter of one where there are few; a wavefront takes a block at a time.  P: parameters, G: gradients.  Bound by
-// memory: 252 M elements with fp32 parameters, 16-bit gradients and moments in 8 bits 686 us (5.1 TB/s; 731 with 1536 workgroups that walk
-// over the chunks), in 32 bits 1353 us (5.2 TB/s).  In 8 bits the vector ALU is busy for nearly as long (about 65 instructions an element: with
-// the library's root and quotient and codes that allow for everything in every block it took 884 us).
+// memory: 252 M elements with fp32 parameters, 16-bit gradients and moments in 8 bits 694 us (5.1 TB/s; 45 more with 1536 workgroups that walk
+// over the chunks), in 32 bits 1353 us (5.2 TB/s).  In 8 bits the vector ALU is busy for nearly as long (about 75 instructions an element: with
+// the library's root and quotient and codes that allow for everything in every block it took 884 us), and parameters and gradients of 16
+// bits leave it the bound (201 M elements 491 us, 4.1 TB/s).
 template <typename P, typename G, int BITS, bool MASTER>
 __global__ __launch_bounds__(kAdamThreads) void adamw_kernel(const AdamStep a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -307,30 +324,40 @@ __global__ __launch_bounds__(kAdamThreads) void adamw_kernel(const AdamStep a) {
         load4(p, param + i, here);
       held.get(m, v);
       bool odd = false;
+      double m64[4], v64[4], r64[4];   // moments that will be coded
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float gs = g[e] * scale;
-        m[e] = beta1 * m[e] + m_part * gs;
-        v[e] = beta2 * v[e] + v_part * (gs * gs);
+        if constexpr (BITS == 32) {
+          const float gs = g[e] * scale;
+          m[e] = beta1 * m[e] + m_part * gs;
+          v[e] = beta2 * v[e] + v_part * (gs * gs);
+        } else {
+          const double gs = (double)g[e] * (double)scale;
+          m64[e] = a.beta1 * (double)m[e] + (1.0 - a.beta1) * gs;
+          v64[e] = a.beta2 * (double)v[e] + (1.0 - a.beta2) * (gs * gs);
+          m[e] = (float)m64[e];
+          v[e] = (float)v64[e];
+        }
         odd |= __builtin_amdgcn_classf(m[e], kClassNotFinite) || !__builtin_amdgcn_classf(v[e], kClassZeroOrNormal);
       }
       const bool plain = !any_lane(odd);
-      if (plain) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) r[e] = quick_root(v[e]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) r[e] = sqrtf(v[e]);
-      }
-#pragma unroll
-      for (int e = 0; e < 4; ++e)   // (the divisor is 0, epsilon or a normal number: the hardware's reciprocal is within a unit in the last place)
+      for (int e = 0; e < 4; ++e) {
+        if constexpr (BITS == 32) {
+          r[e] = plain ? quick_root(v[e]) : sqrtf(v[e]);
+        } else {
+          r64[e] = plain ? quick_root(v64[e], v[e]) : sqrt(v64[e]);
+          r[e] = (float)r64[e];
+        }
+        // (the divisor is 0, epsilon or a normal number: the hardware's reciprocal is within a unit in the last place)
         p[e] = p[e] * keep - (step * m[e]) * __builtin_amdgcn_rcpf(r[e] * scalars.root_unbias + a.eps);
+      }
       if constexpr (BITS == 32) {
         const int64_t at = block * kAdamBlock + 4 * lane;
         store4(m, a.s.m32 + at, 4);
         store4(v, a.s.v32 + at, 4);
       } else {
-        store_codes(a.s, block, m, r, plain, false, dither_start(block * kAdamBlock + 4 * lane, scalars.t));
+        store_codes(a.s, block, m64, r64, plain, false, dither_start(block * kAdamBlock + 4 * lane, scalars.t));
       }
       if constexpr (MASTER) store4(p, master + i, 4);
       store4(p, param + i, here);
@@ -382,10 +409,13 @@ __global__ __launch_bounds__(kAdamThreads) void adamw_set_state_kernel(const Ada
       store4(m, s.m32 + at, 4);
       store4(v, s.v32 + at, 4);
     } else {
-      float r[4];
+      double m64[4], r64[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) r[k] = sqrtf(v[k]);
-      store_codes(s, block, m, r, false, true, 0);
+      for (int k = 0; k < 4; ++k) {
+        m64[k] = (double)m[k];
+        r64[k] = sqrt((double)v[k]);
+      }
+      store_codes(s, block, m64, r64, false, true, 0);
     }
   }
   if (blockIdx.x == 0 && threadIdx.x == 0) *s.scalars = scalars;
