@@ -52,6 +52,7 @@ extern "C" {
 
 #define NGSGD_TANH 0
 #define NGSGD_PNORM 1
+#define NGSGD_LAYERNORM 16   /* added to either: a layer norm follows, with a weight and a bias of its own */
 
 /* Element types of the operators that take 16-bit data. */
 #define NGSGD_FLOAT32 0
@@ -63,6 +64,8 @@ extern "C" {
 
 #define NGSGD_METHOD_ONLINE 0 /* Fisher factors from previous minibatches, App. B (the default)   */
 #define NGSGD_METHOD_SIMPLE 1 /* Fisher factors from the other rows of the minibatch, App. A    */
+#define NGSGD_METHOD_ADAMW 2  /* no factors: AdamW with the plain gradient, moments in fp32     */
+#define NGSGD_METHOD_ADAMW8 3 /* the same with moments in 8 bits                                */
 
 #define NGSGD_SIDE_INPUT 0   /* preconditioner of the layer-input matrix [X_l, 1]   */
 #define NGSGD_SIDE_OUTPUT 1  /* preconditioner of the output-derivative matrix O_l  */
@@ -76,7 +79,11 @@ typedef struct ngsgd_precond ngsgd_precond;  /* one instance of the online metho
  * A p-norm layer (p = 2) maps groups of `pnorm_group` adjacent outputs to their 2-norm, so the
  * next layer's input dimension is dims[l+1] / pnorm_group (must divide).  Each affine layer keeps
  * its bias as the last column of its weight matrix: W_l is dims[l+1] x (in_dim_l + 1)
- * (Sec. 4.4 of the paper).  Defaults of App. B.4/B.5: rank_in 20, rank_out 80, alpha 4,
+ * (Sec. 4.4 of the paper).  nonlin[l] | NGSGD_LAYERNORM puts a layer norm (epsilon 1e-5) between the nonlinearity
+ * (renormalised or not) and the next layer; its weight and bias have no input and output side to precondition:
+ * AdamW updates them with every method, at the step's learning rate (see ngsgd_set_adamw).  With the AdamW methods
+ * max_change_per_sample has to be 0, and ranks and the other numbers of the preconditioner are not used.
+ * Defaults of App. B.4/B.5: rank_in 20, rank_out 80, alpha 4,
  * num_samples_history 2000, epsilon 1e-10, update_period 4, always_update_first 10. */
 typedef struct {
   int32_t n_layers;
@@ -92,7 +99,7 @@ typedef struct {
   int32_t always_update_first;    /*    or J divides t, App. B.4                       */
   int32_t renorm;                 /* 1: rows leave each p-norm layer with unit rms     */
   float max_change_per_sample;    /* App. C.3; 0 disables the limit (paper: 0.075)     */
-  int32_t method;                 /* NGSGD_METHOD_ONLINE (App. B) or _SIMPLE (App. A)  */
+  int32_t method;                 /* NGSGD_METHOD_ONLINE (App. B), _SIMPLE (App. A), _ADAMW or _ADAMW8 */
   float simple_epsilon;           /* floor on tr(X^T X) in beta, App. A.2 (1e-20)      */
   int32_t side_streams;           /* internal streams for the factor updates: 0 = chosen
                                    * by the layers, the ranks and the classes (1 or 2), else
@@ -303,8 +310,8 @@ int ngsgd_step(ngsgd_net* net, const float* dev_x, const int32_t* dev_labels, in
 int ngsgd_join(ngsgd_net* net, void* hip_stream);
 
 /* Parameter averaging of Sec. 3.1: every replica's weights are replaced by the arithmetic mean over
- * the n replicas (same configuration, same device).  With reset_preconditioners != 0 all their
- * preconditioners are reset, as the paper's re-spawned processes do (App. B.3.2).
+ * the n replicas (same configuration, same device), and so are their layer norms'.  With reset_preconditioners != 0 all
+ * their preconditioners are reset, as the paper's re-spawned processes do (App. B.3.2), and AdamW's moments.
  * The replicas may have been stepped on other streams than hip_stream: the averaging kernel waits (on
  * the device) for each replica's latest ngsgd_step and factor updates, and each replica's next call
  * waits for the averaged weights, so the caller needs no synchronisation of its own.  (The call records an
@@ -316,6 +323,17 @@ int ngsgd_average(ngsgd_net* const* nets, int32_t n, int32_t reset_preconditione
 int ngsgd_get_params(const ngsgd_net* net, int32_t layer, float* dev_out, void* hip_stream);
 int ngsgd_set_params(ngsgd_net* net, int32_t layer, const float* dev_in, void* hip_stream);
 
+/* Weight (ones at first) and bias (zeros) of the layer norm behind hidden layer `layer`, as many as the next layer has
+ * inputs; either pointer may be NULL.  NGSGD_EINVAL where there is none. */
+int ngsgd_get_norm(const ngsgd_net* net, int32_t layer, float* dev_weight, float* dev_bias, void* hip_stream);
+int ngsgd_set_norm(ngsgd_net* net, int32_t layer, const float* dev_weight, const float* dev_bias, void* hip_stream);
+
+/* Numbers of the AdamW step over the layer norms' parameters and, with the AdamW methods, the weight matrices: its
+ * learning rate is `rate` times the step's, weight_decay is of the matrices (bias column included) only.  Defaults: rate 1,
+ * beta1 0.9, beta2 0.999, epsilon 1e-8 (not 0), weight_decay 0.  Forgets the moments and synchronises the device.
+ * NGSGD_EINVAL for a network without AdamW; so does ngsgd_step where rate * lr is above 1e18 or not a number. */
+int ngsgd_set_adamw(ngsgd_net* net, float rate, double beta1, double beta2, float epsilon, float weight_decay);
+
 /* Borrowed handle of a layer's preconditioner (side = NGSGD_SIDE_INPUT / NGSGD_SIDE_OUTPUT);
  * owned by the net, valid until ngsgd_destroy.  NULL result when that side's rank is 0. */
 int ngsgd_net_precond(ngsgd_net* net, int32_t layer, int32_t side, ngsgd_precond** out);
@@ -323,11 +341,13 @@ int ngsgd_net_precond(ngsgd_net* net, int32_t layer, int32_t side, ngsgd_precond
 /* Inspection of the latest step, for parity checks.  All outputs are dense row-major copies.
  *   ngsgd_last_preconditioned: the N x dim matrix Obar_l or Xbar_l (already rescaled by gamma)
  *   ngsgd_last_gradient:       a_l * Obar_l^T Xbar_l, dims[layer+1] x (in_dim+1), without lr
- *   ngsgd_last_max_change_scale: a_l of App. C.3 as one double (1 when the limit is disabled) */
+ *   ngsgd_last_max_change_scale: a_l of App. C.3 as one double (1 when the limit is disabled)
+ *   ngsgd_last_norm_gradient:  of the layer norm behind hidden layer `layer`, by its weight and its bias */
 int ngsgd_last_preconditioned(ngsgd_net* net, int32_t layer, int32_t side, float* dev_out,
                               void* hip_stream);
 int ngsgd_last_gradient(ngsgd_net* net, int32_t layer, float* dev_out, void* hip_stream);
 int ngsgd_last_max_change_scale(ngsgd_net* net, int32_t layer, double* dev_out, void* hip_stream);
+int ngsgd_last_norm_gradient(ngsgd_net* net, int32_t layer, float* dev_dweight, float* dev_dbias, void* hip_stream);
 
 /* ---- timing of kernel groups (for benchmarks) ------------------------------------------------
  * While enabled, every launch group of the categories below is bracketed by a pair of HIP events
@@ -342,14 +362,14 @@ int ngsgd_last_max_change_scale(ngsgd_net* net, int32_t layer, double* dev_out, 
  * So is B_t, and the check's W W^T, in that of W_{t+1}. */
 #define NGSGD_PROF_GEMM_FWD 0        /* A_l = [X_l, 1] W_l^T, tanh                               */
 #define NGSGD_PROF_GEMM_BWD 1        /* dX_l = O_l W_l, mostly with the derivative of tanh       */
-#define NGSGD_PROF_GEMM_UPD 2        /* W_l += lr a_l Obar_l^T Xbar_l, max-change (one launch)   */
+#define NGSGD_PROF_GEMM_UPD 2        /* W_l += lr a_l Obar_l^T Xbar_l, max-change (one launch); AdamW */
 #define NGSGD_PROF_PRECOND_H 3       /* H = X W^T and tr(X X^T)                                  */
 #define NGSGD_PROF_PRECOND_J 4       /* J = H^T X                                                */
 #define NGSGD_PROF_PRECOND_XHAT 5    /* Xhat = X - H W and row norms                             */
 #define NGSGD_PROF_PRECOND_KL 6      /* K = J J^T, L = H^T H                                     */
 #define NGSGD_PROF_PRECOND_SMALL 7   /* R x R update: Z_t, eigen-decomposition, A_t              */
 #define NGSGD_PROF_PRECOND_WNEW 8    /* B_t, W_{t+1} = A_t B_t                                   */
-#define NGSGD_PROF_ELEMENTWISE 9     /* nonlinearities behind no product, log-softmax            */
+#define NGSGD_PROF_ELEMENTWISE 9     /* nonlinearities behind no product, layer norms, log-softmax */
 #define NGSGD_PROF_PRECOND_MISC 10   /* clears, gamma, orthogonality check, rescale              */
 #define NGSGD_PROF_INIT 11           /* state initialisation from the first minibatch            */
 #define NGSGD_PROF_SIMPLE_GRAM 12    /* simple method: X^T X or X X^T                            */

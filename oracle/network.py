@@ -30,16 +30,22 @@ Two stabilisers of the paper's recipe are optional here:
   * `max_change_per_sample` (App. C.3): the update of each layer is scaled by
         a_t = min(1, N * max_change_per_sample / (lr * sum_i ||obar_i|| ||xbar_i||))
     using the rows of the preconditioned matrices (a_t = 1 if the sum is 0).
+
+A layer whose nonlinearity carries LAYERNORM passes its output through a layer norm with a weight and a bias, which AdamW
+updates at the step's learning rate; with method="adamw" it updates the weight matrices too, with their plain gradients.
 """
 from __future__ import annotations
 
 import numpy as np
 
+from . import adamw, layer_norm
 from .online_ng import OnlineNaturalGradient
 from .simple_ng import simple_ng
 
 TANH = 0
 PNORM = 1
+LAYERNORM = 16           # added to either: a layer norm follows
+NORM_EPSILON = 1.0e-5
 RENORM_FLOOR = 1.0e-20
 
 
@@ -94,13 +100,14 @@ class NGSGDNetwork:
                  epsilon: float = 1.0e-10, update_period: int = 4, natural_gradient: bool = True,
                  renorm: bool = False, max_change_per_sample: float = 0.0, method: str = "online",
                  simple_epsilon: float = 1.0e-20):
-        assert method in ("online", "simple")
+        assert method in ("online", "simple", "adamw")
         self.method = method                 # which estimate of the Fisher factors (Sec. 4.5)
         self.simple_alpha = alpha
         self.simple_epsilon = simple_epsilon
         self.dims = list(dims)
         self.n_layers = len(dims) - 1
-        self.nonlin = list(nonlin)
+        self.norm = [bool(f & LAYERNORM) for f in nonlin] + [False]
+        self.nonlin = [f & ~LAYERNORM for f in nonlin]
         assert len(self.nonlin) == self.n_layers - 1
         self.pnorm_group = pnorm_group
         self.natural_gradient = natural_gradient
@@ -122,12 +129,28 @@ class NGSGDNetwork:
         self.precond_out = [OnlineNaturalGradient(dims[l + 1], rank_out, **kw)
                             for l in range(self.n_layers)]
         self.last = {}
+        self.gain = [np.ones(d) for d in self.in_dims[1:]]
+        self.shift = [np.zeros(d) for d in self.in_dims[1:]]
+        self.adamw = dict(beta1=0.9, beta2=0.999, epsilon=1e-8, decay=0.0, rate=1.0)
+        self.reset_adamw()
+
+    def reset_adamw(self):
+        """Forgets AdamW's moments."""
+        self._moments, self._t = {}, 0
+
+    def _adamw(self, key, p, ascent, lr, decay):
+        m, v = self._moments.get(key, (np.zeros_like(p), np.zeros_like(p)))
+        a = self.adamw
+        p, m, v = adamw.step(p, -ascent, m, v, self._t, lr * a["rate"], a["beta1"], a["beta2"], a["epsilon"], decay)
+        self._moments[key] = (m, v)
+        return p
 
     # -- pieces, exposed for the tests ---------------------------------------------
     def forward(self, x: np.ndarray):
         """Returns (layer inputs with ones column, affine outputs, log-probabilities)."""
         Xin, A = [], []
         self._sigma = [None] * self.n_layers
+        self._plain, self._stats = [None] * self.n_layers, [None] * self.n_layers   # outputs before a layer norm, its mean and rstd
         cur = np.asarray(x, dtype=np.float64)
         for l in range(self.n_layers):
             Xl = append_ones(cur)
@@ -141,6 +164,9 @@ class NGSGDNetwork:
                     cur = pnorm_forward(Al, self.pnorm_group)
                     if self.renorm:
                         cur, self._sigma[l] = renorm_forward(cur)
+                if self.norm[l]:
+                    self._plain[l] = cur
+                    cur, *self._stats[l] = layer_norm.forward(cur, self.gain[l], self.shift[l], NORM_EPSILON)
         return Xin, A, log_softmax(A[-1])
 
     def objective(self, x: np.ndarray, labels: np.ndarray) -> float:
@@ -154,10 +180,14 @@ class NGSGDNetwork:
         Olast = -np.exp(logp)
         Olast[np.arange(N), labels] += 1.0
         O[-1] = Olast
+        self.norm_gradients = {}
         for l in range(self.n_layers - 1, 0, -1):
             dX = O[l] @ self.W[l][:, :-1]                      # drop the bias column
             Aprev = A[l - 1]
             Yprev = Xin[l][:, :-1]
+            if self.norm[l - 1]:
+                Yprev = self._plain[l - 1]
+                dX, *self.norm_gradients[l - 1] = layer_norm.backward(dX, Yprev, *self._stats[l - 1], self.gain[l - 1])
             if self.nonlin[l - 1] == TANH:
                 O[l - 1] = dX * (1.0 - Yprev * Yprev)
             else:
@@ -183,7 +213,10 @@ class NGSGDNetwork:
         O = self.backward(Xin, A, logp, labels)
         deltas, Obar_all, Xbar_all, scales = [], [], [], []
         for l in range(self.n_layers):
-            if self.natural_gradient and self.method == "simple":
+            if self.method == "adamw":
+                Obar, Xbar = O[l], Xin[l]
+                rn_o, rn_x = np.sum(Obar * Obar, axis=1), np.sum(Xbar * Xbar, axis=1)
+            elif self.natural_gradient and self.method == "simple":
                 Obar, _, rn_o = simple_ng(O[l], self.simple_alpha, self.simple_epsilon)
                 Xbar, _, rn_x = simple_ng(Xin[l], self.simple_alpha, self.simple_epsilon)
             elif self.natural_gradient:
@@ -202,8 +235,15 @@ class NGSGDNetwork:
             deltas.append(delta)
             Obar_all.append(Obar)
             Xbar_all.append(Xbar)
+        self._t += 1
         for l in range(self.n_layers):
-            self.W[l] = self.W[l] + lr * deltas[l]
+            if self.method == "adamw":
+                self.W[l] = self._adamw(("W", l), self.W[l], deltas[l], lr, self.adamw["decay"])
+            else:
+                self.W[l] = self.W[l] + lr * deltas[l]
+        for l, (dgain, dshift) in self.norm_gradients.items():
+            self.gain[l] = self._adamw(("gain", l), self.gain[l], dgain, lr, 0.0)
+            self.shift[l] = self._adamw(("shift", l), self.shift[l], dshift, lr, 0.0)
         self.last = dict(O=O, Xin=Xin, Obar=Obar_all, Xbar=Xbar_all, delta=deltas, logp=logp,
                          max_change_scale=scales)
         return obj

@@ -23,6 +23,7 @@ NGSGD_ENOMEM = -2
 NGSGD_EHIP = -3
 NGSGD_TANH = 0
 NGSGD_PNORM = 1
+NGSGD_LAYERNORM = 16
 NGSGD_FLOAT32 = 0
 NGSGD_BFLOAT16 = 1
 NGSGD_FLOAT16 = 2
@@ -32,6 +33,8 @@ NGSGD_MAX_RANK = 96
 NGSGD_MAX_LAYERS = 16
 NGSGD_METHOD_ONLINE = 0
 NGSGD_METHOD_SIMPLE = 1
+NGSGD_METHOD_ADAMW = 2
+NGSGD_METHOD_ADAMW8 = 3
 
 
 class NgsgdError(RuntimeError):
@@ -98,6 +101,10 @@ _SIGNATURES = {
     "ngsgd_average": (c_int, [POINTER(c_void_p), c_int32, c_int32, c_void_p]),
     "ngsgd_get_params": (c_int, [c_void_p, c_int32, c_void_p, c_void_p]),
     "ngsgd_set_params": (c_int, [c_void_p, c_int32, c_void_p, c_void_p]),
+    "ngsgd_get_norm": (c_int, [c_void_p, c_int32, c_void_p, c_void_p, c_void_p]),
+    "ngsgd_set_norm": (c_int, [c_void_p, c_int32, c_void_p, c_void_p, c_void_p]),
+    "ngsgd_set_adamw": (c_int, [c_void_p, c_float, c_double, c_double, c_float, c_float]),
+    "ngsgd_last_norm_gradient": (c_int, [c_void_p, c_int32, c_void_p, c_void_p, c_void_p]),
     "ngsgd_net_precond": (c_int, [c_void_p, c_int32, c_int32, POINTER(c_void_p)]),
     "ngsgd_last_preconditioned": (c_int, [c_void_p, c_int32, c_int32, c_void_p, c_void_p]),
     "ngsgd_last_gradient": (c_int, [c_void_p, c_int32, c_void_p, c_void_p]),
@@ -542,7 +549,9 @@ class Network:
                  renorm=False, max_change_per_sample=0.0, method="online", simple_epsilon=1e-20, side_streams=0):
         import torch
         self.lib = load_library()
-        self.method = {"online": NGSGD_METHOD_ONLINE, "simple": NGSGD_METHOD_SIMPLE}[method]
+        self.handle = None
+        self.method = {"online": NGSGD_METHOD_ONLINE, "simple": NGSGD_METHOD_SIMPLE, "adamw": NGSGD_METHOD_ADAMW,
+                       "adamw8": NGSGD_METHOD_ADAMW8}[method]
         self.dims = list(dims)
         self.nonlin = list(nonlin)
         self.n_layers = len(dims) - 1
@@ -554,7 +563,7 @@ class Network:
         for l in range(self.n_layers):
             self.in_dims.append(d_in)
             if l < self.n_layers - 1:
-                d_in = dims[l + 1] // pnorm_group if nonlin[l] == NGSGD_PNORM else dims[l + 1]
+                d_in = dims[l + 1] // pnorm_group if nonlin[l] & ~NGSGD_LAYERNORM == NGSGD_PNORM else dims[l + 1]
         self._dims_arr = (c_int32 * len(dims))(*dims)
         self._nonlin_arr = (c_int32 * max(1, len(nonlin)))(*nonlin)
         cfg = ngsgd_config(self.n_layers, self._dims_arr, self._nonlin_arr, pnorm_group, max_batch, rank_in,
@@ -590,6 +599,42 @@ class Network:
         w = torch.empty((self.dims[layer + 1], self.in_dims[layer] + 1), dtype=torch.float32, device="cuda")
         _check(self.lib.ngsgd_get_params(self.handle, layer, _ptr(w), _stream_ptr()), "ngsgd_get_params")
         return w
+
+    def _norm_vectors(self, layer, *vectors):
+        import torch
+        dim = self.in_dims[layer + 1] if 0 <= layer < self.n_layers - 1 else 0
+        for v in vectors:
+            if v is not None:
+                _check_dense(v, "layer-norm vector", self.workspace.device, torch.float32, dim)
+        return dim
+
+    def set_norm(self, layer, weight=None, bias=None, stream=None):
+        """Weight and bias of the layer norm behind hidden layer `layer` (None: left as it is)."""
+        self._norm_vectors(layer, weight, bias)
+        _check(self.lib.ngsgd_set_norm(self.handle, layer, _ptr(weight), _ptr(bias), _stream_ptr(stream)), "ngsgd_set_norm")
+
+    def get_norm(self, layer, stream=None):
+        """(weight, bias) of the layer norm behind hidden layer `layer`."""
+        import torch
+        dim = self._norm_vectors(layer)
+        with _allocate_on(stream):
+            w, b = (torch.empty(dim, dtype=torch.float32, device=self.workspace.device) for _ in range(2))
+        _check(self.lib.ngsgd_get_norm(self.handle, layer, _ptr(w), _ptr(b), _stream_ptr(stream)), "ngsgd_get_norm")
+        return w, b
+
+    def set_adamw(self, rate=1.0, betas=(0.9, 0.999), epsilon=1e-8, weight_decay=0.0):
+        """Numbers of the AdamW step (layer norms; with the AdamW methods the weight matrices too); forgets its moments."""
+        _check(self.lib.ngsgd_set_adamw(self.handle, rate, betas[0], betas[1], epsilon, weight_decay), "ngsgd_set_adamw")
+
+    def last_norm_gradient(self, layer, stream=None):
+        """Gradients of the latest step by the weight and the bias of the layer norm behind hidden layer `layer`."""
+        import torch
+        dim = self._norm_vectors(layer)
+        with _allocate_on(stream):
+            w, b = (torch.empty(dim, dtype=torch.float32, device=self.workspace.device) for _ in range(2))
+        _check(self.lib.ngsgd_last_norm_gradient(self.handle, layer, _ptr(w), _ptr(b), _stream_ptr(stream)),
+               "ngsgd_last_norm_gradient")
+        return w, b
 
     def step(self, x, labels, lr, logprob_out=None, stream=None):
         """Enqueues one minibatch step; the sum of log-probabilities lands in `logprob_out` (1 float64)."""

@@ -5,6 +5,7 @@
 #include <cmath>
 
 #include "host.h"
+#include "operators.h"
 
 using namespace ngsgd;
 
@@ -123,6 +124,19 @@ bool good_matrix(const void* p, const int64_t ld, const int type, const int64_t 
 
 }  // namespace
 
+namespace ngsgd {
+
+int layernorm_forward_f32(const LayerNormForward& a, hipStream_t s) { return launch_forward<float, float>(a, s); }
+
+int layernorm_backward_f32(LayerNormBackward a, hipStream_t s) {
+  a.groups = norm_groups(a.N, a.D);
+  return a.n_slabs > 1 ? launch_backward<float, float, true>(a, s) : launch_backward<float, float, false>(a, s);
+}
+
+size_t layernorm_part_floats(const int64_t max_rows, const int D) { return (size_t)norm_groups(max_rows, D) * 2 * D; }
+
+}  // namespace ngsgd
+
 extern "C" int ngsgd_layernorm_forward(const void* dev_x, int64_t ldx, int32_t type, const void* dev_weight, const void* dev_bias,
                                        int32_t weight_type, int64_t N, int32_t D, float epsilon, void* dev_y, int64_t ldy, float* dev_mean,
                                        float* dev_rstd, void* hip_stream) {
@@ -139,7 +153,7 @@ extern "C" int ngsgd_layernorm_forward(const void* dev_x, int64_t ldx, int32_t t
 extern "C" int ngsgd_layernorm_workspace_bytes(int64_t max_rows, int32_t D, size_t* out_bytes) {
   if (out_bytes == nullptr || max_rows < 0 || D < 1 || D > kMostColumns) return NGSGD_EINVAL;
   Carver c(nullptr);
-  (void)c.take<float>((size_t)norm_groups(max_rows, D) * 2 * D);
+  (void)c.take<float>(layernorm_part_floats(max_rows, D));
   *out_bytes = align_up(c.off, 256);
   return NGSGD_OK;
 }

@@ -17,6 +17,7 @@
 #include "host.h"
 #include "init.h"
 #include "kernels.h"
+#include "operators.h"
 #include "simple_ng.h"
 #include "small_update.h"
 #include "split_gemm.h"
@@ -1520,6 +1521,13 @@ struct ngsgd_layer {
   float* A = nullptr;               // max_batch x lda, affine output, later O_l
   float* sigma = nullptr;           // max_batch renorm divisors
   double* mc_scale = nullptr;       // max-change scale of the latest step
+  // layer norm behind the nonlinearity (NGSGD_LAYERNORM)
+  bool norm = false;
+  float* Y = nullptr;               // max_batch x ldy, the nonlinearity's output, whose norm is the next layer's input
+  int ldy = 0;
+  float *gain = nullptr, *shift = nullptr;               // weight and bias, `groups` each
+  float *gain_gradient = nullptr, *shift_gradient = nullptr;
+  float *mean = nullptr, *rstd = nullptr;                // max_batch
   ngsgd_precond pin, pout;
   SimpleWork sin, sout;             // scratch of the simple method (only laid out when it is selected)
 };
@@ -1533,8 +1541,15 @@ struct ngsgd_net {
   int method = NGSGD_METHOD_ONLINE;
   double alpha = 4.0, simple_epsilon = 1e-20;
   std::vector<ngsgd_layer> layers;
-  float* params = nullptr;
-  size_t n_params_padded = 0;
+  float* params = nullptr;          // all weight matrices, then all layer norms' weights and biases
+  size_t n_weights_padded = 0, n_params_padded = 0;
+  // AdamW: of the layer norms' parameters, and with its method of the weight matrices
+  float* gradients = nullptr;       // laid out as params (without the matrices where the method does not need them)
+  float* norm_part = nullptr;       // sums over groups of rows
+  void* adamw_workspace = nullptr;
+  size_t adamw_bytes = 0;
+  ngsgd_adamw* adamw = nullptr;
+  float adamw_rate = 1.f, adamw_decay = 0.f;
   float* dX = nullptr;
   int lddx = 0;
   double* rowobj = nullptr;
@@ -1562,6 +1577,38 @@ int output_side_group(int l, int n_layers, int n_side) {
   return std::min(n_side - 1, 1 + (n_layers - 2 - l) / 2);
 }
 
+bool by_adamw(const int method) { return method == NGSGD_METHOD_ADAMW || method == NGSGD_METHOD_ADAMW8; }
+
+constexpr float kNormEpsilon = 1e-5f;   // layer norms
+
+// AdamW over the layer norms' parameters (the last tensor, without decay) and, with its method, over the weight matrices (the first one).
+struct NetAdamW {
+  void* params[2];
+  int64_t sizes[2];
+  float decay[2];
+  ngsgd_adamw_config cfg;
+  NetAdamW(const ngsgd_net& net, const double beta1, const double beta2, const float epsilon, const float weight_decay);
+  NetAdamW(const NetAdamW&) = delete;
+};
+NetAdamW::NetAdamW(const ngsgd_net& net, const double beta1, const double beta2, const float epsilon, const float weight_decay) {
+  // (sizing has no addresses yet: any that do not overlap do)
+  float* const base = net.params != nullptr ? net.params : reinterpret_cast<float*>((uintptr_t)256);
+  const int64_t n_norm = (int64_t)(net.n_params_padded - net.n_weights_padded);
+  int n = 0;
+  if (by_adamw(net.method)) {
+    params[n] = base;
+    sizes[n] = (int64_t)net.n_weights_padded;
+    decay[n++] = weight_decay;
+  }
+  if (n_norm > 0) {
+    params[n] = base + net.n_weights_padded;
+    sizes[n] = n_norm;
+    decay[n++] = 0.f;
+  }
+  cfg = ngsgd_adamw_config{n, params, sizes, decay, nullptr, NGSGD_FLOAT32, NGSGD_FLOAT32, net.method == NGSGD_METHOD_ADAMW8 ? 8 : 32, 0,
+                           beta1, beta2, epsilon};
+}
+
 int net_check_config(const ngsgd_config* cfg) {
   if (cfg == nullptr || cfg->dims == nullptr || cfg->n_layers < 1 || cfg->n_layers > NGSGD_MAX_LAYERS)
     return NGSGD_EINVAL;
@@ -1569,24 +1616,26 @@ int net_check_config(const ngsgd_config* cfg) {
   if (cfg->max_batch < 1 || cfg->pnorm_group < 1) return NGSGD_EINVAL;
   if (cfg->dims[0] < 1 || (cfg->dims[0] & 3)) return NGSGD_EINVAL;
   if (!(cfg->max_change_per_sample >= 0.f)) return NGSGD_EINVAL;
-  if (cfg->method != NGSGD_METHOD_ONLINE && cfg->method != NGSGD_METHOD_SIMPLE) return NGSGD_EINVAL;
-  const bool simple = cfg->method == NGSGD_METHOD_SIMPLE;
+  if (cfg->method != NGSGD_METHOD_ONLINE && cfg->method != NGSGD_METHOD_SIMPLE && !by_adamw(cfg->method)) return NGSGD_EINVAL;
+  if (by_adamw(cfg->method) && cfg->max_change_per_sample != 0.f) return NGSGD_EINVAL;   // a limit on the natural gradient's steps
+  const bool simple = cfg->method == NGSGD_METHOD_SIMPLE, factors = cfg->method == NGSGD_METHOD_ONLINE;
   if (cfg->side_streams < 0 || cfg->side_streams > kSideStreams) return NGSGD_EINVAL;
   if (simple && (cfg->max_batch < 2 || !(cfg->alpha > 0.f) || !(cfg->simple_epsilon > 0.f))) return NGSGD_EINVAL;
   int din = cfg->dims[0];
   for (int l = 0; l < cfg->n_layers; ++l) {
     const int dout = cfg->dims[l + 1];
     if (dout < 1) return NGSGD_EINVAL;
-    // the simple method keeps no factors: the ranks are not used
-    NG_TRY(precond_check_config(din + 1, simple ? 0 : cfg->rank_in, cfg->max_batch, cfg->alpha,
+    // only the online method keeps factors: the ranks are not used
+    NG_TRY(precond_check_config(din + 1, factors ? cfg->rank_in : 0, cfg->max_batch, cfg->alpha,
                                 cfg->num_samples_history, cfg->epsilon, cfg->update_period, cfg->always_update_first));
-    NG_TRY(precond_check_config(dout, simple ? 0 : cfg->rank_out, cfg->max_batch, cfg->alpha,
+    NG_TRY(precond_check_config(dout, factors ? cfg->rank_out : 0, cfg->max_batch, cfg->alpha,
                                 cfg->num_samples_history, cfg->epsilon, cfg->update_period, cfg->always_update_first));
     if (l < cfg->n_layers - 1) {
-      if (cfg->nonlin[l] == NGSGD_PNORM) {
+      const int nonlin = cfg->nonlin[l] & ~NGSGD_LAYERNORM;
+      if (nonlin == NGSGD_PNORM) {
         if (dout % cfg->pnorm_group || dout / cfg->pnorm_group > kPnormMaxGroupsLds) return NGSGD_EINVAL;
         din = dout / cfg->pnorm_group;
-      } else if (cfg->nonlin[l] == NGSGD_TANH) {
+      } else if (nonlin == NGSGD_TANH) {
         din = dout;
       } else {
         return NGSGD_EINVAL;
@@ -1605,10 +1654,10 @@ void net_layout(ngsgd_net& net, const ngsgd_config* cfg, Carver& c) {
   net.method = cfg->method;
   net.alpha = cfg->alpha;
   net.simple_epsilon = cfg->simple_epsilon;
-  const bool simple = cfg->method == NGSGD_METHOD_SIMPLE;
+  const bool simple = cfg->method == NGSGD_METHOD_SIMPLE, factors = cfg->method == NGSGD_METHOD_ONLINE;
   net.layers.assign(cfg->n_layers, ngsgd_layer());
   int din = cfg->dims[0];
-  size_t n_params = 0;
+  size_t n_params = 0, n_norm = 0, norm_part = 0;
   int max_ldx = 0;
   for (int l = 0; l < cfg->n_layers; ++l) {
     ngsgd_layer& L = net.layers[l];
@@ -1618,19 +1667,46 @@ void net_layout(ngsgd_net& net, const ngsgd_config* cfg, Carver& c) {
     L.ldw = pad32(L.in1);
     L.ldx = pad32(L.in1);
     L.lda = pad32(L.dout);
-    L.nonlin = l < cfg->n_layers - 1 ? cfg->nonlin[l] : -1;
+    L.nonlin = l < cfg->n_layers - 1 ? cfg->nonlin[l] & ~NGSGD_LAYERNORM : -1;
+    L.norm = l < cfg->n_layers - 1 && (cfg->nonlin[l] & NGSGD_LAYERNORM) != 0;
     L.groups = L.nonlin == NGSGD_PNORM ? L.dout / cfg->pnorm_group : L.dout;
     n_params += (size_t)L.dout * L.ldw;
+    if (L.norm) {
+      n_norm += 2 * (size_t)pad32(L.groups);
+      norm_part = std::max(norm_part, layernorm_part_floats(cfg->max_batch, L.groups));
+    }
     max_ldx = std::max(max_ldx, L.ldx);
     din = L.groups;
   }
-  net.n_params_padded = n_params;
+  net.n_weights_padded = n_params;
+  net.n_params_padded = n_params + n_norm;
   net.n_side = cfg->side_streams > 0 ? cfg->side_streams : default_side_streams(*cfg);
-  net.params = c.take<float>(n_params);
+  net.params = c.take<float>(net.n_params_padded);
   size_t off = 0;
   for (auto& L : net.layers) {
     L.W = net.params ? net.params + off : nullptr;
     off += (size_t)L.dout * L.ldw;
+  }
+  if (by_adamw(cfg->method) || n_norm > 0) {
+    const size_t skipped = by_adamw(cfg->method) ? 0 : n_params;   // gradients of weight matrices that nobody asks for
+    float* const g = c.take<float>(net.n_params_padded - skipped);
+    net.gradients = g != nullptr ? g - skipped : nullptr;
+    for (auto& L : net.layers) {
+      if (!L.norm) continue;
+      const size_t at[2] = {off, off + pad32(L.groups)};
+      off += 2 * (size_t)pad32(L.groups);
+      if (net.params != nullptr) {
+        L.gain = net.params + at[0];
+        L.shift = net.params + at[1];
+        L.gain_gradient = net.gradients + at[0];
+        L.shift_gradient = net.gradients + at[1];
+      }
+    }
+    net.norm_part = c.take<float>(norm_part);
+    const NetAdamW rule(net, 0.9, 0.999, 1e-8f, 0.f);
+    net.adamw_bytes = 0;
+    (void)ngsgd_adamw_workspace_bytes(&rule.cfg, &net.adamw_bytes);
+    net.adamw_workspace = c.take<char>(net.adamw_bytes);
   }
   net.lddx = max_ldx;
   net.dX = c.take<float>((size_t)kMaxBwdSplits * net.max_batch * net.lddx);
@@ -1641,9 +1717,15 @@ void net_layout(ngsgd_net& net, const ngsgd_config* cfg, Carver& c) {
     L.A = c.take<float>((size_t)net.max_batch * L.lda);
     L.sigma = c.take<float>(net.max_batch);
     L.mc_scale = c.take<double>(1);
-    precond_configure(L.pin, L.in1, simple ? 0 : cfg->rank_in, cfg->max_batch, cfg->alpha, cfg->num_samples_history,
+    if (L.norm) {
+      L.ldy = pad32(L.groups + 1);   // (the p-norm kernel appends its one)
+      L.Y = c.take<float>((size_t)net.max_batch * L.ldy);
+      L.mean = c.take<float>(net.max_batch);
+      L.rstd = c.take<float>(net.max_batch);
+    }
+    precond_configure(L.pin, L.in1, factors ? cfg->rank_in : 0, cfg->max_batch, cfg->alpha, cfg->num_samples_history,
                       cfg->epsilon, cfg->update_period, cfg->always_update_first);
-    precond_configure(L.pout, L.dout, simple ? 0 : cfg->rank_out, cfg->max_batch, cfg->alpha,
+    precond_configure(L.pout, L.dout, factors ? cfg->rank_out : 0, cfg->max_batch, cfg->alpha,
                       cfg->num_samples_history, cfg->epsilon, cfg->update_period, cfg->always_update_first);
     L.pin.owned_by_net = L.pout.owned_by_net = true;
     L.pin.sync = &net.side[0];
@@ -1720,6 +1802,18 @@ extern "C" int ngsgd_create(const ngsgd_config* cfg, void* dev_workspace, size_t
     if (e == hipSuccess) e = hipMemcpy(L.pout.st, &init, sizeof(init), hipMemcpyHostToDevice);
     if (e == hipSuccess) e = hipMemcpy(L.mc_scale, &one, sizeof(one), hipMemcpyHostToDevice);
   }
+  for (auto& L : net->layers)
+    if (e == hipSuccess && L.norm) {
+      hipLaunchKernelGGL(fill_u32_kernel, dim3(64), dim3(256), 0, nullptr, reinterpret_cast<uint32_t*>(L.gain), (size_t)L.groups, 0x3f800000u);
+      e = hipGetLastError();
+    }
+  if (e == hipSuccess && net->adamw_bytes > 0) {
+    const NetAdamW rule(*net, 0.9, 0.999, 1e-8f, 0.f);
+    if (ngsgd_adamw_create(&rule.cfg, net->adamw_workspace, net->adamw_bytes, &net->adamw) != NGSGD_OK) {
+      ngsgd_destroy(net);
+      return NGSGD_EHIP;
+    }
+  }
   // second stream for the factor updates: default priority, does not synchronise with the NULL stream
   if (e == hipSuccess) e = hipEventCreateWithFlags(&net->step_done, hipEventDisableTiming);
   if (e == hipSuccess) e = hipEventCreateWithFlags(&net->avg_done, hipEventDisableTiming);
@@ -1753,6 +1847,7 @@ extern "C" int ngsgd_destroy(ngsgd_net* net) {
   }
   for (hipEvent_t ev : {net->step_done, net->avg_done})
     if (ev != nullptr) (void)hipEventDestroy(ev);
+  if (net->adamw != nullptr) (void)ngsgd_adamw_destroy(net->adamw);
   delete net;
   return NGSGD_OK;
 }
@@ -1762,6 +1857,9 @@ extern "C" int ngsgd_step(ngsgd_net* net, const float* dev_x, const int32_t* dev
   if (net == nullptr || dev_x == nullptr || dev_labels == nullptr) return NGSGD_EINVAL;
   if (N < 1 || N > net->max_batch || !aligned16(dev_x)) return NGSGD_EINVAL;
   if (net->method == NGSGD_METHOD_SIMPLE && N < 2) return NGSGD_EINVAL;   // nothing to hold out
+  const float adamw_lr = lr * net->adamw_rate;
+  // AdamW runs over the padding too, whose zeros have to stay zeros: no product with them may be one of zero and infinity
+  if (net->adamw != nullptr && !(std::fabs(adamw_lr) <= 1e18f && std::fabs(adamw_lr * net->adamw_decay) <= 1e30f)) return NGSGD_EINVAL;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   const int nl = net->n_layers;
   auto& Ls = net->layers;
@@ -1790,9 +1888,10 @@ extern "C" int ngsgd_step(ngsgd_net* net, const float* dev_x, const int32_t* dev
     g.M = N; g.N = L.dout; g.K = L.in1;
     if (L.nonlin == NGSGD_TANH) {   // the next layer's input straight from the product
       ngsgd_layer& Nx = Ls[l + 1];
-      g.C = Nx.Xin; g.ldc = Nx.ldx;
+      g.C = L.norm ? L.Y : Nx.Xin;
+      g.ldc = L.norm ? L.ldy : Nx.ldx;
       g.act = kActTanh;
-      g.pad_to = Nx.ldx;
+      g.pad_to = L.norm ? L.dout : Nx.ldx;
     }
     {
       ProfScope prof(NGSGD_PROF_GEMM_FWD, s);
@@ -1804,14 +1903,29 @@ extern "C" int ngsgd_step(ngsgd_net* net, const float* dev_x, const int32_t* dev
     } else {
       ProfScope prof(NGSGD_PROF_ELEMENTWISE, s);
       ngsgd_layer& Nx = Ls[l + 1];
+      float* const Y = L.norm ? L.Y : Nx.Xin;
+      const int ldy = L.norm ? L.ldy : Nx.ldx;
       if (L.dout >= kWideRow) {
-        hipLaunchKernelGGL(pnorm_forward_kernel<512>, dim3(N), dim3(512), 0, s, L.A, L.lda, Nx.Xin, Nx.ldx,
+        hipLaunchKernelGGL(pnorm_forward_kernel<512>, dim3(N), dim3(512), 0, s, L.A, L.lda, Y, ldy,
                            L.sigma, N, L.groups, net->pnorm_group, net->renorm);
       } else {
-        hipLaunchKernelGGL(pnorm_forward_kernel<256>, dim3(N), dim3(256), 0, s, L.A, L.lda, Nx.Xin, Nx.ldx,
+        hipLaunchKernelGGL(pnorm_forward_kernel<256>, dim3(N), dim3(256), 0, s, L.A, L.lda, Y, ldy,
                            L.sigma, N, L.groups, net->pnorm_group, net->renorm);
       }
       LAUNCH_CHECK();
+    }
+    if (L.norm) {
+      ProfScope prof(NGSGD_PROF_ELEMENTWISE, s);
+      ngsgd_layer& Nx = Ls[l + 1];
+      LayerNormForward a{};
+      a.x = L.Y; a.ldx = L.ldy;
+      a.w = L.gain; a.b = L.shift;
+      a.y = Nx.Xin; a.ldy = Nx.ldx;
+      a.mean = L.mean; a.rstd = L.rstd;
+      a.N = N; a.D = L.groups;
+      a.eps = kNormEpsilon;
+      a.pad_to = Nx.ldx;   // the bias input and the padding
+      NG_TRY(layernorm_forward_f32(a, s));
     }
   }
   ngsgd_layer& last = Ls[nl - 1];
@@ -1876,7 +1990,7 @@ extern "C" int ngsgd_step(ngsgd_net* net, const float* dev_x, const int32_t* dev
     g.c_split_stride = (long long)slab;
     const int tiles = ((N + 63) / 64) * ((L.din + 63) / 64);
     g.splits = std::min(kMaxBwdSplits, choose_splits(tiles, (L.dout + 31) / 32));
-    const bool whole = P.nonlin == NGSGD_TANH && backward_in_one(g);
+    const bool whole = P.nonlin == NGSGD_TANH && !P.norm && backward_in_one(g);
     if (whole) {   // the derivative straight from the product
       g.splits = 1;
       g.C = P.A; g.ldc = P.lda;
@@ -1888,19 +2002,36 @@ extern "C" int ngsgd_step(ngsgd_net* net, const float* dev_x, const int32_t* dev
       ProfScope prof(NGSGD_PROF_GEMM_BWD, s);
       NG_TRY(launch_layer_gemms(GEMM_BWD, &g, 1, s, &n_slabs));
     }
+    if (P.norm) {   // the derivative of the nonlinearity's output takes the place of the first slab
+      ProfScope prof(NGSGD_PROF_ELEMENTWISE, s);
+      LayerNormBackward a{};
+      a.dy = net->dX; a.lddy = net->lddx;
+      a.n_slabs = n_slabs; a.slab_stride = (int64_t)slab;
+      a.x = P.Y; a.ldx = P.ldy;
+      a.w = P.gain;
+      a.mean = P.mean; a.rstd = P.rstd;
+      a.dx = net->dX; a.lddx = net->lddx;
+      a.dw = P.gain_gradient; a.db = P.shift_gradient;
+      a.N = N; a.D = P.groups;
+      a.part = net->norm_part;
+      NG_TRY(layernorm_backward_f32(a, s));
+      n_slabs = 1;
+    }
     if (whole) {
       prof_place();
     } else {
       ProfScope prof(NGSGD_PROF_ELEMENTWISE, s);
+      const float* const Y = P.norm ? P.Y : L.Xin;
+      const int ldy = P.norm ? P.ldy : L.ldx;
       if (P.nonlin == NGSGD_TANH) {
         hipLaunchKernelGGL(tanh_backward_kernel, dim3((P.dout + 1023) / 1024, N), dim3(256), 0, s, net->dX, net->lddx,
-                           n_slabs, slab, L.Xin, L.ldx, P.A, P.lda, N, P.dout);
+                           n_slabs, slab, Y, ldy, P.A, P.lda, N, P.dout);
       } else if (P.dout >= kWideRow) {
         hipLaunchKernelGGL(pnorm_backward_kernel<512>, dim3(N), dim3(512), 0, s, net->dX, net->lddx, n_slabs, slab,
-                           L.Xin, L.ldx, P.sigma, P.A, P.lda, N, P.groups, net->pnorm_group, net->renorm);
+                           Y, ldy, P.sigma, P.A, P.lda, N, P.groups, net->pnorm_group, net->renorm);
       } else {
         hipLaunchKernelGGL(pnorm_backward_kernel<256>, dim3(N), dim3(256), 0, s, net->dX, net->lddx, n_slabs, slab,
-                           L.Xin, L.ldx, P.sigma, P.A, P.lda, N, P.groups, net->pnorm_group, net->renorm);
+                           Y, ldy, P.sigma, P.A, P.lda, N, P.groups, net->pnorm_group, net->renorm);
       }
       LAUNCH_CHECK();
     }
@@ -1935,7 +2066,12 @@ extern "C" int ngsgd_step(ngsgd_net* net, const float* dev_x, const int32_t* dev
 
   // natural gradient: both matrices of every layer (Sec. 4.6; 2I instances), grouped calls; the factor updates
   // overlap the rest of this step and the next step's forward and backward passes on the side streams
-  if (net->method == NGSGD_METHOD_SIMPLE) {
+  if (by_adamw(net->method)) {   // the plain gradient of every weight matrix; AdamW below
+    std::vector<GemmDesc> grad;
+    for (auto& L : Ls) grad.push_back(update_desc(L, N, 1.f, 0.f, net->gradients + (L.W - net->params), L.ldw));
+    ProfScope prof(NGSGD_PROF_GEMM_UPD, s);
+    NG_TRY(launch_layer_gemms(GEMM_UPD, grad.data(), (int)grad.size(), s));
+  } else if (net->method == NGSGD_METHOD_SIMPLE) {
     // App. A instead: the factors come from the other rows of this minibatch, no state
     std::vector<SimpleCall> calls;
     for (auto& L : Ls) {
@@ -2000,6 +2136,14 @@ extern "C" int ngsgd_step(ngsgd_net* net, const float* dev_x, const int32_t* dev
       NG_TRY(update_layers(layers[1]));
     }
   }
+  if (net->adamw != nullptr) {   // upwards
+    ProfScope prof(NGSGD_PROF_GEMM_UPD, s);
+    const void* grads[2];
+    int n = 0;
+    if (by_adamw(net->method)) grads[n++] = net->gradients;
+    if (net->n_params_padded > net->n_weights_padded) grads[n++] = net->gradients + net->n_weights_padded;
+    NG_TRY(ngsgd_adamw_step(net->adamw, grads, adamw_lr, nullptr, -1.f, nullptr, s));
+  }
   net->last_N = N;
   net->last_lr = lr;
   net->step_stream = s;   // an averaging call on another stream orders itself behind this stream's work so far
@@ -2021,7 +2165,8 @@ extern "C" int ngsgd_average(ngsgd_net* const* nets, int32_t n, int32_t reset_pr
     if (nets[i]->n_params_padded != nets[0]->n_params_padded || nets[i]->n_layers != nets[0]->n_layers)
       return NGSGD_EINVAL;
     for (int l = 0; l < nets[0]->n_layers; ++l)
-      if (nets[i]->layers[l].dout != nets[0]->layers[l].dout || nets[i]->layers[l].din != nets[0]->layers[l].din)
+      if (nets[i]->layers[l].dout != nets[0]->layers[l].dout || nets[i]->layers[l].din != nets[0]->layers[l].din ||
+          nets[i]->layers[l].norm != nets[0]->layers[l].norm)
         return NGSGD_EINVAL;
   }
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
@@ -2042,6 +2187,9 @@ extern "C" int ngsgd_average(ngsgd_net* const* nets, int32_t n, int32_t reset_pr
   if (blocks > 4096) blocks = 4096;
   hipLaunchKernelGGL(average_kernel, dim3((unsigned)blocks), dim3(256), 0, s, a);
   LAUNCH_CHECK();
+  if (reset_preconditioners)
+    for (int i = 0; i < n; ++i)
+      if (nets[i]->adamw != nullptr) NG_TRY(ngsgd_adamw_set_state(nets[i]->adamw, nullptr, nullptr, nullptr, 0, s));
   for (int i = 0; i < n; ++i) {   // the replicas' next steps (on their own streams) wait for the new weights
     HIP_TRY(hipEventRecord(nets[i]->avg_done, s));
     nets[i]->avg_pending = true;
@@ -2064,6 +2212,50 @@ extern "C" int ngsgd_set_params(ngsgd_net* net, int32_t layer, const float* dev_
   ngsgd_layer& L = net->layers[layer];
   NG_TRY(order_after_average(net, static_cast<hipStream_t>(hip_stream), false));
   return copy2d(dev_in, L.in1, L.W, L.ldw, L.dout, L.in1, 1.f, nullptr, static_cast<hipStream_t>(hip_stream));
+}
+
+extern "C" int ngsgd_set_adamw(ngsgd_net* net, float rate, double beta1, double beta2, float epsilon, float weight_decay) {
+  if (net == nullptr || net->adamw == nullptr || !std::isfinite(rate) || !std::isfinite(weight_decay) || !(epsilon > 0.f)) return NGSGD_EINVAL;   // (epsilon 0: see ngsgd_step)
+  const NetAdamW rule(*net, beta1, beta2, epsilon, weight_decay);
+  size_t need = 0;
+  NG_TRY(ngsgd_adamw_workspace_bytes(&rule.cfg, &need));   // (the same size: checks the numbers)
+  ngsgd_adamw* made = nullptr;
+  NG_TRY(ngsgd_adamw_create(&rule.cfg, net->adamw_workspace, net->adamw_bytes, &made));
+  (void)ngsgd_adamw_destroy(net->adamw);
+  net->adamw = made;
+  net->adamw_rate = rate;
+  net->adamw_decay = weight_decay;
+  return NGSGD_OK;
+}
+
+namespace {
+// A layer norm's two vectors, copied out or in.
+int copy_pair(const float* a, const float* b, float* to_a, float* to_b, const int n, hipStream_t s) {
+  if (a != nullptr && to_a != nullptr) NG_TRY(copy2d(a, n, to_a, n, 1, n, 1.f, nullptr, s));
+  if (b != nullptr && to_b != nullptr) NG_TRY(copy2d(b, n, to_b, n, 1, n, 1.f, nullptr, s));
+  return NGSGD_OK;
+}
+bool has_norm(const ngsgd_net* net, const int layer) { return net != nullptr && layer >= 0 && layer < net->n_layers && net->layers[layer].norm; }
+}  // namespace
+
+extern "C" int ngsgd_get_norm(const ngsgd_net* net, int32_t layer, float* dev_weight, float* dev_bias, void* hip_stream) {
+  if (!has_norm(net, layer)) return NGSGD_EINVAL;
+  const ngsgd_layer& L = net->layers[layer];
+  NG_TRY(order_after_average(const_cast<ngsgd_net*>(net), static_cast<hipStream_t>(hip_stream), false));
+  return copy_pair(L.gain, L.shift, dev_weight, dev_bias, L.groups, static_cast<hipStream_t>(hip_stream));
+}
+
+extern "C" int ngsgd_set_norm(ngsgd_net* net, int32_t layer, const float* dev_weight, const float* dev_bias, void* hip_stream) {
+  if (!has_norm(net, layer)) return NGSGD_EINVAL;
+  ngsgd_layer& L = net->layers[layer];
+  NG_TRY(order_after_average(net, static_cast<hipStream_t>(hip_stream), false));
+  return copy_pair(dev_weight, dev_bias, L.gain, L.shift, L.groups, static_cast<hipStream_t>(hip_stream));
+}
+
+extern "C" int ngsgd_last_norm_gradient(ngsgd_net* net, int32_t layer, float* dev_dweight, float* dev_dbias, void* hip_stream) {
+  if (!has_norm(net, layer) || net->last_N < 1) return NGSGD_EINVAL;
+  const ngsgd_layer& L = net->layers[layer];
+  return copy_pair(L.gain_gradient, L.shift_gradient, dev_dweight, dev_dbias, L.groups, static_cast<hipStream_t>(hip_stream));
 }
 
 extern "C" int ngsgd_net_precond(ngsgd_net* net, int32_t layer, int32_t side, ngsgd_precond** out) {
