@@ -1544,7 +1544,8 @@ struct ngsgd_net {
   float* params = nullptr;          // all weight matrices, then all layer norms' weights and biases
   size_t n_weights_padded = 0, n_params_padded = 0;
   // AdamW: of the layer norms' parameters, and with its method of the weight matrices
-  float* gradients = nullptr;       // laid out as params (without the matrices where the method does not need them)
+  float* gradients = nullptr;       // laid out as params from element `first_gradient` on: the matrices' are left out where nobody needs them
+  size_t first_gradient = 0;
   float* norm_part = nullptr;       // sums over groups of rows
   void* adamw_workspace = nullptr;
   size_t adamw_bytes = 0;
@@ -1688,9 +1689,8 @@ void net_layout(ngsgd_net& net, const ngsgd_config* cfg, Carver& c) {
     off += (size_t)L.dout * L.ldw;
   }
   if (by_adamw(cfg->method) || n_norm > 0) {
-    const size_t skipped = by_adamw(cfg->method) ? 0 : n_params;   // gradients of weight matrices that nobody asks for
-    float* const g = c.take<float>(net.n_params_padded - skipped);
-    net.gradients = g != nullptr ? g - skipped : nullptr;
+    net.first_gradient = by_adamw(cfg->method) ? 0 : n_params;
+    net.gradients = c.take<float>(net.n_params_padded - net.first_gradient);
     for (auto& L : net.layers) {
       if (!L.norm) continue;
       const size_t at[2] = {off, off + pad32(L.groups)};
@@ -1698,8 +1698,8 @@ void net_layout(ngsgd_net& net, const ngsgd_config* cfg, Carver& c) {
       if (net.params != nullptr) {
         L.gain = net.params + at[0];
         L.shift = net.params + at[1];
-        L.gain_gradient = net.gradients + at[0];
-        L.shift_gradient = net.gradients + at[1];
+        L.gain_gradient = net.gradients + (at[0] - net.first_gradient);
+        L.shift_gradient = net.gradients + (at[1] - net.first_gradient);
       }
     }
     net.norm_part = c.take<float>(norm_part);
@@ -2141,7 +2141,7 @@ extern "C" int ngsgd_step(ngsgd_net* net, const float* dev_x, const int32_t* dev
     const void* grads[2];
     int n = 0;
     if (by_adamw(net->method)) grads[n++] = net->gradients;
-    if (net->n_params_padded > net->n_weights_padded) grads[n++] = net->gradients + net->n_weights_padded;
+    if (net->n_params_padded > net->n_weights_padded) grads[n++] = net->gradients + (net->n_weights_padded - net->first_gradient);
     NG_TRY(ngsgd_adamw_step(net->adamw, grads, adamw_lr, nullptr, -1.f, nullptr, s));
   }
   net->last_N = N;
@@ -2340,4 +2340,4 @@ extern "C" int ngsgd_set_wait_limit_us(int64_t microseconds) {
 }
 
 extern "C" int ngsgd_last_hip_error(void) { return g_last_hip_error; }
-extern "C" int ngsgd_version(void) { return 100; }
+extern "C" int ngsgd_version(void) { return 200; }

@@ -135,3 +135,17 @@ def test_binding_refuses_tensors_off_the_device():
         ng._check_dense(torch.zeros(8), "weight", ln.device)
     with pytest.raises(ValueError):
         ng._type_of(torch.float64)
+
+
+def test_binding_refuses_another_current_device(monkeypatch):
+    torch = pytest.importorskip("torch")
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    ng._current_device(torch.device("cuda", 1))
+    ln = ng.LayerNorm.__new__(ng.LayerNorm)
+    ln.device = torch.device("cuda", 0)
+    opt = ng.AdamW.__new__(ng.AdamW)
+    opt.device, opt.handle, opt.grad_dtype, opt.sizes, opt._m = ln.device, None, torch.float32, [1], None
+    for call in (lambda: ln.forward(None), lambda: ln.backward(None, None, None, None), lambda: opt.step([None], 0.1), lambda: opt.state(),
+                 lambda: opt.set_state(None, None, 0), lambda: opt.steps()):
+        with pytest.raises(ValueError):
+            call()
