@@ -483,6 +483,7 @@ class AdamW:
         numbers or float32 tensors of one element on the device."""
         import torch
         device, dtype, sizes, addresses = self.device, self.grad_dtype, self.sizes, []
+        index = device.index
         _current_device(device)
         if len(grads) != len(sizes):
             raise ValueError(f"{len(grads)} gradients for {len(sizes)} tensors")
@@ -490,7 +491,7 @@ class AdamW:
             if g is None or size == 0:
                 addresses.append(None)
                 continue
-            if g.dtype != dtype or g.numel() != size or g.device != device or not g.is_contiguous():
+            if g.dtype != dtype or g.numel() != size or g.get_device() != index or not g.is_contiguous():
                 raise ValueError(f"gradient {len(addresses)}: {g.dtype}, {g.numel()} elements on {g.device}, for {dtype}, {size} on "
                                  f"{device}, dense")
             addresses.append(g.data_ptr())

@@ -288,7 +288,7 @@ __device__ __forceinline__ T constant(const T* p, const int i) {
 
 // A workgroup per chunk, or per quarter of one where there are few; a wavefront takes a block at a time.  P: parameters, G: gradients.  Bound by
 // memory: 252 M elements with fp32 parameters, 16-bit gradients and moments in 8 bits 694 us (5.1 TB/s; 45 more with 1536 workgroups that walk
-// over the chunks), in 32 bits 1353 us (5.2 TB/s).  In 8 bits the vector ALU is busy for nearly as long (about 75 instructions an element: with
+// over the chunks), in 32 bits 1353 us (5.2 TB/s).  In 8 bits the vector ALU is busy for nearly as long (83 instructions an element: with
 // the library's root and quotient and codes that allow for everything in every block it took 884 us), and parameters and gradients of 16
 // bits leave it the bound (201 M elements 491 us, 4.1 TB/s).
 template <typename P, typename G, int BITS, bool MASTER>

@@ -344,6 +344,38 @@ def test_on_another_stream(ngsgd):
     assert all(torch.equal(x, y) for x, y in zip(a.params + list(want), b.params + list(got)))
 
 
+@pytest.mark.parametrize("bits", [8, 32])
+def test_more_than_2_31_elements(ngsgd, bits):
+    """The last elements of a tensor whose places need more than 32 bits, and the first ones."""
+    import torch
+    n, ends = 2 ** 31 + 300, 600
+    p = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    g = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    rng = np.random.default_rng(5)
+    # from places that begin a block: 2^31 - 512 and 0
+    for at in (0, 2 ** 31 - 512):
+        p[at:at + ends] = torch.from_numpy(rng.standard_normal(ends)).bfloat16().cuda()
+        g[at:at + ends] = torch.from_numpy(rng.standard_normal(ends)).bfloat16().cuda()
+    before = {at: (f64(p[at:at + ends]), f64(g[at:at + ends])) for at in (0, 2 ** 31 - 512)}
+    opt = ngsgd.AdamW([p], state_bits=bits)
+    opt.step([g], 0.01)
+    m, v = opt.state()
+    for at, (p0, g0) in before.items():
+        want, m1, v1 = oracle.step(p0, g0, np.zeros(ends), np.zeros(ends), 1, float(np.float32(0.01)))
+        assert np.all(np.abs(f64(p[at:at + ends]) - want) <= 2.0 ** -8 * np.abs(want) + 16 * U * 0.01 + 3 * U * np.abs(p0))
+        k = slice(at, at + 512)          # whole blocks
+        if bits == 8:
+            for got, which, a in ((m, oracle.coded_m, m1), (v, oracle.coded_v, v1)):
+                want = np.concatenate([which(a[i:i + 256], oracle.share(256, 1, at + i)) for i in (0, 256)])
+                assert np.array_equal(f64(got[k]), want)
+        else:
+            assert np.all(np.abs(f64(m[k]) - m1[:512]) <= 4 * U * np.abs(m1[:512])) and np.all(np.abs(f64(v[k]) - v1[:512]) <= 6 * U * v1[:512])
+    middle = slice(2 ** 30, 2 ** 30 + 10 ** 6)
+    assert not bool(p[middle].any()) and not bool(m[middle].any()) and not bool(v[middle].any())
+    del p, g, m, v, opt
+    torch.cuda.empty_cache()
+
+
 def test_state_goes_out_and_in(ngsgd):
     """A second optimizer with the first one's state goes on as the first does."""
     import torch

@@ -334,6 +334,41 @@ def test_captured_calls(ngsgd):
             assert all(torch.equal(p, q) for p, q in zip(got, want))
 
 
+@pytest.mark.parametrize("D", [100, 3000, 20000])
+def test_offsets_beyond_32_bits(ngsgd, D):
+    """Rows more than 2^30 elements apart: the third one starts behind 2^31."""
+    import torch
+    N, apart = 3, 2 ** 30 + 40
+    x, dy, w, b = inputs(torch, N, D, torch.bfloat16, torch.float32)
+    ln, (y, mean, rstd), (dx, dw, db) = both(torch, ngsgd, x, dy, w, b)
+
+    def far(t=None):
+        rows = torch.empty(N * apart, dtype=torch.bfloat16, device="cuda").as_strided((N, D), (apart, 1))
+        return rows if t is None else rows.copy_(t)
+
+    fx, fdy, fy = far(x), far(dy), far()
+    y2, mean2, rstd2 = ln.forward(fx, w, b, out=fy)
+    dx2, dw2, db2 = ln.backward(fdy, fx, mean, rstd, w, dx=fy)
+    assert torch.equal(mean2, mean) and torch.equal(rstd2, rstd) and torch.equal(dw2, dw) and torch.equal(db2, db)
+    assert torch.equal(dx2, dx)
+    ln.forward(fx, w, b, out=fy)
+    assert torch.equal(fy, y)
+    torch.cuda.empty_cache()
+
+
+def test_rows_that_are_not_given_stay(ngsgd):
+    import torch
+    for D in (64, 1000, 3000, 20000):
+        x, dy, w, b = inputs(torch, 9, D, torch.float32, torch.float32)
+        y, dx = (torch.full((9, D), 4.0, device="cuda") for _ in range(2))
+        mean, rstd = (torch.full((9,), 5.0, device="cuda") for _ in range(2))
+        ln = ngsgd.LayerNorm(9, D)
+        ln.forward(x[:7], w, b, out=y[:7], mean=mean[:7], rstd=rstd[:7])
+        ln.backward(dy[:7], x[:7], mean[:7], rstd[:7], w, dx=dx[:7])
+        assert bool((y[7:] == 4.0).all()) and bool((dx[7:] == 4.0).all()) and bool((mean[7:] == 5.0).all()) and bool((rstd[7:] == 5.0).all())
+        assert bool((y[:7] != 4.0).any(dim=1).all()) and bool((dx[:7] != 4.0).any(dim=1).all())
+
+
 def test_refusals(ngsgd):
     import torch
     ln = ngsgd.LayerNorm(8, 64)
