@@ -272,7 +272,7 @@ __device__ __forceinline__ AdamScalars counted(AdamScalars st, const double beta
   return st;
 }
 // Counts the step in a launch of its own, about 1.5 us (and 2.5 us of the host's time).  A counter by which the step's last workgroup knows itself
-// costs 60 ns for each workgroup, one after the other: 90 us for 1536 of them, so only steps of few workgroups count that way.
+// costs 30 to 60 ns for each workgroup, one after the other: 90 us for 1536 of them, so only steps of few workgroups count that way.
 __global__ void adamw_count_kernel(AdamScalars* st, const double beta1, const double beta2) { *st = counted(*st, beta1, beta2); }
 
 // What no thread of the launch writes: read through the scalar cache.
