@@ -12,8 +12,9 @@ using namespace ngsgd;
 namespace {
 
 constexpr int kMostColumns = 1 << 25;   // (a launch has less than 2^32 threads)
-constexpr int kWideGrid = 2048;      // workgroups that walk over rows wider than registers hold
-constexpr int kNormGroups = 512;     // most groups of rows that are summed on their own
+// Rows wider than registers hold: workgroups that walk over them; groups of rows, with at most so many columns of sums in all where
+// there are more than eight of them.
+constexpr int kWideGrid = 2048, kWideGroups = 512, kWideSums = 1 << 23;
 
 inline int type_bytes(const int type) { return type == NGSGD_FLOAT32 ? 4 : 2; }
 inline bool known_type(const int type) { return type == NGSGD_FLOAT32 || type == NGSGD_BFLOAT16 || type == NGSGD_FLOAT16; }
@@ -40,7 +41,7 @@ RowPlan row_plan(const int D, const bool backward) {
 // sums are written and read once more: with 16 wavefronts to a unit 32768 x 4096 bf16 takes 165 us instead of 150, 16384 x 1024 29 instead of 25.)
 int norm_groups(const int64_t N, const int D) {
   const RowPlan p = row_plan(D, true);
-  if (p.e == 0) return (int)std::min<int64_t>(kNormGroups, std::max<int64_t>(1, (N + 7) / 8));
+  if (p.e == 0) return (int)std::min<int64_t>({kWideGroups, std::max(8, kWideSums / D), std::max<int64_t>(1, (N + 7) / 8)});
   const int most = 256 * std::max(1, 640 / p.nt);
   return (int)std::min<int64_t>(most, std::max<int64_t>(1, (N + p.rows() - 1) / p.rows()));
 }

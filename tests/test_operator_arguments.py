@@ -52,6 +52,11 @@ def test_layernorm_workspace(lib):
         last = n.value
         assert backward(lib, N=max(rows, 1), D=1000, ldx=1000, lddy=1000, lddx=1000, nbytes=2 * 1000 * 4 - 1) == ng.NGSGD_ENOMEM
     assert last < 64 << 20
+    for dim in (16384, 16385, 40000, 10 ** 6, 1 << 25):      # rows of any width: no more than 64 MiB, or eight sums of them
+        last = 0
+        for rows in (0, 1, 100, 10 ** 4, 10 ** 9):
+            assert lib.ngsgd_layernorm_workspace_bytes(rows, dim, byref(n)) == 0 and last <= n.value <= max(64 << 20, 64 * dim) + 512
+            last = n.value
     for rows, dim in ((-1, 8), (4, 0), (4, (1 << 25) + 1)):
         assert lib.ngsgd_layernorm_workspace_bytes(rows, dim, byref(n)) == ng.NGSGD_EINVAL
     assert lib.ngsgd_layernorm_workspace_bytes(4, 8, None) == ng.NGSGD_EINVAL
