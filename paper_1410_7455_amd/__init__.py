@@ -118,11 +118,12 @@ _SIGNATURES = {
 }
 
 _lib = None
+_torch = None   # for calls that are short enough for an import statement to count
 
 
 def load_library():
     """Loads libngsgd.so and binds every declared entry point; raises if the library is missing."""
-    global _lib
+    global _lib, _torch
     if _lib is not None:
         return _lib
     if not os.path.exists(LIB_PATH):
@@ -132,7 +133,8 @@ def load_library():
     try:
         # PyTorch ships its own HIP runtime: load it first, so that the library binds to the same copy as the
         # tensors whose pointers it is given (two runtimes in one process do not know each other's memory)
-        import torch  # noqa: F401
+        import torch
+        _torch = torch
     except ImportError:
         pass
     lib = ctypes.CDLL(LIB_PATH)
@@ -276,14 +278,13 @@ def _type_of(dtype):
 # formed when they are needed (the calls are short: a small layer norm takes 2 us on the GPU).
 
 def _current_device(device):
-    import torch
-    if device.index != torch.cuda.current_device():
+    if device.index != _torch.cuda.current_device():
         raise ValueError(f"made for {device}, which is not the current device")
 
 
 def _check_dense(t, name, device, dtype=None, numel=None):
     """A dense tensor on the device."""
-    if t.device != device:
+    if t.get_device() != device.index:
         raise ValueError(f"{name} is on {t.device}, not on {device}")
     if not t.is_contiguous():
         raise ValueError(f"{name} is not dense")
@@ -294,8 +295,7 @@ def _check_dense(t, name, device, dtype=None, numel=None):
 
 
 def _raw_stream(stream, device):
-    import torch
-    return (torch.cuda.current_stream(device.index) if stream is None else stream).cuda_stream
+    return (_torch.cuda.current_stream(device.index) if stream is None else stream).cuda_stream
 
 
 def _address(t):
@@ -304,8 +304,7 @@ def _address(t):
 
 def _allocate_on(stream):
     """Outputs are allocated on the stream that writes them."""
-    import torch
-    return nullcontext() if stream is None else torch.cuda.stream(stream)
+    return nullcontext() if stream is None else _torch.cuda.stream(stream)
 
 
 class LayerNorm:
@@ -327,7 +326,7 @@ class LayerNorm:
 
     def _rows(self, t, name, like=None):
         """(number of rows, leading dimension)"""
-        if t.device != self.device:
+        if t.get_device() != self.device.index:
             raise ValueError(f"{name} is on {t.device}, not on {self.device}")
         shape = t.shape
         if len(shape) < 1 or shape[-1] != self.dim:
@@ -346,36 +345,35 @@ class LayerNorm:
 
     def _vector_dtype(self, x, *named):
         """The type of the given weights (of the first one present; float32 if there is none)."""
-        import torch
         dtype = None
         for name, v in named:
             if v is None:
                 continue
             if dtype is None:
                 dtype = v.dtype
-                if dtype != x.dtype and dtype != torch.float32:
+                if dtype != x.dtype and dtype != _torch.float32:
                     raise ValueError(f"{name} is {dtype} for {x.dtype} rows")
             _check_dense(v, name, self.device, dtype, self.dim)
-        return torch.float32 if dtype is None else dtype
+        return _torch.float32 if dtype is None else dtype
 
     def forward(self, x, weight=None, bias=None, out=None, mean=None, rstd=None, stream=None):
         """(y, mean, rstd); y into `out` if given (which may be x), the rows' float32 mean and rstd into `mean` and `rstd`."""
-        import torch
         _current_device(self.device)
         rows, ldx = self._rows(x, "x")
         weight_type = _type_of(self._vector_dtype(x, ("weight", weight), ("bias", bias)))
         ldy = self.dim if out is None else self._rows(out, "out", x)[1]
-        for name, v in (("mean", mean), ("rstd", rstd)):
-            if v is not None:
-                _check_dense(v, name, self.device, torch.float32, rows)
+        if mean is not None:
+            _check_dense(mean, "mean", self.device, _torch.float32, rows)
+        if rstd is not None:
+            _check_dense(rstd, "rstd", self.device, _torch.float32, rows)
         if out is None or mean is None or rstd is None:
             with _allocate_on(stream):
                 if out is None:
-                    out = torch.empty_like(x, memory_format=torch.contiguous_format)
+                    out = _torch.empty_like(x, memory_format=_torch.contiguous_format)
                 if mean is None:
-                    mean = torch.empty(rows, dtype=torch.float32, device=self.device)
+                    mean = _torch.empty(rows, dtype=_torch.float32, device=self.device)
                 if rstd is None:
-                    rstd = torch.empty(rows, dtype=torch.float32, device=self.device)
+                    rstd = _torch.empty(rows, dtype=_torch.float32, device=self.device)
         _check(self.lib.ngsgd_layernorm_forward(x.data_ptr(), ldx, _type_of(x.dtype), _address(weight), _address(bias), weight_type,
                                                 rows, self.dim, self.epsilon, out.data_ptr(), ldy, mean.data_ptr(),
                                                 rstd.data_ptr(), _raw_stream(stream, self.device)), "ngsgd_layernorm_forward")
@@ -385,21 +383,20 @@ class LayerNorm:
                  stream=None):
         """(dx, dweight, dbias) for the derivative dy of y and the mean and rstd of the forward pass; None where `needs`
         says so and none is given.  dx may be dy.  dweight and dbias are of the weight's type (float32 without a weight)."""
-        import torch
         _current_device(self.device)
         rows, ldx = self._rows(x, "x")
         _, lddy = self._rows(dy, "dy", x)
-        _check_dense(mean, "mean", self.device, torch.float32, rows)
-        _check_dense(rstd, "rstd", self.device, torch.float32, rows)
+        _check_dense(mean, "mean", self.device, _torch.float32, rows)
+        _check_dense(rstd, "rstd", self.device, _torch.float32, rows)
         vector = self._vector_dtype(x, ("weight", weight), ("dweight", dweight), ("dbias", dbias))
         lddx = self.dim if dx is None else self._rows(dx, "dx", x)[1]
         with _allocate_on(stream):
             if dx is None and needs[0]:
-                dx = torch.empty_like(x, memory_format=torch.contiguous_format)
+                dx = _torch.empty_like(x, memory_format=_torch.contiguous_format)
             if dweight is None and needs[1]:
-                dweight = torch.empty(self.dim, dtype=vector, device=self.device)
+                dweight = _torch.empty(self.dim, dtype=vector, device=self.device)
             if dbias is None and needs[2]:
-                dbias = torch.empty(self.dim, dtype=vector, device=self.device)
+                dbias = _torch.empty(self.dim, dtype=vector, device=self.device)
         _check(self.lib.ngsgd_layernorm_backward(dy.data_ptr(), lddy, x.data_ptr(), ldx, _type_of(x.dtype), _address(weight),
                                                  _type_of(vector), mean.data_ptr(), rstd.data_ptr(), rows, self.dim,
                                                  _address(dx), lddx, _address(dweight), _address(dbias),
@@ -481,7 +478,6 @@ class AdamW:
     def step(self, grads, lr, grad_scale=None, stream=None):
         """One step.  grads: a dense tensor of grad_dtype for each parameter, or None to leave that one as it is.  lr and grad_scale are
         numbers or float32 tensors of one element on the device."""
-        import torch
         device, dtype, sizes, addresses = self.device, self.grad_dtype, self.sizes, []
         index = device.index
         _current_device(device)
@@ -498,8 +494,8 @@ class AdamW:
         self._grads[:] = addresses
         factors = []
         for name, value in (("lr", lr), ("grad_scale", grad_scale)):
-            if isinstance(value, torch.Tensor):
-                _check_dense(value, name, device, torch.float32, 1)
+            if isinstance(value, _torch.Tensor):
+                _check_dense(value, name, device, _torch.float32, 1)
                 factors += [1.0, value.data_ptr()]
             else:
                 factors += [1.0 if value is None else value, None]
@@ -509,14 +505,13 @@ class AdamW:
         """(m, v), flat; tensor k's are [offsets[k] : offsets[k] + sizes[k]].  With 32 bits the arrays themselves (or copies in
         bfloat16, if asked for); with 8 bits the values of the codes, in float32 or in bfloat16, which holds them exactly (but for a
         v below 2^-126)."""
-        import torch
-        dtype = torch.float32 if dtype is None else dtype
-        if self._m is not None and dtype == torch.float32:
+        dtype = _torch.float32 if dtype is None else dtype
+        if self._m is not None and dtype == _torch.float32:
             return self._m, self._v
         _current_device(self.device)
         with _allocate_on(stream):
-            m = torch.empty(self.elements, dtype=dtype, device=self.device)
-            v = torch.empty(self.elements, dtype=dtype, device=self.device)
+            m = _torch.empty(self.elements, dtype=dtype, device=self.device)
+            v = _torch.empty(self.elements, dtype=dtype, device=self.device)
         _check(self.lib.ngsgd_adamw_get_state(self.handle, m.data_ptr(), v.data_ptr(), _type_of(dtype), None, _raw_stream(stream, self.device)),
                "ngsgd_adamw_get_state")
         return m, v

@@ -215,6 +215,35 @@ struct BackwardRow {
   }
 };
 
+// Sums over the rows that a workgroup worked on side by side, in order, to `to_w` and `to_b` (nullptr: not asked for).
+template <typename S, typename T, int LDS>
+__device__ __forceinline__ void store_sums(const float (&dw)[S::E], const float (&db)[S::E], T* to_w, T* to_b, float (&sums)[LDS],
+                                           const RowColumns<S>& cols) {
+  constexpr int E = S::E;
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    T* const to = which == 0 ? to_w : to_b;
+    if (to == nullptr) continue;   // (uniform)
+    if constexpr (S::ROWS == 1) {
+      store_row<S, true>(which == 0 ? dw : db, to, cols);
+    } else {
+      __syncthreads();
+#pragma unroll
+      for (int e = 0; e < E; ++e) sums[threadIdx.x * E + e] = which == 0 ? dw[e] : db[e];
+      __syncthreads();
+      if (S::row() != 0) continue;
+      float v[E];
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        v[e] = 0.f;
+#pragma unroll
+        for (int r = 0; r < S::ROWS; ++r) v[e] += sums[(r * S::threads() + S::member()) * E + e];
+      }
+      store_row<S, true>(v, to, cols);
+    }
+  }
+}
+
 // Sums of a workgroup's rows go to part[workgroup][dw, db][D].  Bound by memory, as long as enough rows are in flight: 16384 x 8192 bf16 takes
 // 168 us with one row to come and 151 with two (5.3 TB/s, the rate of a large copy); the gradient is formed from x and dy again behind the
 // row's sums, so that registers hold rows to come instead of xhat and g.
@@ -281,28 +310,11 @@ __global__ __launch_bounds__(S::NT) void layernorm_backward_kernel(const LayerNo
     }
   }
   if (a.part == nullptr) return;
-  float* const part = a.part + (size_t)blockIdx.x * 2 * a.D;
-  if (S::ROWS == 1) {
-    store_row<S, true>(dw, part, cols);
-    store_row<S, true>(db, part + a.D, cols);
-    return;
-  }
-  // the rows that the workgroup worked on side by side, in order
-#pragma unroll
-  for (int which = 0; which < 2; ++which) {
-    __syncthreads();
-#pragma unroll
-    for (int e = 0; e < E; ++e) sums[threadIdx.x * E + e] = which == 0 ? dw[e] : db[e];
-    __syncthreads();
-    if (S::row() != 0) continue;
-    float v[E];
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      v[e] = 0.f;
-#pragma unroll
-      for (int r = 0; r < S::ROWS; ++r) v[e] += sums[(r * S::threads() + S::member()) * E + e];
-    }
-    store_row<S, true>(v, part + (size_t)which * a.D, cols);
+  if (a.groups == 1) {   // these are the sums
+    store_sums<S>(dw, db, static_cast<W*>(a.dw), static_cast<W*>(a.db), sums, cols);
+  } else {
+    float* const part = a.part + (size_t)blockIdx.x * 2 * a.D;
+    store_sums<S>(dw, db, part, part + a.D, sums, cols);
   }
 }
 

@@ -144,6 +144,7 @@ def test_binding_refuses_tensors_off_the_device():
 
 def test_binding_refuses_another_current_device(monkeypatch):
     torch = pytest.importorskip("torch")
+    ng.load_library()
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
     ng._current_device(torch.device("cuda", 1))
     ln = ng.LayerNorm.__new__(ng.LayerNorm)
