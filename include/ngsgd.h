@@ -298,7 +298,8 @@ int ngsgd_create(const ngsgd_config* cfg, void* dev_workspace, size_t workspace_
 int ngsgd_destroy(ngsgd_net* net);
 
 /* One NG-SGD minibatch step (Sec. 2, 4.5-4.7): maximises sum_i log p(y_i | x_i) by
- * W_l += lr * a_l * Obar_l^T Xbar_l for every layer, gradients summed over the minibatch.
+ * W_l += lr * a_l * Obar_l^T Xbar_l for every layer (with the AdamW methods by an AdamW step along O_l^T X_l), gradients
+ * summed over the minibatch.
  *   dev_x       N x dims[0] features, dense (ld = dims[0], which must be a multiple of 4)
  *   dev_labels  N class indices in [0, dims[n_layers])
  *   dev_logprob_sum (optional, 1 double) receives sum_i log p(y_i | x_i) evaluated before the update */

@@ -320,7 +320,6 @@ __global__ __launch_bounds__(S::NT) void layernorm_backward_kernel(const LayerNo
 
 // ---- rows of any width, read from memory in every pass -------------------------------------------------
 constexpr int kWideThreads = 1024;
-constexpr int kRegisterColumns = 16384;   // the widest rows of the kernels above
 
 // f(column, value) for a thread's elements of a row
 template <typename T, typename F>
@@ -365,27 +364,19 @@ __global__ __launch_bounds__(kWideThreads) void layernorm_forward_wide_kernel(co
   }
 }
 
-template <typename T, bool SLABS>
-__device__ __forceinline__ float dy_of(const LayerNormBackward& a, const int64_t row, const int64_t c) {
-  const T* const p = static_cast<const T*>(a.dy) + row * a.lddy + c;
-  float v = to_float(p[0]);
-  if constexpr (SLABS)
-    for (int k = 1; k < a.n_slabs; ++k) v += to_float(p[k * a.slab_stride]);
-  return v;
-}
-
-template <typename T, typename W, bool SLABS>
+template <typename T, typename W>
 __global__ __launch_bounds__(kWideThreads) void layernorm_backward_rows_kernel(const LayerNormBackward a) {
   __shared__ BlockScratch red;
   const W* const w = static_cast<const W*>(a.w);
   int parity = 0;
   for (int64_t row = blockIdx.x; row < a.N; row += gridDim.x, parity ^= 1) {
     const T* const x = static_cast<const T*>(a.x) + row * a.ldx;
+    const T* const dy = static_cast<const T*>(a.dy) + row * a.lddy;
     T* const dx = static_cast<T*>(a.dx) + row * a.lddx;
     const float mean = a.mean[row], rstd = a.rstd[row];
     float c1 = 0.f, c2 = 0.f;
     for_row(x, a.D, [&](int c, float v) {
-      float g = dy_of<T, SLABS>(a, row, c);
+      float g = to_float(dy[c]);
       if (w != nullptr) g *= to_float(w[c]);
       c1 += g;
       c2 += g * ((v - mean) * rstd);
@@ -394,7 +385,7 @@ __global__ __launch_bounds__(kWideThreads) void layernorm_backward_rows_kernel(c
     c1 /= (float)a.D;
     c2 /= (float)a.D;
     for_row(x, a.D, [&](int c, float v) {
-      float g = dy_of<T, SLABS>(a, row, c);
+      float g = to_float(dy[c]);
       if (w != nullptr) g *= to_float(w[c]);
       dx[c] = from_float<T>(rstd * (g - c1 - ((v - mean) * rstd) * c2));
     });
@@ -403,14 +394,14 @@ __global__ __launch_bounds__(kWideThreads) void layernorm_backward_rows_kernel(c
 
 // Sums over the rows of a group: grid (columns / 256, groups), a thread per column.
 constexpr int kColumnThreads = 256;
-template <typename T, bool SLABS>
+template <typename T>
 __global__ __launch_bounds__(kColumnThreads) void layernorm_backward_columns_kernel(const LayerNormBackward a) {
   const int64_t c = (int64_t)blockIdx.x * kColumnThreads + threadIdx.x;
   if (c >= a.D) return;
   const int64_t first = a.N * blockIdx.y / a.groups, end = a.N * (blockIdx.y + 1) / a.groups;
   float dw = 0.f, db = 0.f;
   for (int64_t row = first; row < end; ++row) {
-    const float dy = dy_of<T, SLABS>(a, row, c);
+    const float dy = to_float(static_cast<const T*>(a.dy)[row * a.lddy + c]);
     dw += dy * ((to_float(static_cast<const T*>(a.x)[row * a.ldx + c]) - a.mean[row]) * a.rstd[row]);
     db += dy;
   }

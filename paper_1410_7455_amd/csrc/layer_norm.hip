@@ -39,6 +39,9 @@ RowPlan row_plan(const int D, const bool backward) {
 }
 // Groups of rows whose sums are formed on their own: the workgroups of the backward pass, about ten wavefronts to a compute unit.  (Their
 // sums are written and read once more: with 16 wavefronts to a unit 32768 x 4096 bf16 takes 165 us instead of 150, 16384 x 1024 29 instead of 25.)
+int backward_grid(const int64_t N, const RowPlan& p) {
+  return (int)std::min<int64_t>(256 * std::max(1, 640 / p.nt), std::max<int64_t>(1, (N + p.rows() - 1) / p.rows()));
+}
 int norm_groups(const int64_t N, const int D) {
   const RowPlan p = row_plan(D, true);
   if (p.e == 0) return (int)std::min<int64_t>({kWideGroups, std::max(8, kWideSums / D), std::max<int64_t>(1, (N + 7) / 8)});
@@ -46,8 +49,7 @@ int norm_groups(const int64_t N, const int D) {
   // instead of 6.1, 16 x 512 bf16 4.6 instead of 5.4, 4 x 4096 5.8 instead of 5.9 (eight rounds: 8 x 4096 8.9 instead of 6.0), and the host
   // saves 3 of 14 us.  With one row in hand at a time only one is: 4 x 16384 29 instead of 16.
   if (N <= (p.e == 16 && p.tpr == 0 ? 1 : 4) * p.rows()) return 1;
-  const int most = 256 * std::max(1, 640 / p.nt);
-  return (int)std::min<int64_t>(most, std::max<int64_t>(1, (N + p.rows() - 1) / p.rows()));
+  return backward_grid(N, p);
 }
 unsigned forward_grid(const int64_t N, const RowPlan& p) {
   return (unsigned)std::min<int64_t>(256 * std::max(1, 1536 / p.nt), (N + p.rows() - 1) / p.rows());
@@ -73,18 +75,19 @@ int launch_backward(const LayerNormBackward& a, hipStream_t s) {
   const int64_t columns = ((int64_t)a.D + kColumnThreads - 1) / kColumnThreads;
   if (a.N > 0 && plan.e != 0) {
     with_row_shape<T>(plan, [&](auto shape) {
-      hipLaunchKernelGGL((layernorm_backward_kernel<T, W, decltype(shape), SLABS>), dim3(a.part != nullptr ? a.groups : norm_groups(a.N, a.D)),
+      hipLaunchKernelGGL((layernorm_backward_kernel<T, W, decltype(shape), SLABS>), dim3(a.part != nullptr ? a.groups : backward_grid(a.N, plan)),
                          dim3(plan.nt), 0, s, a);
     });
     LAUNCH_CHECK();
+  } else if (SLABS) {
+    return NGSGD_EINVAL;
   } else if (a.N > 0) {
     if (a.part != nullptr) {   // the sums first: the gradient may overwrite dy
-      hipLaunchKernelGGL((layernorm_backward_columns_kernel<T, SLABS>), dim3((unsigned)columns, a.groups), dim3(kColumnThreads), 0, s, a);
+      hipLaunchKernelGGL(layernorm_backward_columns_kernel<T>, dim3((unsigned)columns, a.groups), dim3(kColumnThreads), 0, s, a);
       LAUNCH_CHECK();
     }
     if (a.dx != nullptr) {
-      hipLaunchKernelGGL((layernorm_backward_rows_kernel<T, W, SLABS>), dim3((unsigned)std::min<int64_t>(a.N, kWideGrid)), dim3(kWideThreads), 0,
-                         s, a);
+      hipLaunchKernelGGL((layernorm_backward_rows_kernel<T, W>), dim3((unsigned)std::min<int64_t>(a.N, kWideGrid)), dim3(kWideThreads), 0, s, a);
       LAUNCH_CHECK();
     }
   }

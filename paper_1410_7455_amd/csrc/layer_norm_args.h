@@ -5,6 +5,8 @@
 
 namespace ngsgd {
 
+constexpr int kRegisterColumns = 16384;   // wider rows are read from memory in every pass
+
 struct LayerNormForward {
   const void* x;
   int64_t ldx;
@@ -36,7 +38,7 @@ struct LayerNormBackward {
   int D;
   float* part;       // [groups][2][D] sums over a group of rows; nullptr: none
   int groups;
-  int n_slabs;       // dy is the sum of so many matrices (partial products), slab_stride elements apart
+  int n_slabs;       // dy is the sum of so many matrices (partial products), slab_stride elements apart; 1 above kRegisterColumns
   int64_t slab_stride;
 };
 

@@ -1990,6 +1990,7 @@ extern "C" int ngsgd_step(ngsgd_net* net, const float* dev_x, const int32_t* dev
     g.c_split_stride = (long long)slab;
     const int tiles = ((N + 63) / 64) * ((L.din + 63) / 64);
     g.splits = std::min(kMaxBwdSplits, choose_splits(tiles, (L.dout + 31) / 32));
+    if (P.norm && L.din > kRegisterColumns) g.splits = 1;   // (as many tiles are not split anyway)
     const bool whole = P.nonlin == NGSGD_TANH && !P.norm && backward_in_one(g);
     if (whole) {   // the derivative straight from the product
       g.splits = 1;

@@ -101,6 +101,15 @@ def test_steps_match_the_oracle(ngsgd, dims, nonlin, rows, method):
         p.step(1e-3)
 
 
+@pytest.mark.parametrize("dims,nonlin,rows", [([16, 30, 200, 700, 400, 300], [PNORM | LAYERNORM] + [TANH | LAYERNORM] * 3, 40),
+                                              ([16, 2080, 9000, 600], [TANH | LAYERNORM] * 2, 33), ([16, 17000, 600], [TANH | LAYERNORM], 5)])
+def test_every_width_of_row(ngsgd, dims, nonlin, rows):
+    """Rows of 6, 200, 700, 400 numbers (parts of a wavefront), 2080 and 9000 (workgroups), most behind split products, and 17000 (from memory)."""
+    p = Pair(ngsgd, dims, nonlin, rows, method="adamw")
+    for t in range(2):
+        p.step(1e-3)
+
+
 @pytest.mark.parametrize("side_streams", [1, 3])
 def test_past_the_always_update_phase(ngsgd, side_streams):
     p = Pair(ngsgd, [24, 200, 60, 50], [PNORM | LAYERNORM, TANH | LAYERNORM], 64, renorm=True, max_change=0.075, side_streams=side_streams)
