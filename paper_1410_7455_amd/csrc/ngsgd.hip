@@ -1778,6 +1778,7 @@ extern "C" int ngsgd_workspace_bytes(const ngsgd_config* cfg, size_t* out_bytes)
   ngsgd_net net;
   Carver c(nullptr);
   net_layout(net, cfg, c);
+  if ((by_adamw(net.method) || net.n_params_padded > net.n_weights_padded) && net.adamw_bytes == 0) return NGSGD_EINVAL;   // more than AdamW takes
   *out_bytes = align_up(c.off, 256);
   return NGSGD_OK;
 }

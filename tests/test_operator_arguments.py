@@ -155,3 +155,30 @@ def test_binding_refuses_another_current_device(monkeypatch):
                  lambda: opt.set_state(None, None, 0), lambda: opt.steps()):
         with pytest.raises(ValueError):
             call()
+
+
+def test_networks_with_layer_norm_or_adamw(lib):
+    from test_library_abi import make_cfg
+    n = c_size_t(0)
+
+    def need(nonlin, **kw):
+        rc = lib.ngsgd_workspace_bytes(byref(make_cfg([40, 128, 50], [nonlin], rank_in=4, rank_out=8, max_batch=64, **kw)), byref(n))
+        return n.value if rc == 0 else rc
+
+    plain = need(ng.NGSGD_TANH)
+    normed = need(ng.NGSGD_TANH | ng.NGSGD_LAYERNORM)
+    # the nonlinearity's output, parameters, gradients and two moments
+    assert normed >= plain + 64 * 128 * 4 + 5 * 2 * 128 * 4
+    params = 128 * 64 + 50 * 160                       # padded rows
+    by32, by8 = (need(ng.NGSGD_TANH, method=m) for m in (ng.NGSGD_METHOD_ADAMW, ng.NGSGD_METHOD_ADAMW8))
+    assert by32 - by8 == pytest.approx(6 * params, abs=2048)
+    assert need(ng.NGSGD_PNORM | ng.NGSGD_LAYERNORM, pnorm_group=4) > 0
+    for nonlin, kw in ((ng.NGSGD_LAYERNORM + 2, {}), (2 * ng.NGSGD_LAYERNORM, {}), (-1, {}), (ng.NGSGD_TANH, dict(method=4)),
+                       (ng.NGSGD_TANH, dict(method=ng.NGSGD_METHOD_ADAMW, max_change_per_sample=0.1)),
+                       (ng.NGSGD_PNORM | ng.NGSGD_LAYERNORM, dict(pnorm_group=5))):
+        assert need(nonlin, **kw) == ng.NGSGD_EINVAL
+    huge = make_cfg([4, 2 ** 31 - 65, 2 ** 10], [ng.NGSGD_TANH], max_batch=1, method=ng.NGSGD_METHOD_ADAMW)
+    assert lib.ngsgd_workspace_bytes(byref(huge), byref(n)) == ng.NGSGD_EINVAL
+    for call in (lambda: lib.ngsgd_get_norm(None, 0, None, None, None), lambda: lib.ngsgd_set_norm(None, 0, None, None, None),
+                 lambda: lib.ngsgd_last_norm_gradient(None, 0, None, None, None), lambda: lib.ngsgd_set_adamw(None, 1.0, 0.9, 0.999, 1e-8, 0.0)):
+        assert call() == ng.NGSGD_EINVAL
