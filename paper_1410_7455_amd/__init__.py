@@ -294,8 +294,14 @@ def _check_dense(t, name, device, dtype=None, numel=None):
         raise ValueError(f"{name} has {t.numel()} elements, not {numel}")
 
 
-def _raw_stream(stream, device):
-    return (_torch.cuda.current_stream(device.index) if stream is None else stream).cuda_stream
+def _raw_stream(stream, device, workspace=None, home=None):
+    """The stream's hipStream_t.  A workspace that is used on another stream than the one it was allocated on (`home`) is not given to
+    anybody else before that stream is done with it, though its owner may be gone."""
+    stream = _torch.cuda.current_stream(device.index) if stream is None else stream
+    raw = stream.cuda_stream
+    if workspace is not None and raw != home:
+        workspace.record_stream(stream)
+    return raw
 
 
 def _address(t):
@@ -312,7 +318,8 @@ class LayerNorm:
 
     Inputs are float32, bfloat16 or float16, (..., dim) with up to max_rows rows; rows are dense (the last stride is 1) and,
     as a matrix, may lie any distance apart.  Weight and bias (optional) have the input's type or float32, the same for both.  Calls on
-    one object are issued in order on one stream: the workspace is shared."""
+    one object are issued in order on one stream: the workspace is shared.  As with torch's own operators, tensors that are given to a
+    call on another stream than their own are the caller's to keep until it has run (torch.Tensor.record_stream)."""
 
     def __init__(self, max_rows, dim, epsilon=1e-5):
         import torch
@@ -323,6 +330,7 @@ class LayerNorm:
         self.workspace_bytes = nbytes.value
         self.workspace = torch.empty(nbytes.value, dtype=torch.uint8, device="cuda")
         self.device = self.workspace.device
+        self._home = _raw_stream(None, self.device)
 
     def _rows(self, t, name, like=None):
         """(number of rows, leading dimension)"""
@@ -400,7 +408,8 @@ class LayerNorm:
         _check(self.lib.ngsgd_layernorm_backward(dy.data_ptr(), lddy, x.data_ptr(), ldx, _type_of(x.dtype), _address(weight),
                                                  _type_of(vector), mean.data_ptr(), rstd.data_ptr(), rows, self.dim,
                                                  _address(dx), lddx, _address(dweight), _address(dbias),
-                                                 self.workspace.data_ptr(), self.workspace_bytes, _raw_stream(stream, self.device)),
+                                                 self.workspace.data_ptr(), self.workspace_bytes,
+                                                 _raw_stream(stream, self.device, self.workspace, self._home)),
                "ngsgd_layernorm_backward")
         return dx, dweight, dbias
 
@@ -410,7 +419,8 @@ class AdamW:
 
     The parameters are dense tensors, updated in place where they lie.  weight_decay and rate (a factor on the learning rate) are
     numbers or one number per tensor.  state_bits is 32 or 8; master keeps fp32 copies of parameters in 16 bits.  Calls on
-    one object are issued in order on one stream."""
+    one object are issued in order on one stream.  As with torch's own operators, tensors that are given to a call on another
+    stream than their own are the caller's to keep until it has run (torch.Tensor.record_stream)."""
 
     def __init__(self, params, betas=(0.9, 0.999), epsilon=1e-8, weight_decay=0.0, rate=1.0, grad_dtype=None, state_bits=32,
                  master=False):
@@ -447,6 +457,7 @@ class AdamW:
         _check(self.lib.ngsgd_adamw_workspace_bytes(byref(cfg), byref(nbytes)), "ngsgd_adamw_workspace_bytes")
         self.workspace_bytes = nbytes.value
         self.workspace = torch.empty(nbytes.value, dtype=torch.uint8, device=self.device)
+        self._home = _raw_stream(None, self.device)
         h = c_void_p(0)
         _check(self.lib.ngsgd_adamw_create(byref(cfg), _ptr(self.workspace), nbytes.value, byref(h)), "ngsgd_adamw_create")
         self.handle = h
@@ -499,7 +510,7 @@ class AdamW:
                 factors += [1.0, value.data_ptr()]
             else:
                 factors += [1.0 if value is None else value, None]
-        _check(self.lib.ngsgd_adamw_step(self.handle, self._grads, *factors, _raw_stream(stream, self.device)), "ngsgd_adamw_step")
+        _check(self.lib.ngsgd_adamw_step(self.handle, self._grads, *factors, _raw_stream(stream, self.device, self.workspace, self._home)), "ngsgd_adamw_step")
 
     def state(self, dtype=None, stream=None):
         """(m, v), flat; tensor k's are [offsets[k] : offsets[k] + sizes[k]].  With 32 bits the arrays themselves (or copies in
@@ -512,7 +523,7 @@ class AdamW:
         with _allocate_on(stream):
             m = _torch.empty(self.elements, dtype=dtype, device=self.device)
             v = _torch.empty(self.elements, dtype=dtype, device=self.device)
-        _check(self.lib.ngsgd_adamw_get_state(self.handle, m.data_ptr(), v.data_ptr(), _type_of(dtype), None, _raw_stream(stream, self.device)),
+        _check(self.lib.ngsgd_adamw_get_state(self.handle, m.data_ptr(), v.data_ptr(), _type_of(dtype), None, _raw_stream(stream, self.device, self.workspace, self._home)),
                "ngsgd_adamw_get_state")
         return m, v
 
@@ -524,7 +535,7 @@ class AdamW:
         for name, a in (("m", m), ("v", v), ("master", master)):
             if a is not None:
                 _check_dense(a, name, self.device, torch.float32, self.elements)
-        _check(self.lib.ngsgd_adamw_set_state(self.handle, _address(m), _address(v), _address(master), int(t), _raw_stream(stream, self.device)),
+        _check(self.lib.ngsgd_adamw_set_state(self.handle, _address(m), _address(v), _address(master), int(t), _raw_stream(stream, self.device, self.workspace, self._home)),
                "ngsgd_adamw_set_state")
 
     def steps(self):
@@ -532,7 +543,7 @@ class AdamW:
         import torch
         _current_device(self.device)
         t = torch.empty(1, dtype=torch.int64, device=self.device)
-        _check(self.lib.ngsgd_adamw_get_state(self.handle, None, None, NGSGD_FLOAT32, t.data_ptr(), _raw_stream(None, self.device)),
+        _check(self.lib.ngsgd_adamw_get_state(self.handle, None, None, NGSGD_FLOAT32, t.data_ptr(), _raw_stream(None, self.device, self.workspace, self._home)),
                "ngsgd_adamw_get_state")
         return int(t.item())
 

@@ -113,3 +113,40 @@ def test_two_programs_on_two_streams(ngsgd):
     torch.cuda.synchronize()
     for p in both:
         assert all(np.array_equal(x, y) for x, y in zip(p.values(), want.values()))
+
+
+def test_objects_that_are_gone_before_their_work(ngsgd):
+    """Calls on another stream than the objects were made on, the objects deleted before that stream gets to them: their workspaces are
+    nobody else's until then."""
+    import torch
+    N, D = 4000, 2000
+    torch.manual_seed(5)
+    x, dy = torch.randn(N, D, device="cuda"), torch.randn(N, D, device="cuda")
+    w = torch.ones(D, device="cuda")
+    y, mean, rstd = ngsgd.LayerNorm(N, D).forward(x, w)
+    want = ngsgd.LayerNorm(N, D).backward(dy, x, mean, rstd, w)
+    start = torch.randn(300000, device="cuda")
+    grad = torch.randn(300000, device="cuda")
+    moved = start.clone()
+    ngsgd.AdamW([moved], state_bits=8).step([grad], 0.1)
+    s = torch.cuda.Stream()
+    big = torch.randn(4096, 4096, device="cuda")
+    for given in (True, False):
+        ln, p = ngsgd.LayerNorm(N, D), start.clone()
+        opt = ngsgd.AdamW([p], state_bits=8)
+        sizes = [ln.workspace.numel(), opt.workspace.numel()]
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            for _ in range(30):          # some milliseconds before its turn
+                big = big @ big * 1e-3
+            if not given:
+                got = ln.backward(dy, x, mean, rstd, w)
+                opt.step([grad], 0.1)
+        if given:
+            got = ln.backward(dy, x, mean, rstd, w, stream=s)
+            opt.step([grad], 0.1, stream=s)
+        del ln, opt
+        taken = [torch.zeros(n, dtype=torch.uint8, device="cuda") for n in sizes for _ in range(3)]   # (a table of zeros is one without work)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)) and torch.equal(p, moved)
+        del taken
