@@ -262,7 +262,7 @@ int ngsgd_adamw_destroy(ngsgd_adamw* h);
  *   dev_lr, dev_grad_scale (optional, 1 float each) are multiplied to lr and grad_scale: a schedule or the
  *               factor of a clipped norm that only the device knows
  * The step count lives on the device, so a captured step counts on at each replay (with the gradients' addresses,
- * lr and grad_scale of its capture).  Up to 448 tensors take one launch.
+ * lr and grad_scale of its capture; the workspace has to be there as long as the graph).  Up to 448 tensors take one launch.
  * Moments in 8 bits: m as a sign, 4 bits of exponent and 3 behind the point, sqrt(v) as 5 and 3 bits, below an exponent that 256
  * elements share; p is updated from this step's moments before they are coded.  They are rounded down
  * after a share of a step has been added, frac(i A + t B) of the element's place i in the flat arrays and t (A, B = 0x9E3779B1,
