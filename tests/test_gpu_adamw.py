@@ -421,3 +421,46 @@ def test_refusals(ngsgd):
     with pytest.raises(ngsgd.NgsgdError):
         opt.set_state(flat, flat, 1, master=flat)
     assert opt.steps() == 0
+
+
+@pytest.mark.parametrize("lr,decay", [(2e-5, 0.01), (1e-5, 0.01), (1e-6, 0.1), (1e-6, 0.01)])
+@pytest.mark.parametrize("bits,master", [(32, False), (8, False), (32, True), (8, True)])
+def test_small_decays_are_applied(ngsgd, bits, master, lr, decay):
+    """A decay of less than a step of fp32 shows in the mean over many elements.
+
+    Tolerance for the mean of (p - want) / before: an element is rounded once, by at most u of itself, evenly over the elements (their
+    steps differ by many times their last bit), so the mean has a standard deviation of u / sqrt(3 n), taken six times; the step, known to 16 u, has
+    a sign of its own in each element.  A factor 1 - lr decay rounded to fp32 would be off by up to u in all elements alike, 300 times that."""
+    import torch
+    n = 1 << 20
+    b = Bench(torch, ngsgd, [n], *(("bfloat16", "bfloat16") if master else ()), bits=bits, master=master, t=500, weight_decay=decay)
+    start = b.rng.choice([-1.0, 1.0], n) * b.rng.uniform(1 / 16, 1 / 8, n)
+    fp32 = torch.from_numpy(start).float().cuda()
+    m, v = (a.clone() for a in b.opt.state())
+    if not master:
+        b.params[0].copy_(fp32)
+    b.opt.set_state(m, v, 500, master=fp32 if master else None)
+    (p0,), (m0,), (v0,) = b.before()
+    grads = b.gradients()
+    b.opt.step(grads, lr)
+    rate, fade = float(np.float32(lr)), float(np.float32(decay))
+    want, _, _ = oracle.step(p0, f64(grads[0]), m0, v0, 501, rate, decay=fade)
+    got = f64(b.opt.master if master else b.params[0])
+    moved = want - p0 * (1 - rate * fade)
+    assert abs(np.mean((got - want) / p0)) <= 6 * U / np.sqrt(3 * n) + 16 * U * abs(np.mean(moved / p0))
+
+
+@pytest.mark.parametrize("decay", [0.0, 0.25])
+@pytest.mark.parametrize("bits", [32, 8])
+def test_infinite_parameters_stay(ngsgd, bits, decay):
+    """p (1 - lr decay) of an infinite p (a bias that masks) is p; its neighbours move as without it."""
+    import torch
+    a, b = (Bench(torch, ngsgd, [300], bits=bits, t=3, weight_decay=decay) for _ in range(2))
+    for at, value in ((5, float("inf")), (299, float("-inf"))):
+        b.params[0][at] = value
+    grads = a.gradients()
+    for opt in (a.opt, b.opt):
+        opt.step(grads, 0.5)
+    assert float(b.params[0][5]) == float("inf") and float(b.params[0][299]) == float("-inf")
+    others = [i for i in range(300) if i not in (5, 299)]
+    assert torch.equal(a.params[0][others], b.params[0][others])
