@@ -464,3 +464,35 @@ def test_infinite_parameters_stay(ngsgd, bits, decay):
     assert float(b.params[0][5]) == float("inf") and float(b.params[0][299]) == float("-inf")
     others = [i for i in range(300) if i not in (5, 299)]
     assert torch.equal(a.params[0][others], b.params[0][others])
+
+
+@pytest.mark.parametrize("betas", [(0.99999, 0.999995), (0.999995, 0.99999), (0.9999, 0.9999)])
+def test_betas_near_one(ngsgd, betas):
+    """Moments in fp32 fade by 1 - beta in the mean, though beta itself has no more than 24 bits there.
+
+    Tolerance, with c = (1 - beta) 2^23 the steps of the last bit by which a number of 1 fades: roundings are even over many elements (6 standard deviations
+    of u / sqrt(3 n)), but for the ends of the range of what fades, c to 2 c steps, which shift the mean by at most 1 / 8 of a step's c-th
+    part at either."""
+    import torch
+    n = 1 << 20
+    b = Bench(torch, ngsgd, [n], betas=betas, t=500)
+    _, (m0,), (v0,) = b.before()
+    b.opt.step([torch.zeros(n, device="cuda")], 1e-3)
+    _, (m1,), (v1,) = b.before()
+    for before, after, beta in ((m0, m1, betas[0]), (v0, v1, betas[1])):
+        part, c = 1 - beta, (1 - beta) * 2 ** 23
+        assert abs(np.mean((before - after) / before) - part) <= 6 * U / np.sqrt(3 * n) + part * 0.25 / c ** 2
+
+
+@pytest.mark.parametrize("betas", [(0.9, 0.999), (0.5, 0.5)])
+def test_infinite_moments_stay_infinite(ngsgd, betas):
+    """A v above what fp32 holds stays so, and its element (whose step is 0) where it is."""
+    import torch
+    p = torch.ones(4, device="cuda")
+    opt = ngsgd.AdamW([p], betas=betas)
+    opt.step([torch.tensor([1e30, 1.0, -1e30, 0.0], device="cuda")], 0.125)
+    for _ in range(2):
+        v = opt.state()[1]
+        assert v[[0, 2]].tolist() == [float("inf")] * 2 and bool(v[[1, 3]].isfinite().all())
+        assert p[[0, 2, 3]].tolist() == [1.0] * 3
+        opt.step([torch.zeros(4, device="cuda")], 0.125)
