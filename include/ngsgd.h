@@ -272,7 +272,8 @@ int ngsgd_adamw_step(ngsgd_adamw* h, const void* const* dev_grads, float lr, con
                      float grad_scale, const float* dev_grad_scale, void* hip_stream);
 
 /* The flat arrays: their length, and their addresses in the workspace (NULL for moments in 8 bits, or without fp32
- * copies).  Tensor k's elements start behind those of the tensors before it, each rounded up to a multiple of 256. */
+ * copies).  Tensor k's elements start behind those of the tensors before it, each rounded up to a multiple of 256.  What lies
+ * between the tensors is zero and no step changes it. */
 int ngsgd_adamw_arrays(const ngsgd_adamw* h, int64_t* elements, float** dev_m, float** dev_v, float** dev_master);
 
 /* The moments as values, to flat arrays in fp32 or bf16 (which holds those of 8-bit codes exactly, but for a v below
@@ -280,7 +281,7 @@ int ngsgd_adamw_arrays(const ngsgd_adamw* h, int64_t* elements, float** dev_m, f
 int ngsgd_adamw_get_state(const ngsgd_adamw* h, void* dev_m, void* dev_v, int32_t type, int64_t* dev_t,
                           void* hip_stream);
 
-/* Installs moments (flat, 16-byte aligned; NULL: zeros; in 8 bits rounded to the nearest code, which gives back what
+/* Installs moments (flat, zeros between the tensors, 16-byte aligned; NULL: zeros; in 8 bits rounded to the nearest code, which gives back what
  * ngsgd_adamw_get_state gave) and the step count t >= 0.  fp32 copies are taken from dev_master (flat), with the parameters
  * rounded from it, or with NULL from the parameters. */
 int ngsgd_adamw_set_state(ngsgd_adamw* h, const float* dev_m, const float* dev_v, const float* dev_master,

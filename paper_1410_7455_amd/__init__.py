@@ -528,7 +528,7 @@ class AdamW:
         return m, v
 
     def set_state(self, m, v, t, master=None, stream=None):
-        """Installs flat float32 moments (None: zeros) and the step count; the fp32 copies from `master` (flat), which is rounded to the
+        """Installs flat float32 moments (zeros between the tensors; None: zeros) and the step count; the fp32 copies from `master` (flat), which is rounded to the
         parameters too, or from the parameters."""
         import torch
         _current_device(self.device)

@@ -349,8 +349,17 @@ __global__ __launch_bounds__(kAdamThreads) void adamw_kernel(const AdamStep a) {
           m[e] = (float)m64[e];
           v[e] = (float)v64[e];
         }
-        odd |= __builtin_amdgcn_classf(m[e], kClassNotFinite) || !__builtin_amdgcn_classf(v[e], kClassZeroOrNormal);
       }
+      if (i0 + kAdamBlock > chunk.n) {   // (uniform) behind the tensor's end the moments stay zero, also where the factors are not finite
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (e < here) continue;
+          m[e] = v[e] = 0.f;
+          if constexpr (BITS == 8) m64[e] = v64[e] = 0.0;
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) odd |= __builtin_amdgcn_classf(m[e], kClassNotFinite) || !__builtin_amdgcn_classf(v[e], kClassZeroOrNormal);
       const bool plain = !any_lane(odd);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
@@ -372,7 +381,7 @@ __global__ __launch_bounds__(kAdamThreads) void adamw_kernel(const AdamStep a) {
       } else {
         store_codes(a.s, block, m64, r64, plain, false, dither_start(block * kAdamBlock + 4 * lane, scalars.t));
       }
-      if constexpr (MASTER) store4(p, master + i, 4);
+      if constexpr (MASTER) store4(p, master + i, here);
       store4(p, param + i, here);
     }
   }

@@ -496,3 +496,21 @@ def test_infinite_moments_stay_infinite(ngsgd, betas):
         assert v[[0, 2]].tolist() == [float("inf")] * 2 and bool(v[[1, 3]].isfinite().all())
         assert p[[0, 2, 3]].tolist() == [1.0] * 3
         opt.step([torch.zeros(4, device="cuda")], 0.125)
+
+
+@pytest.mark.parametrize("master", [False, True])
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("bad", ["epsilon", "lr", "scale"])
+def test_what_is_behind_a_tensor_stays_zero(ngsgd, bad, bits, master):
+    """The flat arrays' padding, whatever becomes of the elements."""
+    import torch
+    sizes = [1, 300, 256, 4097, 6]
+    dtype = "bfloat16" if master else "float32"
+    b = Bench(torch, ngsgd, sizes, dtype, dtype, bits=bits, master=master, weight_decay=0.1, **({"epsilon": 0.0} if bad == "epsilon" else {}))
+    infinite = torch.tensor([float("inf")], device="cuda")
+    for grads in (b.gradients(), [torch.zeros_like(p) for p in b.params]):
+        b.opt.step(grads, infinite if bad == "lr" else 1e-3, grad_scale=infinite if bad == "scale" else None)
+    flat = list(b.opt.state()) + list(b.opt.state(torch.bfloat16)) + ([b.opt.master] if master else [])
+    for a in flat:
+        for o, n in zip(b.opt.offsets, sizes):
+            assert bool((a[o + n:o + -(-n // 256) * 256] == 0).all())
