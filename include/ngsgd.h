@@ -267,7 +267,7 @@ int ngsgd_adamw_destroy(ngsgd_adamw* h);
  * elements share; p is updated from this step's moments before they are coded.  They are rounded down
  * after a share of a step has been added, frac(i A + t B) of the element's place i in the flat arrays and t (A, B = 0x9E3779B1,
  * 0x6A09E667 over 2^32, the upper 20 bits), so that over the steps changes much smaller than a code's step
- * add up.  An infinity or NaN makes its own element NaN, not its block. */
+ * add up.  An infinity or NaN makes its own element NaN, not its block; an m above 1.875 2^127 and a root above 1.875 2^63 are held as those. */
 int ngsgd_adamw_step(ngsgd_adamw* h, const void* const* dev_grads, float lr, const float* dev_lr,
                      float grad_scale, const float* dev_grad_scale, void* hip_stream);
 

@@ -24,13 +24,15 @@ def share(n, t, start=0):
     return (u >> np.uint64(12)).astype(np.float64) / 2.0 ** 20
 
 
-def _exponent(a, lowest):
-    """The least E, not below `lowest`, with 1.875 2^E >= every finite number of the block."""
+def _exponent(a, lowest, highest):
+    """The least E, not below `lowest`, with 1.875 2^E >= every finite number of the block; `highest` where that is highest + 1: the largest
+    moments of fp32 are held as the largest code that stands for a number of fp32."""
     top = np.max(np.where(np.isfinite(a), a, 0.0), initial=0.0)
     if top == 0.0:
         return lowest
     f, e = np.frexp(top)
-    return max(int(e) - 1 if 2.0 * f <= 1.875 else int(e), lowest)
+    E = max(int(e) - 1 if 2.0 * f <= 1.875 else int(e), lowest)
+    return highest if E == highest + 1 else E
 
 
 def _grid(a, shares):
@@ -45,7 +47,7 @@ def coded_m(m, shares=HALF, top_of=None):
     """The values that the codes of one block of m stand for.  `top_of`: the numbers that set the exponent, if others."""
     m = np.asarray(m, np.float64)
     a = np.abs(m)
-    E = _exponent(a if top_of is None else np.abs(top_of), 16 - 127)
+    E = _exponent(a if top_of is None else np.abs(top_of), 16 - 127, 127)
     least = 1.125 * 2.0 ** (E - 15)
     held = np.clip(_grid(a, shares), least, 1.875 * 2.0 ** E)
     held = np.where(a < least, np.where(a > shares * least, least, 0.0), held)
@@ -56,7 +58,7 @@ def coded_v(v, shares=HALF, top_of=None):
     """The values that the codes of one block of v stand for: v is held by its root."""
     with np.errstate(invalid="ignore"):
         r = np.sqrt(np.asarray(v, np.float64))
-        E = _exponent(r if top_of is None else np.sqrt(top_of), 32 - 127)
+        E = _exponent(r if top_of is None else np.sqrt(top_of), 32 - 127, 63)
     held = np.clip(_grid(r, shares), 1.25 * 2.0 ** (E - 31), 1.875 * 2.0 ** E)
     return np.where(np.isfinite(r), np.where(r > 0.0, held, 0.0) ** 2, np.nan)
 

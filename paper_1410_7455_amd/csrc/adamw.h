@@ -97,9 +97,12 @@ __device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
 }
 __device__ __forceinline__ bool any_lane(const bool b) { return __builtin_amdgcn_ballot_w64(b) != 0; }
 
-// E (biased as in fp32) of a block with this largest finite magnitude; not below what the least code can be written with.
-__device__ __forceinline__ uint32_t exponent_of(const uint32_t top, const uint32_t lowest) { return max((top + 0xFFFFFu) >> 23, lowest); }
-constexpr uint32_t kLowestM = 16, kLowestV = 32;
+// E (biased as in fp32) of a block with this largest finite magnitude; not below what the least code can be written with, and not above what keeps
+// the largest code, or its square, a finite number of fp32: what is above 1.875 2^127 (v: (1.875 2^63)^2) is held as that.
+__device__ __forceinline__ uint32_t exponent_of(const uint32_t top, const uint32_t lowest, const uint32_t highest) {
+  return max(min(top + 0xFFFFFu, highest << 23) >> 23, lowest);
+}
+constexpr uint32_t kLowestM = 16, kLowestV = 32, kHighestM = 127 + 127, kHighestV = 63 + 127;
 
 __device__ __forceinline__ int base_m(const uint32_t e) { return (int)(e + 1) * 8 - 128; }
 __device__ __forceinline__ int base_v(const uint32_t e) { return (int)(e + 1) * 8 - 255; }
@@ -223,7 +226,7 @@ __device__ __forceinline__ void store_codes(const AdamState& s, const int64_t bl
     }
     nan = any_lane(odd) ? 1u : 0u;
   }
-  const uint32_t me = exponent_of(wave_max_u32(mt), kLowestM), ve = exponent_of(wave_max_u32(rt), kLowestV);
+  const uint32_t me = exponent_of(wave_max_u32(mt), kLowestM, kHighestM), ve = exponent_of(wave_max_u32(rt), kLowestV, kHighestV);
   const int mb = base_m(me), vb = base_v(ve);
   // (a code's first number and the one above it: what rounds to the first in fp32 is not below it by more than that)
   const uint32_t m_least = ((uint32_t)(mb + 1) << 20) + 1, r_least = ((uint32_t)(vb + 1) << 20) + 1;

@@ -514,3 +514,24 @@ def test_what_is_behind_a_tensor_stays_zero(ngsgd, bad, bits, master):
     for a in flat:
         for o, n in zip(b.opt.offsets, sizes):
             assert bool((a[o + n:o + -(-n // 256) * 256] == 0).all())
+
+
+def test_codes_of_the_largest_numbers(ngsgd):
+    """What fp32 holds is held as a number, not as infinity, when it is installed and by the steps."""
+    import torch
+    top = float(torch.finfo(torch.float32).max)
+    m = np.zeros(512)
+    m[:5] = top, -top, 3.3e38, -3.19e38, 1e38
+    m[256:260] = 2.0 ** 127, 1.9 * 2.0 ** 126, 1.0, -2.0 ** 112
+    v = np.abs(m)
+    for betas in ((0.9, 0.999), (1 - 1e-9, 1 - 1e-9)):
+        opt = ngsgd.AdamW([torch.zeros(512, device="cuda")], state_bits=8, betas=betas)
+        opt.set_state(*(torch.from_numpy(a).float().cuda() for a in (m, v)), 100)
+        held = [f64(a) for a in opt.state()]
+        for got, which, a in zip(held, (oracle.coded_m, oracle.coded_v), (m, v)):
+            assert np.all(np.isfinite(got)) and np.array_equal(got, oracle.coded(which, a.astype(np.float32)))
+        for t in range(101, 109):
+            opt.step([torch.zeros(512, device="cuda")], 0.0)
+            for k, (which, beta) in enumerate(zip((oracle.coded_m, oracle.coded_v), betas)):
+                held[k] = oracle.coded(which, beta * held[k], t)
+                assert np.all(np.isfinite(held[k])) and np.array_equal(f64(opt.state()[k]), held[k])

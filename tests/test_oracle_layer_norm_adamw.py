@@ -86,3 +86,13 @@ def test_small_changes_add_up():
         near = adamw.coded_v(0.999 * near + 0.001 * 4.0)
     assert np.array_equal(near, np.full(256, 1.0))
     assert abs(v.mean() - 4.0) < 0.2   # the codes around the root 2 are an eighth and a quarter apart
+
+
+def test_codes_stand_for_numbers_of_fp32():
+    """The largest numbers that fp32 holds are held as numbers, whatever share of a step is added."""
+    top = float(np.finfo(np.float32).max)
+    for a in (np.array([top, 1.0, 0.0]), np.array([1.9 * 2.0 ** 126, 2.0 ** 126])):
+        for share in (0.0, 0.5, 1.0 - 2.0 ** -20):
+            m, v = adamw.coded_m(-a, share), adamw.coded_v(a, share)
+            assert np.all(np.abs(m) <= 1.875 * 2.0 ** 127) and np.all(v <= (1.875 * 2.0 ** 63) ** 2)
+            assert np.all(np.abs(m[:1] + a[0]) <= a[0] / 8) and np.all(np.abs(np.sqrt(v[:1]) - np.sqrt(a[0])) <= np.sqrt(a[0]) / 8)
