@@ -538,14 +538,15 @@ class AdamW:
         _check(self.lib.ngsgd_adamw_set_state(self.handle, _address(m), _address(v), _address(master), int(t), _raw_stream(stream, self.device, self.workspace, self._home)),
                "ngsgd_adamw_set_state")
 
-    def steps(self):
-        """The step count; waits for the stream."""
+    def steps(self, stream=None):
+        """The step count behind the calls on `stream` so far (None: the current one); waits for them."""
         import torch
         _current_device(self.device)
-        t = torch.empty(1, dtype=torch.int64, device=self.device)
-        _check(self.lib.ngsgd_adamw_get_state(self.handle, None, None, NGSGD_FLOAT32, t.data_ptr(), _raw_stream(None, self.device, self.workspace, self._home)),
-               "ngsgd_adamw_get_state")
-        return int(t.item())
+        with _allocate_on(stream):
+            t = torch.empty(1, dtype=torch.int64, device=self.device)
+            _check(self.lib.ngsgd_adamw_get_state(self.handle, None, None, NGSGD_FLOAT32, t.data_ptr(),
+                                                  _raw_stream(stream, self.device, self.workspace, self._home)), "ngsgd_adamw_get_state")
+            return int(t.item())
 
 
 class Network:

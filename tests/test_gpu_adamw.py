@@ -535,3 +535,22 @@ def test_codes_of_the_largest_numbers(ngsgd):
             for k, (which, beta) in enumerate(zip((oracle.coded_m, oracle.coded_v), betas)):
                 held[k] = oracle.coded(which, beta * held[k], t)
                 assert np.all(np.isfinite(held[k])) and np.array_equal(f64(opt.state()[k]), held[k])
+
+
+def test_steps_on_the_stream_that_steps(ngsgd):
+    import torch
+    big = torch.randn(4096, 4096, device="cuda")
+    opt = ngsgd.AdamW([torch.zeros(300, device="cuda")])
+    g = torch.ones(300, device="cuda")
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        for _ in range(30):          # some milliseconds before the steps' turn
+            big = big @ big * 1e-3
+    for _ in range(3):
+        opt.step([g], 1e-3, stream=s)
+    assert opt.steps(stream=s) == 3
+    with torch.cuda.stream(s):
+        opt.step([g], 1e-3)
+        assert opt.steps() == 4
+    torch.cuda.current_stream().wait_stream(s)
