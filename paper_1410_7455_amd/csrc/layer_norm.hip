@@ -16,6 +16,7 @@ constexpr int kMostColumns = 1 << 25;   // (a launch has less than 2^32 threads)
 // there are more than eight of them.
 constexpr int kWideGrid = 2048, kWideGroups = 512, kWideSums = 1 << 23;
 
+inline int64_t parts(const int64_t N, const int size) { return N / size + (N % size != 0); }   // (any N: N + size - 1 may not fit)
 inline int type_bytes(const int type) { return type == NGSGD_FLOAT32 ? 4 : 2; }
 inline bool known_type(const int type) { return type == NGSGD_FLOAT32 || type == NGSGD_BFLOAT16 || type == NGSGD_FLOAT16; }
 inline bool on_element(const void* p, const int type) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(type_bytes(type) - 1)) == 0; }
@@ -40,11 +41,11 @@ RowPlan row_plan(const int D, const bool backward) {
 // Groups of rows whose sums are formed on their own: the workgroups of the backward pass, about ten wavefronts to a compute unit.  (Their
 // sums are written and read once more: with 16 wavefronts to a unit 32768 x 4096 bf16 takes 165 us instead of 150, 16384 x 1024 29 instead of 25.)
 int backward_grid(const int64_t N, const RowPlan& p) {
-  return (int)std::min<int64_t>(256 * std::max(1, 640 / p.nt), std::max<int64_t>(1, (N + p.rows() - 1) / p.rows()));
+  return (int)std::min<int64_t>(256 * std::max(1, 640 / p.nt), std::max<int64_t>(1, parts(N, p.rows())));
 }
 int norm_groups(const int64_t N, const int D) {
   const RowPlan p = row_plan(D, true);
-  if (p.e == 0) return (int)std::min<int64_t>({kWideGroups, std::max(8, kWideSums / D), std::max<int64_t>(1, (N + 7) / 8)});
+  if (p.e == 0) return (int)std::min<int64_t>({kWideGroups, std::max(8, kWideSums / D), std::max<int64_t>(1, parts(N, 8))});
   // Few rows: one workgroup takes them and has the sums, without a second launch.  Four rounds are no slower than it: 64 x 128 fp32 5.6 us
   // instead of 6.1, 16 x 512 bf16 4.6 instead of 5.4, 4 x 4096 5.8 instead of 5.9 (eight rounds: 8 x 4096 8.9 instead of 6.0), and the host
   // saves 3 of 14 us.  With one row in hand at a time only one is: 4 x 16384 29 instead of 16.
@@ -52,7 +53,7 @@ int norm_groups(const int64_t N, const int D) {
   return backward_grid(N, p);
 }
 unsigned forward_grid(const int64_t N, const RowPlan& p) {
-  return (unsigned)std::min<int64_t>(256 * std::max(1, 1536 / p.nt), (N + p.rows() - 1) / p.rows());
+  return (unsigned)std::min<int64_t>(256 * std::max(1, 1536 / p.nt), parts(N, p.rows()));
 }
 
 // f(shape) for rows of this width

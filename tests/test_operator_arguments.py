@@ -182,3 +182,13 @@ def test_networks_with_layer_norm_or_adamw(lib):
     for call in (lambda: lib.ngsgd_get_norm(None, 0, None, None, None), lambda: lib.ngsgd_set_norm(None, 0, None, None, None),
                  lambda: lib.ngsgd_last_norm_gradient(None, 0, None, None, None), lambda: lib.ngsgd_set_adamw(None, 1.0, 0.9, 0.999, 1e-8, 0.0)):
         assert call() == ng.NGSGD_EINVAL
+
+
+def test_layernorm_workspace_of_any_count(lib):
+    """Up to the largest count that its type holds: never less than for fewer rows."""
+    n = c_size_t(0)
+    for dim in (5, 200, 1000, 5000, 16384, 20000):
+        last = 0
+        for rows in (10 ** 9, 2 ** 62, 2 ** 63 - 16, 2 ** 63 - 2, 2 ** 63 - 1):
+            assert lib.ngsgd_layernorm_workspace_bytes(rows, dim, byref(n)) == 0 and n.value >= last
+            last = n.value
