@@ -388,3 +388,53 @@ def test_refusals(ngsgd):
         ln.forward(torch.zeros(1, 64, device="cuda").expand(8, 64))      # rows that overlap
     with pytest.raises(ngsgd.NgsgdError):
         ln.backward(x, x, mean, mean, v, needs=(False, False, False))
+
+
+def check_large(torch, x, dy, w, b, out, grads, eps=1e-5):
+    """Some 90 rows (fewer of very wide ones) and the last ones; all of the sums over the rows, in 64 bits on the GPU."""
+    N, D = x.shape
+    count = min(90, max(3, (1 << 22) // D))
+    rows = sorted(set(range(0, N, -(-N // count))) | set(range(max(0, N - count // 3), N)))
+    check_forward(torch, x[rows], w, b, eps, *(t[rows] for t in out))
+    _, mean, rstd = out
+    check_backward(torch, dy[rows], x[rows], mean[rows], rstd[rows], w, grads[0][rows], None, None)
+    terms = x.double()
+    terms -= mean.double()[:, None]
+    terms *= rstd.double()[:, None]
+    for got in (grads[1], grads[2]):
+        d = dy.double()
+        if got is grads[1]:
+            d *= terms
+        want = d.sum(dim=0)
+        u = half_step(torch, got.dtype)
+        e = (N + 12) * U * d.abs_().sum(dim=0)
+        assert bool(((got.double() - want).abs() <= e * (1 + 2 * u) + u * want.abs() + tiny(torch, got.dtype)).all())
+
+
+@pytest.mark.parametrize("N,D", [(24584, 7), (24583, 24), (49159, 100), (12293, 200), (24577, 133), (6149, 300), (12297, 512), (6151, 600), (18439, 1001),
+                                 (8198, 100), (16411, 65), (4099, 250), (8195, 129), (4101, 1500), (8200, 2049), (2051, 16390), (4100, 16385),
+                                 (3400, 20000), (65, 1100003)])
+@pytest.mark.parametrize("types", [COMBOS[0], COMBOS[2]], ids="-".join)
+def test_more_rows_than_a_grid(ngsgd, N, D, types):
+    """A second and third round of rows, the last one not full, of every shape, forward (1536 wavefronts' grids) and backward (640); rows from memory in
+    more than 2048 workgroups, and as many groups of their sums as the workspace's bound leaves (3400 x 20000, 65 x 1100003)."""
+    import torch
+    dtype, wtype = (getattr(torch, t) for t in types)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(N + D)
+    x = torch.randn(N, D, generator=g, device="cuda")
+    x *= torch.rand(N, 1, generator=g, device="cuda") * 2.0 + 0.25
+    x += torch.randn(N, 1, generator=g, device="cuda")
+    x = x.to(dtype)
+    dy = torch.randn(N, D, generator=g, device="cuda").to(dtype)
+    w = (1.0 + 0.3 * torch.randn(D, generator=g, device="cuda")).to(wtype)
+    b = (0.3 * torch.randn(D, generator=g, device="cuda")).to(wtype)
+    ln = ngsgd.LayerNorm(N, D)
+    out = ln.forward(x, w, b)
+    grads = ln.backward(dy, x, out[1], out[2], w)
+    check_large(torch, x, dy, w, b, out, grads)
+    # in place, and with nothing but the sums, the same bits
+    d, y = dy.clone(), x.clone()
+    assert torch.equal(ln.forward(y, w, b, out=y)[0], out[0])
+    assert torch.equal(ln.backward(d, x, out[1], out[2], w, dx=d)[0], grads[0])
+    assert all(torch.equal(p, q) for p, q in zip(ln.backward(dy, x, out[1], out[2], w, needs=(False, True, True))[1:], grads[1:]))
