@@ -438,3 +438,36 @@ def test_more_rows_than_a_grid(ngsgd, N, D, types):
     assert torch.equal(ln.forward(y, w, b, out=y)[0], out[0])
     assert torch.equal(ln.backward(d, x, out[1], out[2], w, dx=d)[0], grads[0])
     assert all(torch.equal(p, q) for p, q in zip(ln.backward(dy, x, out[1], out[2], w, needs=(False, True, True))[1:], grads[1:]))
+
+
+def test_each_gradient_is_its_difference(ngsgd):
+    """As above with bounds near the kernels' own, entry by entry.  f = sum(dy y) is summed in 64 bits and only what moves is counted: a row
+    for an element of x, a column for one of w or b.
+    Rounding: 2 e / 2h with the error e of y as at the top; w and b leave xhat as it is, and y is off by u of |xhat w| and u of |y|.
+    Curvature: h^2 / 6 times the third derivative, which is 0 in w and b.  For x, |xhat| <= sqrt(D) gives |r'| <= r^2 D^(-1/2), |r''| <= 4 r^3 / D and
+    |r'''| <= 24 r^4 D^(-3/2), and so |xhat'''| <= 3 |r''| + |xhat r''' / r| <= 36 r^3 / D."""
+    import torch
+    N, D, h = 4, 12, 2.0 ** -8
+    rng = np.random.default_rng(77)
+    # rows of deviation near 1 and a mean below 1
+    x = torch.from_numpy(rng.standard_normal((N, D)) + rng.uniform(-1, 1, (N, 1))).float().cuda()
+    _, dy, w, b = inputs(torch, N, D, torch.float32, torch.float32)
+    ln, (y, mean, rstd), grads = both(torch, ngsgd, x, dy, w, b, 0.1)
+    Y, DY, W, X, r = np.abs(f64(y)), np.abs(f64(dy)), np.abs(f64(w)), f64(x), f64(rstd)
+    xhat = np.abs((X - f64(mean)[:, None]) * r[:, None])
+    K = D / 64 + 24
+    e_y = U * (W * (K * r * np.abs(X).mean(axis=1))[:, None] + W * xhat * (K + 12) + 4 * Y)
+    row = (DY * e_y).sum(axis=1) / h + h * h * 6 / D * r ** 3 * (DY * W).sum(axis=1)
+    column = (DY * 2 * U * (W * xhat + Y + h * (xhat + 1))).sum(axis=0) / h
+    bounds = np.repeat(row[:, None], D, axis=1), column, column
+    for at, (grad, bound) in enumerate(zip(grads, bounds)):
+        grad = f64(grad)
+        assert np.median(bound / np.abs(grad)) < 0.05       # (zeros, or another entry's, would not pass)
+        for i in np.ndindex(grad.shape):
+            moved = [[t.clone() for t in (x, w, b)] for _ in range(2)]
+            moved[0][at][i] += h
+            moved[1][at][i] -= h
+            up, down = (f64(ln.forward(*m)[0]) for m in moved)
+            width = float(moved[0][at][i].double() - moved[1][at][i].double())
+            # the gradients' own bounds, of some 40 u, are far below these
+            assert abs((f64(dy) * (up - down)).sum() / width - grad[i]) <= bound[i]
