@@ -554,3 +554,21 @@ def test_steps_on_the_stream_that_steps(ngsgd):
         opt.step([g], 1e-3)
         assert opt.steps() == 4
     torch.cuda.current_stream().wait_stream(s)
+
+
+@pytest.mark.parametrize("types", [("float32", "bfloat16"), ("bfloat16", "float32")], ids="-".join)
+def test_codes_are_those_of_the_definition(ngsgd, types):
+    """Every code of a million, and the same from run to run.  What is coded is known to 2^-44 of itself, and a border between codes is as near
+    to one element in 10^11."""
+    import torch
+    n, t = 1 << 20, 40
+    runs = [Bench(torch, ngsgd, [n], *types, bits=8, t=t) for _ in range(3)]
+    _, (m0,), (v0,) = runs[0].before()
+    grads = runs[0].gradients()
+    for b in runs:
+        b.opt.step(grads, 1e-3, grad_scale=0.375)
+    for b in runs[1:]:
+        assert torch.equal(b.params[0], runs[0].params[0]) and all(torch.equal(x, y) for x, y in zip(b.opt.state(), runs[0].opt.state()))
+    _, m, v = oracle.step(np.zeros(n), f64(grads[0]), m0, v0, t + 1, 1e-3, scale=0.375)
+    for got, which, a in zip(runs[0].opt.state(), (oracle.coded_m, oracle.coded_v), (m, v)):
+        assert np.array_equal(f64(got), oracle.coded(which, a, t + 1).astype(np.float32))
