@@ -204,7 +204,8 @@ int ngsgd_precondition_simple_static(float* dev_M, int32_t N, int32_t D, int32_t
  * Statistics and sums are in fp32, outputs are rounded once.  Leading dimensions count elements, at least D and otherwise free:
  * rows need no alignment beyond an element's (rows on multiples of 16 bytes are faster).  dev_y may be dev_x with
  * the same leading dimension; other overlaps are not allowed.  N may be 0.  Rows do not mix: an infinity or NaN
- * stays in its row.  D is at most 2^25.  epsilon is finite and not negative; with 0 a row of equal numbers gives NaN. */
+ * stays in its row.  D is at most 2^25.  epsilon is finite and not negative; with 0 a row of equal numbers gives NaN, or
+ * what the rounding of its mean leaves.  A variance above what fp32 holds is infinite: rstd is 0. */
 int ngsgd_layernorm_forward(const void* dev_x, int64_t ldx, int32_t type, const void* dev_weight,
                             const void* dev_bias, int32_t weight_type, int64_t N, int32_t D, float epsilon,
                             void* dev_y, int64_t ldy, float* dev_mean, float* dev_rstd, void* hip_stream);
@@ -262,12 +263,15 @@ int ngsgd_adamw_destroy(ngsgd_adamw* h);
  *   dev_lr, dev_grad_scale (optional, 1 float each) are multiplied to lr and grad_scale: a schedule or the
  *               factor of a clipped norm that only the device knows
  * The step count lives on the device, so a captured step counts on at each replay (with the gradients' addresses,
- * lr and grad_scale of its capture; the workspace has to be there as long as the graph).  Up to 448 tensors take one launch.
+ * lr and grad_scale of its capture; the workspace has to be there as long as the graph).  At most 16 pieces of work (4096 elements
+ * of a tensor, or its rest) in no more than 448 tensors take one launch; any other step takes one that counts it and one for every
+ * 448 tensors.  Moments are fp32's: a v above what fp32 holds is infinite, and its element stays where it is (in 8 bits: NaN).
  * Moments in 8 bits: m as a sign, 4 bits of exponent and 3 behind the point, sqrt(v) as 5 and 3 bits, below an exponent that 256
  * elements share; p is updated from this step's moments before they are coded.  They are rounded down
  * after a share of a step has been added, frac(i A + t B) of the element's place i in the flat arrays and t (A, B = 0x9E3779B1,
  * 0x6A09E667 over 2^32, the upper 20 bits), so that over the steps changes much smaller than a code's step
- * add up.  An infinity or NaN makes its own element NaN, not its block; an m above 1.875 2^127 and a root above 1.875 2^63 are held as those. */
+ * add up.  An infinity or NaN makes its own element NaN, not its block; an m above 1.875 2^127 and a root above 1.875 2^63 are
+ * held as those. */
 int ngsgd_adamw_step(ngsgd_adamw* h, const void* const* dev_grads, float lr, const float* dev_lr,
                      float grad_scale, const float* dev_grad_scale, void* hip_stream);
 
@@ -333,7 +337,8 @@ int ngsgd_set_norm(ngsgd_net* net, int32_t layer, const float* dev_weight, const
 /* Numbers of the AdamW step over the layer norms' parameters and, with the AdamW methods, the weight matrices: its
  * learning rate is `rate` times the step's, weight_decay is of the matrices (bias column included) only.  Defaults: rate 1,
  * beta1 0.9, beta2 0.999, epsilon 1e-8 (not 0), weight_decay 0.  Forgets the moments and synchronises the device.
- * NGSGD_EINVAL for a network without AdamW; so does ngsgd_step where rate * lr is above 1e18 or not a number. */
+ * A step captured before keeps the numbers of its capture.  NGSGD_EINVAL for a network without AdamW; so does ngsgd_step where
+ * rate * lr is above 1e18 or not a number. */
 int ngsgd_set_adamw(ngsgd_net* net, float rate, double beta1, double beta2, float epsilon, float weight_decay);
 
 /* Borrowed handle of a layer's preconditioner (side = NGSGD_SIDE_INPUT / NGSGD_SIDE_OUTPUT);

@@ -2,7 +2,7 @@
 //   forward:   y = xhat w + b,  xhat = (x - mean) rstd,  mean = sum x / D,  rstd = (sum (x - mean)^2 / D + eps)^(-1/2)
 //   backward:  g = dy w,  dx = rstd (g - sum g / D - xhat sum(g xhat) / D),  dw = sum over rows dy xhat,  db = sum over rows dy
 // Statistics, sums and gradients are held in fp32; the variance is summed from the differences to the mean, so that
-// a mean far from zero costs no digits.
+// a mean far from zero costs no more than the mean's own rounding.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -67,7 +67,7 @@ struct RowPart {
 #pragma unroll
     for (int i = 0; i < S::E / PER; ++i) asm("" : "+v"(v[i]));
   }
-  // What is behind the row's end keeps its value (nothing but the loads may write to v: it would wait for them).
+  // What is behind the row's end keeps its value (what else writes to v waits for the load).
   __device__ __forceinline__ void load(const T* p, const RowColumns<S>& cols) {
 #pragma unroll
     for (int k = 0; k < S::K; ++k) {
@@ -195,7 +195,9 @@ struct BackwardRow {
       const T* const p = static_cast<const T*>(a.dy) + r * a.lddy;
       x.load(static_cast<const T*>(a.x) + r * a.ldx, cols);
       dy.load(p, cols);
-      if constexpr (SLABS) {   // (fp32) in a fixed order
+      // (fp32) In a fixed order.  The sum waits for the slabs' loads here, before the row in hand is worked on: rows behind split products are not
+      // in flight beside it, as others are.
+      if constexpr (SLABS) {
         for (int k = 1; k < a.n_slabs; ++k) {
           RowPart<S, T> more;
           more.clear();
@@ -319,7 +321,8 @@ __global__ __launch_bounds__(S::NT) void layernorm_backward_kernel(const LayerNo
 }
 
 // ---- rows of any width, read from memory in every pass -------------------------------------------------
-// Bound by the passes' latencies, with two workgroups to a compute unit: 4096 x 20000 bf16 forward 143 us (2.3 TB/s), backward 267 us.
+// Bound by the passes' latencies: with the pieces in flight a thread takes 78 to 119 registers, so that one workgroup is on a compute unit and its waits
+// are not covered by another's work.  4096 x 20000 bf16 forward 143 us (2.3 TB/s), backward 267 us.
 constexpr int kWideThreads = 1024;
 
 // f(piece, its place, how many of its columns belong to the piece before) for a thread's pieces of a row, after `load` of AHEAD of them, which are
