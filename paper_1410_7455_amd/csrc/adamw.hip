@@ -29,10 +29,6 @@ namespace {
 constexpr int kAdamFewChunks = 512, kAdamCounting = 64;
 constexpr int64_t kAdamMostChunks = (1 << 24) - 1;   // (a launch has less than 2^32 threads)
 
-bool known_type(const int type) { return type == NGSGD_FLOAT32 || type == NGSGD_BFLOAT16 || type == NGSGD_FLOAT16; }
-int type_bytes(const int type) { return type == NGSGD_FLOAT32 ? 4 : 2; }
-bool on_element(const void* p, const int type) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(type_bytes(type) - 1)) == 0; }
-
 int check_config(const ngsgd_adamw_config* cfg) {
   if (cfg == nullptr || cfg->n_tensors < 1 || cfg->dev_params == nullptr || cfg->sizes == nullptr) return NGSGD_EINVAL;
   if (!known_type(cfg->param_type) || !known_type(cfg->grad_type)) return NGSGD_EINVAL;

@@ -1,4 +1,4 @@
-// What the host code of all sources shares: error handling, sizes, the workspace carver.
+// What the host code of all sources shares: error handling, sizes, element types, the workspace carver.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -28,6 +28,9 @@ inline thread_local int g_last_hip_error = 0;
 
 inline int pad32(int x) { return (x + 31) / 32 * 32; }
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
+inline bool known_type(int type) { return type == NGSGD_FLOAT32 || type == NGSGD_BFLOAT16 || type == NGSGD_FLOAT16; }
+inline int type_bytes(int type) { return type == NGSGD_FLOAT32 ? 4 : 2; }
+inline bool on_element(const void* p, int type) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(type_bytes(type) - 1)) == 0; }
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // Carves typed arrays out of a caller-provided device workspace; with base == nullptr it only sizes.

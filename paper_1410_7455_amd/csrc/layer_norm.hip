@@ -17,9 +17,6 @@ constexpr int kMostColumns = 1 << 25;   // (a launch has less than 2^32 threads)
 constexpr int kWideGrid = 2048, kWideGroups = 512, kWideSums = 1 << 23;
 
 inline int64_t parts(const int64_t N, const int size) { return N / size + (N % size != 0); }   // (any N: N + size - 1 may not fit)
-inline int type_bytes(const int type) { return type == NGSGD_FLOAT32 ? 4 : 2; }
-inline bool known_type(const int type) { return type == NGSGD_FLOAT32 || type == NGSGD_BFLOAT16 || type == NGSGD_FLOAT16; }
-inline bool on_element(const void* p, const int type) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(type_bytes(type) - 1)) == 0; }
 
 // The threads of a row by its width: as few wavefronts, or parts of one, as hold it with 8 columns a thread; 16 where that keeps it within a
 // wavefront (no barriers) and where a workgroup cannot be larger, and for the forward pass, which has registers to spare, in wide rows
