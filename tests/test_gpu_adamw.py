@@ -430,7 +430,7 @@ def test_small_decays_are_applied(ngsgd, bits, master, lr, decay):
 
     Tolerance for the mean of (p - want) / before: an element is rounded once, by at most u of itself, evenly over the elements (their
     steps differ by many times their last bit), so the mean has a standard deviation of u / sqrt(3 n), taken six times; the step, known to 16 u, has
-    a sign of its own in each element.  A factor 1 - lr decay rounded to fp32 would be off by up to u in all elements alike, 300 times that."""
+    a sign of its own in each element.  A factor 1 - lr decay rounded to fp32 would be off by up to u / 2 in all elements alike, 150 times that."""
     import torch
     n = 1 << 20
     b = Bench(torch, ngsgd, [n], *(("bfloat16", "bfloat16") if master else ()), bits=bits, master=master, t=500, weight_decay=decay)
