@@ -95,7 +95,6 @@ __device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
   const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
   return __builtin_amdgcn_readfirstlane(max((uint32_t)b[0], (uint32_t)b[1]));
 }
-__device__ __forceinline__ bool any_lane(const bool b) { return __builtin_amdgcn_ballot_w64(b) != 0; }
 
 // E (biased as in fp32) of a block with this largest finite magnitude; not below what the least code can be written with, and not above what keeps
 // the largest code, or its square, a finite number of fp32: what is above 1.875 2^127 (v: (1.875 2^63)^2) is held as that.

@@ -44,6 +44,8 @@ __device__ __forceinline__ float half32_add_f32(const float v) {
 }
 __device__ __forceinline__ float wave_sum_f32(const float v) { return half32_add_f32(half16_add_f32(row16_sum_f32(v))); }
 
+__device__ __forceinline__ bool any_lane(const bool b) { return __builtin_amdgcn_ballot_w64(b) != 0; }
+
 // Sums over a workgroup of up to 16 wavefronts at the price of one barrier: `red` is used in turn by parity, so that a wavefront that is
 // ahead writes into the other half.  A lane reads one wavefront's sums, and the 16 lanes of a row add them.
 constexpr int kMaxWaves = 16;

@@ -1,8 +1,8 @@
 // Layer norm and its gradients (gfx950, 64-lane wavefronts).
 //   forward:   y = xhat w + b,  xhat = (x - mean) rstd,  mean = sum x / D,  rstd = (sum (x - mean)^2 / D + eps)^(-1/2)
 //   backward:  g = dy w,  dx = rstd (g - sum g / D - xhat sum(g xhat) / D),  dw = sum over rows dy xhat,  db = sum over rows dy
-// Statistics, sums and gradients are held in fp32; the variance is summed from the differences to the mean, so that
-// a mean far from zero costs no more than the mean's own rounding.
+// Statistics, sums and gradients are held in fp32.  The differences to the mean give the variance and, summed themselves where the mean is far from
+// zero, what it is off by, which is taken off them: it costs no digits, and equal numbers give the bias (3000.1 1000 times: else 0.15 off).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -132,6 +132,15 @@ __device__ __forceinline__ float row_sum(float v, BlockScratch& red, const int p
   return v;
 }
 
+// A mean so many deviations from zero is off by enough of its last bits to show in xhat: such rows take one more sum, of their differences to it, by which
+// it is set right.  (For all rows it would cost 16-bit ones up to 18 %: 8192 x 5000 bf16 37 us instead of 31; this costs them nothing that can be measured.)
+__device__ __forceinline__ bool far_from_zero(const float mean, const float var, const float eps) { return mean * mean > 256.f * (var + eps); }
+// The variance about mean + shift, from that about mean.  (NaN stays.)
+__device__ __forceinline__ float variance_about(const float var, const float shift) {
+  const float v = fmaf(-shift, shift, var);
+  return v < 0.f ? 0.f : v;
+}
+
 // Bound by memory.
 template <typename T, typename W, typename S>
 __global__ __launch_bounds__(S::NT) void layernorm_forward_kernel(const LayerNormForward a) {
@@ -157,14 +166,27 @@ __global__ __launch_bounds__(S::NT) void layernorm_forward_kernel(const LayerNor
       s += cols.counts(e) ? x[e] : 0.f;
     }
     if (row + step < a.N) next.load(static_cast<const T*>(a.x) + (row + step) * a.ldx, cols);
-    const float mean = row_sum<S>(s, red, 0) / (float)a.D;
+    float mean = row_sum<S>(s, red, 0) / (float)a.D;
     float q = 0.f;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       x[e] -= mean;
       q += cols.counts(e) ? x[e] * x[e] : 0.f;
     }
-    const float rstd = 1.f / sqrtf(row_sum<S>(q, red, 1) / (float)a.D + a.eps);
+    float var = row_sum<S>(q, red, 1) / (float)a.D;
+    const bool far = far_from_zero(mean, var, a.eps);
+    if (any_lane(far)) {   // (all threads of a row have the same bits: uniform in the workgroup where it shares a row)
+      float d = 0.f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) d += cols.counts(e) ? x[e] : 0.f;
+      const float sum = row_sum<S>(d, red, 0), shift = far ? sum / (float)a.D : 0.f;   // (a row's result is its own, whoever shares the wavefront)
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[e] -= shift;
+      mean += shift;
+      var = variance_about(var, shift);
+      if constexpr (S::TPR == 0) __syncthreads();   // the next row's first sum takes the same half of `red`
+    }
+    const float rstd = 1.f / sqrtf(var + a.eps);
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       x[e] *= rstd;
@@ -321,7 +343,7 @@ __global__ __launch_bounds__(S::NT) void layernorm_backward_kernel(const LayerNo
 }
 
 // ---- rows of any width, read from memory in every pass -------------------------------------------------
-// Bound by the passes' latencies: with the pieces in flight a thread takes 78 to 119 registers, so that one workgroup is on a compute unit and its waits
+// Bound by the passes' latencies: with the pieces in flight a thread takes 78 to 121 registers, so that one workgroup is on a compute unit and its waits
 // are not covered by another's work.  4096 x 20000 bf16 forward 143 us (2.3 TB/s), backward 267 us.
 constexpr int kWideThreads = 1024;
 
@@ -386,7 +408,18 @@ __global__ __launch_bounds__(kWideThreads) void layernorm_forward_wide_kernel(co
         sq += j >= skip ? d * d : 0.f;
       }
     });
-    const float rstd = 1.f / sqrtf(block_sum_f32(sq, red, 1) / (float)a.D + a.eps);
+    float var = block_sum_f32(sq, red, 1) / (float)a.D, shift = 0.f;
+    if (any_lane(far_from_zero(mean, var, a.eps))) {   // (uniform in the workgroup)
+      float sum = 0.f;
+      for_pieces<Pack<T, V>, V>(a.D, load_x, [&](const Pack<T, V>& q, int, const int skip) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) sum += j >= skip ? to_float(q.v[j]) - mean : 0.f;
+      });
+      shift = block_sum_f32(sum, red, 0) / (float)a.D;
+      var = variance_about(var, shift);
+      __syncthreads();   // the next row's first sum takes the same half of `red`
+    }
+    const float rstd = 1.f / sqrtf(var + a.eps);
     for_pieces<Affine, V>(
         a.D,
         [&](Affine& q, const int at) {
@@ -398,7 +431,7 @@ __global__ __launch_bounds__(kWideThreads) void layernorm_forward_wide_kernel(co
           float v[V];
 #pragma unroll
           for (int j = 0; j < V; ++j) {
-            v[j] = (to_float(q.x.v[j]) - mean) * rstd;
+            v[j] = (to_float(q.x.v[j]) - mean - shift) * rstd;
             if (w != nullptr) v[j] *= to_float(q.w.v[j]);
             if (b != nullptr) v[j] += to_float(q.b.v[j]);
           }
@@ -406,7 +439,7 @@ __global__ __launch_bounds__(kWideThreads) void layernorm_forward_wide_kernel(co
         });
     for (int c = a.D + (int)threadIdx.x; c < a.pad_to; c += kWideThreads) y[c] = from_float<T>(c == a.D ? 1.f : 0.f);
     if (threadIdx.x == 0) {
-      if (a.mean != nullptr) a.mean[row] = mean;
+      if (a.mean != nullptr) a.mean[row] = mean + shift;
       if (a.rstd != nullptr) a.rstd[row] = rstd;
     }
   }

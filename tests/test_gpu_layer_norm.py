@@ -471,3 +471,68 @@ def test_each_gradient_is_its_difference(ngsgd):
             width = float(moved[0][at][i].double() - moved[1][at][i].double())
             # the gradients' own bounds, of some 40 u, are far below these
             assert abs((f64(dy) * (up - down)).sum() / width - grad[i]) <= bound[i]
+
+
+@pytest.mark.parametrize("D", [3, 6, 24, 200, 300, 1000, 1500, 4099, 9000, 16384, 20001])
+def test_rows_far_from_zero(ngsgd, D):
+    """Equal numbers give the bias, and rows of a deviation of 1e-2 around 3000 lose no more of their digits than rows around 0.
+
+    The first mean is off by delta, K u mean|x| at most.  The differences to it (u of each) are summed, which gives delta to (K + 2) u of their mean
+    magnitude, and it is taken off them (u of each).  The variance is the mean of their squares less delta^2: off by (2 K + 6) u of
+    variance + 2 delta^2.  The rest as at the top."""
+    import torch
+    N, K, eps = 5, D / 64 + 24, 1e-5
+    rng = np.random.default_rng(D)
+    x = torch.from_numpy(3000.0 + 1e-2 * rng.standard_normal((N, D)) + rng.standard_normal((N, 1))).float().cuda()
+    x[3] = 3000.1
+    x[4] = -0.7
+    _, _, w, b = inputs(torch, N, D, torch.float32, torch.float32)
+    y, mean, rstd = ngsgd.LayerNorm(N, D, eps).forward(x, w, b)
+    X, W = f64(x), np.abs(f64(w))
+    want, m, r = oracle.forward(X, f64(w), f64(b), eps)
+    d, m, r = np.abs(X - m[:, None]), m[:, None], r[:, None]
+    var, delta = (d * d).mean(axis=1, keepdims=True), K * U * np.abs(X).mean(axis=1, keepdims=True)
+    e_d = U * (d + delta) + (K + 2) * U * (d.mean(axis=1, keepdims=True) + delta) + U * d
+    e_r = (2 * K + 6) * U * (var + 2 * delta ** 2) / (2 * (var + eps)) + 4 * U
+    assert np.all(np.abs(f64(rstd)[:, None] - r) <= e_r * r)
+    assert np.all(np.abs(f64(mean)[:, None] - m) <= U * np.abs(m) + (K + 2) * U * (d.mean(axis=1, keepdims=True) + delta))
+    assert np.all(np.abs(f64(y) - want) <= W * (r * e_d + d * r * (e_r + 4 * U)) + 3 * U * np.abs(want))
+
+
+@pytest.mark.parametrize("D", [5, 200, 1000, 3000, 20000])
+def test_statistics_of_infinite_rows(ngsgd, D):
+    """The mean of a row with one infinity is that; of one with both it is NaN, as with a NaN.  A variance above what fp32 holds: rstd 0, y the bias."""
+    import torch
+    x = torch.randn(5, D, device="cuda")
+    x[0, 1], x[1, D - 1], x[3, 2] = float("inf"), float("-inf"), float("nan")
+    x[2, 0], x[2, D - 1] = float("inf"), float("-inf")
+    x[4, 0], x[4, D - 1] = 1e30, -1e30
+    w, b = torch.full((D,), 2.0, device="cuda"), torch.randn(D, device="cuda")
+    y, mean, rstd = ngsgd.LayerNorm(5, D).forward(x, w, b)
+    assert mean[:2].tolist() == [float("inf"), float("-inf")] and bool(mean[2:4].isnan().all()) and bool(mean[4].isfinite())
+    assert bool(y[:4].isnan().all()) and bool(rstd[:4].isnan().all())
+    assert float(rstd[4]) == 0.0 and torch.equal(y[4], b)
+
+
+@pytest.mark.parametrize("N,D", [(100, 5), (24600, 20), (50, 200), (6200, 600), (3000, 1500), (2100, 5000), (2100, 16400)])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_rows_far_from_zero_among_others(ngsgd, N, D, dtype):
+    """A row's numbers are its own: the same bits whether the rows beside it are far from zero or near, or there are none."""
+    import torch
+    g = torch.Generator(device="cuda")
+    g.manual_seed(N + D)
+    x = torch.randn(N, D, generator=g, device="cuda")
+    far = torch.rand(N, generator=g, device="cuda") < 0.3
+    x[far] += 64.0 * (1 + torch.arange(int(far.sum()), device="cuda") % 7)[:, None]
+    x[far.nonzero()[::5, 0]] = 100.5
+    x = x.to(getattr(torch, dtype))
+    b = torch.randn(D, generator=g, device="cuda").to(x.dtype)
+    ln = ngsgd.LayerNorm(N, D)
+    out = ln.forward(x, None, b)
+    for part in (far, ~far):
+        assert all(torch.equal(whole[part], alone) for whole, alone in zip(out, ln.forward(x[part], None, b)))
+    # equal numbers: what the first mean is off by, K u 100.5 at most, is taken off up to K + 3 u of itself
+    equal, K, B = far.nonzero()[::5, 0], D / 64 + 24, b.double()
+    bound = out[2][equal].double()[:, None] * (K * U * 100.5) * (K + 3) * U + (half_step(torch, x.dtype) + U) * B.abs()
+    assert bool(((out[0][equal].double() - B).abs() <= bound).all())
+    check_forward(torch, x[:64], None, b, 1e-5, *(t[:64] for t in out))
