@@ -205,7 +205,7 @@ int ngsgd_precondition_simple_static(float* dev_M, int32_t N, int32_t D, int32_t
  * rows need no alignment beyond an element's (rows on multiples of 16 bytes are faster).  dev_y may be dev_x with
  * the same leading dimension; other overlaps are not allowed.  N may be 0.  Rows do not mix: an infinity or NaN
  * stays in its row.  D is at most 2^25.  epsilon is finite and not negative; with 0 a row of equal numbers gives NaN, or
- * what the rounding of its mean leaves.  A variance above what fp32 holds is infinite: rstd is 0. */
+ * what rounding leaves of it.  A variance above what fp32 holds is infinite: rstd is 0. */
 int ngsgd_layernorm_forward(const void* dev_x, int64_t ldx, int32_t type, const void* dev_weight,
                             const void* dev_bias, int32_t weight_type, int64_t N, int32_t D, float epsilon,
                             void* dev_y, int64_t ldy, float* dev_mean, float* dev_rstd, void* hip_stream);
