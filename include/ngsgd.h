@@ -58,6 +58,9 @@ extern "C" {
 #define NGSGD_FLOAT32 0
 #define NGSGD_BFLOAT16 1
 #define NGSGD_FLOAT16 2
+/* Types of tokens and labels. */
+#define NGSGD_INT32 3
+#define NGSGD_INT64 4
 
 #define NGSGD_MAX_LAYERS 16
 #define NGSGD_MAX_RANK 96    /* the R x R update runs in one workgroup's LDS */
@@ -226,6 +229,75 @@ int ngsgd_layernorm_backward(const void* dev_dy, int64_t lddy, const void* dev_x
                              const float* dev_rstd, int64_t N, int32_t D, void* dev_dx, int64_t lddx,
                              void* dev_dweight, void* dev_dbias, void* dev_workspace, size_t workspace_bytes,
                              void* hip_stream);
+
+/* ---- embedding -------------------------------------------------------------------------------- */
+
+/* y_i = scale * table[token_i]: row token_i of a table of V rows of D numbers, for each of N tokens.
+ *   dev_tokens     N of index_type (NGSGD_INT32 or NGSGD_INT64), dense.  One outside [0, V) is padding: its y is zeros
+ *   table_type     NGSGD_FLOAT32, or `type`
+ *   type           of y (NGSGD_FLOAT32, NGSGD_BFLOAT16 or NGSGD_FLOAT16)
+ * The product is in fp32 and rounded once.  Leading dimensions as with layer norm: at least D, in elements, no alignment.  y
+ * and the table do not overlap.  N may be 0 (with V >= 1).  N and V are at most 2^30, D at most 2^25. */
+int ngsgd_embedding_forward(const void* dev_tokens, int32_t index_type, int64_t N, const void* dev_table, int64_t ldt,
+                            int32_t table_type, int64_t V, int32_t D, float scale, void* dev_y, int64_t ldy,
+                            int32_t type, void* hip_stream);
+
+/* Device workspace that ngsgd_embedding_backward needs for up to max_tokens tokens; it holds nothing between calls. */
+int ngsgd_embedding_workspace_bytes(int64_t max_tokens, int64_t V, int32_t D, size_t* out_bytes);
+
+/* The table's gradient for the derivative dy of a scalar by y (N x D, `type`):
+ *   dtable[v] = scale * sum of the dy_i with token_i = v          (V x D, table_type)
+ * and zeros in rows that no token names; with accumulate = 1 the sums are added to what dtable holds, and rows that no token
+ * names are neither read nor written (a table that is the last layer's weights too).  Tokens are sorted, and sums are in fp32 in an
+ * order that depends on the tokens and sizes alone: a call repeated gives the same bits.  Rounded once.
+ * dev_workspace is 256-byte aligned; calls that may run at the same time need one each. */
+int ngsgd_embedding_backward(const void* dev_dy, int64_t lddy, int32_t type, const void* dev_tokens, int32_t index_type,
+                             int64_t N, int64_t V, int32_t D, float scale, void* dev_dtable, int64_t lddt,
+                             int32_t table_type, int32_t accumulate, void* dev_workspace, size_t workspace_bytes,
+                             void* hip_stream);
+
+/* ---- cross-entropy ---------------------------------------------------------------------------- */
+
+/* loss_i = log sum_j exp(x_ij) - x_i,label_i  for each of N rows of V logits, and the gradient of
+ * scale * (sum of the losses):  dlogits_ij = scale * (softmax_ij - [j = label_i]).
+ *   dev_labels     N of index_type, dense.  A row whose label is outside [0, V) does not count: its loss and gradient are
+ *                  zeros, its logits are not read
+ *   dev_loss       (optional) N floats
+ *   dev_dlogits    (optional) N x V of `type`; may be dev_logits with the same leading dimension, other overlaps are not allowed
+ *   dev_scale      (optional, 1 float) is multiplied to scale: a loss scale, or one over a number of labels that only the device knows
+ * One of loss and gradient at least.  Statistics are in fp32, and what the label's own term leaves of the sum is kept apart from it, so that
+ * the loss and the label's gradient of a row that is as good as decided keep their digits; the gradient is rounded once.  A logit of -infinity is
+ * a class that is not there: its probability is 0, and as the label's it gives a loss of infinity.  A row with a NaN or
+ * +infinity, or with -infinity alone, has a loss and a gradient of NaN.  Sums are in an order that depends on the sizes alone.  Leading dimensions are
+ * at least V.  N and V are at most 2^30.  dev_workspace (256-byte aligned) holds nothing between calls; calls that may run at the
+ * same time need one each. */
+int ngsgd_cross_entropy_workspace_bytes(int64_t max_rows, int32_t V, size_t* out_bytes);
+int ngsgd_cross_entropy(const void* dev_logits, int64_t ld, int32_t type, const void* dev_labels, int32_t index_type,
+                        int64_t N, int32_t V, float* dev_loss, float scale, const float* dev_scale, void* dev_dlogits,
+                        int64_t ldd, void* dev_workspace, size_t workspace_bytes, void* hip_stream);
+
+/* ---- norm of all gradients, clipping ---------------------------------------------------------- */
+
+/* Device workspace of the two calls below for up to so many tensors of any sizes; it holds nothing between calls. */
+int ngsgd_grad_norm_workspace_bytes(int32_t n_tensors, size_t* out_bytes);
+
+/* norm = sqrt(sum of the squares of all elements of all tensors), and factor = max_norm / norm where norm > max_norm, else 1.
+ *   sizes, dev_grads (host arrays) elements and address of each tensor, dense, of `type`; one whose address is NULL or whose size is 0
+ *                    does not count
+ *   max_norm         not negative; infinity for the norm alone (factor 1)
+ *   dev_norm, dev_factor (1 float each, either may be NULL)
+ * Squares are summed in fp64, in an order that depends on the sizes alone, so no square overflows or vanishes; the norm is rounded to
+ * fp32 and the factor formed before that.  An infinity among the elements gives the norm infinity and the factor 0 (max_norm
+ * infinity: 1), a NaN gives NaN for both.  The factor is what ngsgd_adamw_step takes as dev_grad_scale.  At most 2^40 elements a tensor. */
+int ngsgd_grad_norm(int32_t n_tensors, const int64_t* sizes, const void* const* dev_grads, int32_t type, double max_norm,
+                    float* dev_norm, float* dev_factor, void* dev_workspace, size_t workspace_bytes, void* hip_stream);
+
+/* The same, and every element times the factor, rounded once, to dev_out[i] (of the same type and size; NULL only where dev_grads[i] is or the
+ * size is 0); dev_out NULL: in place, where with a factor of 1 nothing is read again or written.  dev_out[i] may be dev_grads[i]; other
+ * overlaps are not allowed. */
+int ngsgd_grad_clip(int32_t n_tensors, const int64_t* sizes, const void* const* dev_grads, int32_t type, double max_norm,
+                    void* const* dev_out, float* dev_norm, float* dev_factor, void* dev_workspace,
+                    size_t workspace_bytes, void* hip_stream);
 
 /* ---- AdamW over many tensors ------------------------------------------------------------------- */
 

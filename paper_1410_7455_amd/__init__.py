@@ -27,6 +27,8 @@ NGSGD_LAYERNORM = 16
 NGSGD_FLOAT32 = 0
 NGSGD_BFLOAT16 = 1
 NGSGD_FLOAT16 = 2
+NGSGD_INT32 = 3
+NGSGD_INT64 = 4
 NGSGD_SIDE_INPUT = 0
 NGSGD_SIDE_OUTPUT = 1
 NGSGD_MAX_RANK = 96
@@ -86,6 +88,19 @@ _SIGNATURES = {
     "ngsgd_layernorm_backward": (c_int, [c_void_p, c_int64, c_void_p, c_int64, c_int32, c_void_p, c_int32, c_void_p, c_void_p,
                                          c_int64, c_int32, c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_size_t,
                                          c_void_p]),
+    "ngsgd_embedding_forward": (c_int, [c_void_p, c_int32, c_int64, c_void_p, c_int64, c_int32, c_int64, c_int32, c_float,
+                                        c_void_p, c_int64, c_int32, c_void_p]),
+    "ngsgd_embedding_workspace_bytes": (c_int, [c_int64, c_int64, c_int32, POINTER(c_size_t)]),
+    "ngsgd_embedding_backward": (c_int, [c_void_p, c_int64, c_int32, c_void_p, c_int32, c_int64, c_int64, c_int32, c_float,
+                                         c_void_p, c_int64, c_int32, c_int32, c_void_p, c_size_t, c_void_p]),
+    "ngsgd_cross_entropy_workspace_bytes": (c_int, [c_int64, c_int32, POINTER(c_size_t)]),
+    "ngsgd_cross_entropy": (c_int, [c_void_p, c_int64, c_int32, c_void_p, c_int32, c_int64, c_int32, c_void_p, c_float, c_void_p,
+                                    c_void_p, c_int64, c_void_p, c_size_t, c_void_p]),
+    "ngsgd_grad_norm_workspace_bytes": (c_int, [c_int32, POINTER(c_size_t)]),
+    "ngsgd_grad_norm": (c_int, [c_int32, POINTER(c_int64), POINTER(c_void_p), c_int32, c_double, c_void_p, c_void_p, c_void_p,
+                                c_size_t, c_void_p]),
+    "ngsgd_grad_clip": (c_int, [c_int32, POINTER(c_int64), POINTER(c_void_p), c_int32, c_double, POINTER(c_void_p), c_void_p,
+                                c_void_p, c_void_p, c_size_t, c_void_p]),
     "ngsgd_adamw_workspace_bytes": (c_int, [POINTER(ngsgd_adamw_config), POINTER(c_size_t)]),
     "ngsgd_adamw_create": (c_int, [POINTER(ngsgd_adamw_config), c_void_p, c_size_t, POINTER(c_void_p)]),
     "ngsgd_adamw_destroy": (c_int, [c_void_p]),
@@ -412,6 +427,271 @@ class LayerNorm:
                                                  _raw_stream(stream, self.device, self.workspace, self._home)),
                "ngsgd_layernorm_backward")
         return dx, dweight, dbias
+
+
+def _index_type(t, name, device):
+    """NGSGD_INT32 / _INT64 of a dense tensor of tokens or labels on the device."""
+    if t.get_device() != device.index:
+        raise ValueError(f"{name} are on {t.device}, not on {device}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} are not dense")
+    if t.dtype == _torch.int64:
+        return NGSGD_INT64
+    if t.dtype == _torch.int32:
+        return NGSGD_INT32
+    raise ValueError(f"{name} are {t.dtype}: the types are int32 and int64")
+
+
+def _matrix(t, name, device, rows, columns):
+    """Leading dimension of a matrix on the device whose rows are dense; any distance apart."""
+    if t.get_device() != device.index:
+        raise ValueError(f"{name} is on {t.device}, not on {device}")
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != columns:
+        raise ValueError(f"{name} has the shape {tuple(t.shape)}, not {(rows, columns)}")
+    ld, inner = t.stride()
+    if inner != 1 and columns != 1:
+        raise ValueError(f"{name}: rows are not dense")
+    return ld if rows > 1 else columns
+
+
+class Embedding:
+    """ngsgd_embedding_forward / ngsgd_embedding_backward: rows of a table by tokens, times `scale`; the workspace of the gradient is
+    kept for reuse.
+
+    Tokens are int32 or int64, dense, of any shape, up to max_tokens; those outside [0, vocabulary) are padding.  The table is (vocabulary, dim),
+    its rows dense and any distance apart, float32 or of the type of the rows that are looked up (float32, bfloat16 or float16).  Calls on one object
+    are issued in order on one stream: the workspace is shared.  As with torch's own operators, tensors that are given to a
+    call on another stream than their own are the caller's to keep until it has run (torch.Tensor.record_stream)."""
+
+    def __init__(self, max_tokens, vocabulary, dim, scale=1.0):
+        import torch
+        self.lib = load_library()
+        self.max_tokens, self.vocabulary, self.dim, self.scale = max_tokens, vocabulary, dim, scale
+        nbytes = c_size_t(0)
+        _check(self.lib.ngsgd_embedding_workspace_bytes(max_tokens, vocabulary, dim, byref(nbytes)), "ngsgd_embedding_workspace_bytes")
+        self.workspace_bytes = nbytes.value
+        self.workspace = torch.empty(nbytes.value, dtype=torch.uint8, device="cuda")
+        self.device = self.workspace.device
+        self._home = _raw_stream(None, self.device)
+
+    def _tokens(self, tokens):
+        """(count, index type)"""
+        index = _index_type(tokens, "tokens", self.device)
+        n = tokens.numel()
+        if n > self.max_tokens:
+            raise ValueError(f"more than {self.max_tokens} tokens")
+        return n, index
+
+    def _rows(self, t, name, tokens, n):
+        """Leading dimension of tokens.shape + (dim,)."""
+        shape = t.shape
+        if len(shape) != 2 or tokens.dim() != 1:
+            if shape != tokens.shape + (self.dim,):
+                raise ValueError(f"{name} has the shape {tuple(shape)}, not {tuple(tokens.shape) + (self.dim,)}")
+            t = t.view(-1, self.dim) if n else t.new_empty(0, self.dim)
+        return _matrix(t, name, self.device, n, self.dim)
+
+    def _table_type(self, table_dtype, dtype):
+        if table_dtype != dtype and table_dtype != _torch.float32:
+            raise ValueError(f"a table of {table_dtype} for rows of {dtype}")
+        return _type_of(table_dtype)
+
+    def forward(self, tokens, table, dtype=None, out=None, stream=None):
+        """tokens.shape + (dim,) rows of `dtype` (the table's, if none is given), into `out` if given."""
+        _current_device(self.device)
+        n, index = self._tokens(tokens)
+        ldt = _matrix(table, "table", self.device, self.vocabulary, self.dim)
+        if out is not None:
+            if dtype is not None and dtype != out.dtype:
+                raise ValueError(f"out is {out.dtype}, not {dtype}")
+            dtype, ldy = out.dtype, self._rows(out, "out", tokens, n)
+        else:
+            dtype, ldy = table.dtype if dtype is None else dtype, self.dim
+        table_type = self._table_type(table.dtype, dtype)
+        type_ = _type_of(dtype)
+        if out is None:
+            with _allocate_on(stream):
+                out = _torch.empty((*tokens.shape, self.dim), dtype=dtype, device=self.device)
+        _check(self.lib.ngsgd_embedding_forward(tokens.data_ptr(), index, n, table.data_ptr(), ldt, table_type, self.vocabulary, self.dim,
+                                                self.scale, out.data_ptr(), ldy, type_, _raw_stream(stream, self.device)),
+               "ngsgd_embedding_forward")
+        return out
+
+    def backward(self, dy, tokens, dtype=None, dtable=None, accumulate=False, stream=None):
+        """The table's gradient (vocabulary, dim) of `dtype` (dy's, if none is given) for the derivative dy of the rows, into `dtable` if
+        given: in its place, or with `accumulate` added to it."""
+        _current_device(self.device)
+        n, index = self._tokens(tokens)
+        lddy = self._rows(dy, "dy", tokens, n)
+        if dtable is not None:
+            if dtype is not None and dtype != dtable.dtype:
+                raise ValueError(f"dtable is {dtable.dtype}, not {dtype}")
+            dtype, lddt = dtable.dtype, _matrix(dtable, "dtable", self.device, self.vocabulary, self.dim)
+        elif accumulate:
+            raise ValueError("nothing to add to: no dtable")
+        else:
+            dtype, lddt = dy.dtype if dtype is None else dtype, self.dim
+        table_type = self._table_type(dtype, dy.dtype)
+        type_ = _type_of(dy.dtype)
+        if dtable is None:
+            with _allocate_on(stream):
+                dtable = _torch.empty((self.vocabulary, self.dim), dtype=dtype, device=self.device)
+        _check(self.lib.ngsgd_embedding_backward(dy.data_ptr(), lddy, type_, tokens.data_ptr(), index, n, self.vocabulary, self.dim, self.scale,
+                                                 dtable.data_ptr(), lddt, table_type, 1 if accumulate else 0, self.workspace.data_ptr(),
+                                                 self.workspace_bytes, _raw_stream(stream, self.device, self.workspace, self._home)),
+               "ngsgd_embedding_backward")
+        return dtable
+
+
+class CrossEntropy:
+    """ngsgd_cross_entropy: the loss of each row of logits, and the gradient of their sum.
+
+    Logits are float32, bfloat16 or float16, (..., classes) with up to max_rows rows, which are dense and, as a matrix, may lie any
+    distance apart.  Labels are int32 or int64, dense, one for each row; a row whose label is outside [0, classes) does not count.  Calls
+    on one object are issued in order on one stream: the workspace is shared.  As with torch's own operators, tensors that are given to a call on
+    another stream than their own are the caller's to keep until it has run (torch.Tensor.record_stream)."""
+
+    def __init__(self, max_rows, classes):
+        import torch
+        self.lib = load_library()
+        self.max_rows, self.classes = max_rows, classes
+        nbytes = c_size_t(0)
+        _check(self.lib.ngsgd_cross_entropy_workspace_bytes(max_rows, classes, byref(nbytes)), "ngsgd_cross_entropy_workspace_bytes")
+        self.workspace_bytes = nbytes.value
+        self.workspace = torch.empty(nbytes.value, dtype=torch.uint8, device="cuda")
+        self.device = self.workspace.device
+        self._home = _raw_stream(None, self.device)
+
+    def _rows(self, t, name, labels, n):
+        shape = t.shape
+        if len(shape) != 2 or labels.dim() != 1:
+            if shape != labels.shape + (self.classes,):
+                raise ValueError(f"{name} has the shape {tuple(shape)}, not {tuple(labels.shape) + (self.classes,)}")
+            t = t.view(-1, self.classes) if n else t.new_empty(0, self.classes)
+        return _matrix(t, name, self.device, n, self.classes)
+
+    def _call(self, logits, labels, scale, loss, dlogits, wants_gradient, stream):
+        _current_device(self.device)
+        index = _index_type(labels, "labels", self.device)
+        n = labels.numel()
+        if n > self.max_rows:
+            raise ValueError(f"more than {self.max_rows} rows")
+        type_, ld, ldd = _type_of(logits.dtype), self._rows(logits, "logits", labels, n), self.classes
+        if loss is not None:
+            _check_dense(loss, "loss", self.device, _torch.float32, n)
+        if dlogits is not None:
+            if dlogits.dtype != logits.dtype:
+                raise ValueError(f"dlogits is {dlogits.dtype}, not {logits.dtype}")
+            ldd = self._rows(dlogits, "dlogits", labels, n)
+        dev_scale = None
+        if isinstance(scale, _torch.Tensor):
+            _check_dense(scale, "scale", self.device, _torch.float32, 1)
+            scale, dev_scale = 1.0, scale.data_ptr()
+        if loss is None or (wants_gradient and dlogits is None):
+            with _allocate_on(stream):
+                if loss is None:
+                    loss = _torch.empty(labels.shape, dtype=_torch.float32, device=self.device)
+                if wants_gradient and dlogits is None:
+                    dlogits = _torch.empty_like(logits, memory_format=_torch.contiguous_format)
+        _check(self.lib.ngsgd_cross_entropy(logits.data_ptr(), ld, type_, labels.data_ptr(), index, n, self.classes, loss.data_ptr(), scale,
+                                            dev_scale, _address(dlogits), ldd, self.workspace.data_ptr(), self.workspace_bytes,
+                                            _raw_stream(stream, self.device, self.workspace, self._home)), "ngsgd_cross_entropy")
+        return loss, dlogits
+
+    def forward(self, logits, labels, loss=None, stream=None):
+        """The loss of each row, float32 of the labels' shape, into `loss` if given."""
+        return self._call(logits, labels, 1.0, loss, None, False, stream)[0]
+
+    def gradient(self, logits, labels, scale=1.0, loss=None, dlogits=None, stream=None):
+        """(loss, dlogits): the loss of each row, and the gradient of `scale` times their sum, into `dlogits` if given (which may be the
+        logits).  scale is a number or a float32 tensor of one element on the device."""
+        return self._call(logits, labels, scale, loss, dlogits, True, stream)
+
+
+class GradientNorm:
+    """ngsgd_grad_norm / ngsgd_grad_clip: the norm of many gradients as one vector, and clipping, on the current device.
+
+    `like` are tensors of the gradients' sizes (the parameters, or the gradients themselves): only their sizes, device and type are taken.
+    grad_dtype is the gradients' type, `like`'s if none is given.  Calls on one object are issued in order on one stream: the
+    workspace is shared.  As with torch's own operators, tensors that are given to a call on another stream than their own are the
+    caller's to keep until it has run (torch.Tensor.record_stream)."""
+
+    def __init__(self, like, grad_dtype=None):
+        import torch
+        self.lib = load_library()
+        like = list(like)
+        n = len(like)
+        if n == 0:
+            raise ValueError("no tensors")
+        if not like[0].is_cuda:
+            raise ValueError("the tensors are not on the GPU")
+        self.device = like[0].device
+        _current_device(self.device)
+        for i, p in enumerate(like):
+            if p.device != self.device:
+                raise ValueError(f"tensor {i} is on {p.device}, not on {self.device}")
+        self.grad_dtype = like[0].dtype if grad_dtype is None else grad_dtype
+        self.type = _type_of(self.grad_dtype)
+        self.sizes = [p.numel() for p in like]
+        self._sizes = (c_int64 * n)(*self.sizes)
+        self._grads, self._out = (c_void_p * n)(), (c_void_p * n)()
+        nbytes = c_size_t(0)
+        _check(self.lib.ngsgd_grad_norm_workspace_bytes(n, byref(nbytes)), "ngsgd_grad_norm_workspace_bytes")
+        self.workspace_bytes = nbytes.value
+        self.workspace = torch.empty(nbytes.value, dtype=torch.uint8, device=self.device)
+        self._home = _raw_stream(None, self.device)
+
+    def _addresses(self, tensors, name, array):
+        dtype, index, sizes, addresses = self.grad_dtype, self.device.index, self.sizes, []
+        if len(tensors) != len(sizes):
+            raise ValueError(f"{len(tensors)} {name}s for {len(sizes)} tensors")
+        for t, size in zip(tensors, sizes):
+            if t is None or size == 0:
+                addresses.append(None)
+                continue
+            if t.dtype != dtype or t.numel() != size or t.get_device() != index or not t.is_contiguous():
+                raise ValueError(f"{name} {len(addresses)}: {t.dtype}, {t.numel()} elements on {t.device}, for {dtype}, {size} on "
+                                 f"{self.device}, dense")
+            addresses.append(t.data_ptr())
+        array[:] = addresses
+        return array
+
+    def _results(self, norm, factor, stream):
+        for name, t in (("norm", norm), ("factor", factor)):
+            if t is not None:
+                _check_dense(t, name, self.device, _torch.float32, 1)
+        if norm is None or factor is None:
+            with _allocate_on(stream):
+                if norm is None:
+                    norm = _torch.empty(1, dtype=_torch.float32, device=self.device)
+                if factor is None:
+                    factor = _torch.empty(1, dtype=_torch.float32, device=self.device)
+        return norm, factor
+
+    def norm(self, grads, max_norm=float("inf"), norm=None, factor=None, stream=None):
+        """(norm, factor), float32 tensors of one element: the norm of all gradients, and max_norm / norm where the norm is above max_norm, else 1, which
+        AdamW.step takes as grad_scale.  grads: a dense tensor of grad_dtype for each size, or None for one that does not count."""
+        _current_device(self.device)
+        grads = self._addresses(grads, "gradient", self._grads)
+        norm, factor = self._results(norm, factor, stream)
+        _check(self.lib.ngsgd_grad_norm(len(self.sizes), self._sizes, grads, self.type, max_norm, norm.data_ptr(), factor.data_ptr(),
+                                        self.workspace.data_ptr(), self.workspace_bytes,
+                                        _raw_stream(stream, self.device, self.workspace, self._home)), "ngsgd_grad_norm")
+        return norm, factor
+
+    def clip(self, grads, max_norm, out=None, norm=None, factor=None, stream=None):
+        """(norm, factor); every gradient is multiplied by the factor, in place or into `out` (a tensor for each gradient, which may be it)."""
+        _current_device(self.device)
+        if out is not None:
+            if any(g is not None and size != 0 and o is None for g, o, size in zip(grads, out, self.sizes)):
+                raise ValueError("out has no tensor for a gradient")
+            out = self._addresses(out, "output", self._out)
+        grads = self._addresses(grads, "gradient", self._grads)
+        norm, factor = self._results(norm, factor, stream)
+        _check(self.lib.ngsgd_grad_clip(len(self.sizes), self._sizes, grads, self.type, max_norm, out, norm.data_ptr(), factor.data_ptr(),
+                                        self.workspace.data_ptr(), self.workspace_bytes,
+                                        _raw_stream(stream, self.device, self.workspace, self._home)), "ngsgd_grad_clip")
+        return norm, factor
 
 
 class AdamW:

@@ -122,11 +122,6 @@ int check_types(const int type, const int weight_type, const int64_t N, const in
   if (!known_type(type) || !known_type(weight_type) || (weight_type != type && weight_type != NGSGD_FLOAT32)) return NGSGD_EINVAL;
   return N < 0 || D < 1 || D > kMostColumns ? NGSGD_EINVAL : NGSGD_OK;
 }
-// A matrix argument: present, rows that do not overlap, whole elements.
-bool good_matrix(const void* p, const int64_t ld, const int type, const int64_t N, const int32_t D) {
-  if (N == 0) return true;
-  return p != nullptr && on_element(p, type) && (ld >= D || N == 1) && ld >= 0 && ld <= INT64_MAX / 8 / N;
-}
 
 }  // namespace
 
