@@ -26,6 +26,11 @@ struct EmbeddingForward {
   int lanes;         // threads that share a row, a power of two
 };
 
+// A token that is sorted: its row of the table (V: padding, which goes last) and its place among the tokens.
+struct SortedToken {
+  uint32_t key, place;
+};
+
 struct EmbeddingBackward {
   const void* dy;
   int64_t lddy;
@@ -36,6 +41,12 @@ struct EmbeddingBackward {
   void* dtable;
   int64_t lddt;
   int accumulate;
+  const SortedToken* sorted;
+  float* parts;       // [chunks][2][pieces E]: sums that a chunk shares with the one before it, and the one behind it
+  int chunk;          // sorted tokens that are added one after the other, a power of two
+  int64_t chunks;
+  int pieces, lanes, slabs;   // pieces of E columns of a row; threads that share a chunk, each with one of them; groups of so many pieces
+  unsigned sum_groups;   // workgroups that add; those behind them write the rows that no token names
 };
 
 // -1 for padding
@@ -75,28 +86,342 @@ __global__ __launch_bounds__(kLookupThreads) void embedding_forward_kernel(const
   }
 }
 
-// A wavefront per row of the table and 64 columns: it looks through all tokens and adds the rows that name it.
-template <typename T, typename W, typename I>
-__global__ __launch_bounds__(256) void embedding_backward_kernel(const EmbeddingBackward a) {
-  const int lane = threadIdx.x & 63;
-  const int64_t v = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (v >= a.V) return;
-  for (int64_t c = (int64_t)blockIdx.y * 64 + lane; c - lane < a.D; c += (int64_t)gridDim.y * 64) {
-    float sum = 0.f;
-    bool named = false;
-    for (int64_t base = 0; base < a.N; base += 64) {
-      const bool here = base + lane < a.N && token_of(static_cast<const I*>(a.tokens), base + lane, a.V) == v;
-      uint64_t mask = __builtin_amdgcn_ballot_w64(here);
-      named |= mask != 0;
-      for (; mask != 0; mask &= mask - 1) {
-        const int64_t i = base + __builtin_ctzll(mask);
-        if (c < a.D) sum += to_float(static_cast<const T*>(a.dy)[i * a.lddy + c]);
+// ---- sorting ----------------------------------------------------------------------------------------------
+template <typename I>
+__device__ __forceinline__ uint32_t key_of(const I* tokens, const int64_t i, const int64_t V) {
+  const int64_t t = tokens[i];
+  return t >= 0 && t < V ? (uint32_t)t : (uint32_t)V;
+}
+
+// Few tokens: each one's rank is counted, sum_j [key_j < key_i or (key_j = key_i and j < i)].  A workgroup's 16 wavefronts share 64 tokens
+// and deal the others between them.
+constexpr int kRankThreads = 1024;
+template <typename I>
+__global__ __launch_bounds__(kRankThreads) void embedding_rank_kernel(const I* tokens, const int N, const int64_t V, SortedToken* sorted) {
+  __shared__ int counts[kRankThreads / 64][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = blockIdx.x * 64 + lane;
+  const uint32_t key = i < N ? key_of(tokens, i, V) : 0xffffffffu;
+  int count = 0;
+  for (int base = wave * 64; base < N; base += kRankThreads) {
+    const uint32_t other = base + lane < N ? key_of(tokens, base + lane, V) : 0xffffffffu;
+    const uint32_t limit = base < (int)blockIdx.x * 64 ? key + 1 : key;   // those in front go first among equals
+#pragma unroll 16
+    for (int k = 0; k < 64; ++k) count += (uint32_t)__builtin_amdgcn_readlane(other, k) < limit;
+    if (base == (int)blockIdx.x * 64) {
+#pragma unroll 16
+      for (int k = 0; k < 64; ++k) count += (uint32_t)__builtin_amdgcn_readlane(other, k) == key && k < lane;
+    }
+  }
+  counts[wave][lane] = count;
+  __syncthreads();
+  if (wave != 0 || i >= N) return;
+  int rank = 0;
+#pragma unroll
+  for (int k = 0; k < kRankThreads / 64; ++k) rank += counts[k][lane];
+  sorted[rank] = SortedToken{key, (uint32_t)i};
+}
+
+// More: a radix sort from the lowest digit, each pass stable.  A workgroup has a tile of tokens; counts[tile][digit].
+constexpr int kSortThreads = 256, kSortBits = 10, kSortBins = 1 << kSortBits;
+constexpr int kSortInline = 64;   // tiles up to which a workgroup adds up the counts in front of it itself
+
+struct EmbeddingSort {
+  const void* tokens;          // of the first pass
+  const SortedToken* in;       // of the others
+  SortedToken* out;
+  int64_t N, V;
+  uint32_t* counts;            // [tiles][bins]
+  uint32_t* totals;            // [bins], where there are more tiles than kSortInline
+  int tiles, tile;             // tokens of a tile, a multiple of kSortThreads
+  int shift, bins;             // of this pass's digit; a power of two
+};
+
+template <typename I, bool FIRST>
+__device__ __forceinline__ SortedToken sort_input(const EmbeddingSort& a, const int64_t i) {
+  if (FIRST) return SortedToken{key_of(static_cast<const I*>(a.tokens), i, a.V), (uint32_t)i};
+  return a.in[i];
+}
+
+template <typename I, bool FIRST>
+__global__ __launch_bounds__(kSortThreads) void embedding_count_kernel(const EmbeddingSort a) {
+  __shared__ uint32_t bins[kSortBins];
+  for (int d = threadIdx.x; d < a.bins; d += kSortThreads) bins[d] = 0;
+  __syncthreads();
+  const int64_t from = (int64_t)blockIdx.x * a.tile, to = min(from + a.tile, a.N);
+  for (int64_t i = from + threadIdx.x; i < to; i += kSortThreads) atomicAdd(&bins[sort_input<I, FIRST>(a, i).key >> a.shift & (a.bins - 1)], 1u);
+  __syncthreads();
+  for (int d = threadIdx.x; d < a.bins; d += kSortThreads) a.counts[(int64_t)blockIdx.x * a.bins + d] = bins[d];
+}
+
+// Many tiles: counts become those of the tiles in front.  A lane per digit; 16 wavefronts share the tiles.
+__global__ __launch_bounds__(1024) void embedding_scan_kernel(const EmbeddingSort a) {
+  __shared__ uint32_t sums[16][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, d = blockIdx.x * 64 + lane;
+  const int share = (a.tiles + 15) / 16, from = min(wave * share, a.tiles), to = min(from + share, a.tiles);
+  uint32_t sum = 0;
+  if (d < a.bins)
+    for (int t = from; t < to; ++t) sum += a.counts[(int64_t)t * a.bins + d];
+  sums[wave][lane] = sum;
+  __syncthreads();
+  uint32_t before = 0, total = 0;
+  for (int k = 0; k < 16; ++k) {
+    if (k < wave) before += sums[k][lane];
+    total += sums[k][lane];
+  }
+  if (d >= a.bins) return;
+  for (int t = from; t < to; ++t) {
+    uint32_t* const at = a.counts + (int64_t)t * a.bins + d;
+    const uint32_t here = *at;
+    *at = before;
+    before += here;
+  }
+  if (wave == 0) a.totals[d] = total;
+}
+
+// Places: digits in order, tiles in order within a digit, a tile's tokens in order within that.  A wavefront ranks 64 tokens at a time: lanes
+// with the same digit find each other by one ballot a bit.
+template <typename I, bool FIRST, int ROUNDS>
+__global__ __launch_bounds__(kSortThreads) void embedding_scatter_kernel(const EmbeddingSort a) {
+  constexpr int kWaves = kSortThreads / 64, kOwn = kSortBins / kSortThreads;
+  __shared__ uint32_t bins[kWaves][kSortBins];   // of each wavefront: its count, then where its next token with that digit goes
+  __shared__ uint32_t waves[kWaves];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  for (int d = threadIdx.x; d < kWaves * a.bins; d += kSortThreads) bins[d / a.bins][d & (a.bins - 1)] = 0;
+  __syncthreads();
+  // counts within the wavefronts, and each token's rank within its wavefront
+  const int64_t from = (int64_t)blockIdx.x * a.tile + (int64_t)wave * ROUNDS * 64;
+  SortedToken token[ROUNDS];
+  uint32_t rank[ROUNDS];
+#pragma unroll
+  for (int r = 0; r < ROUNDS; ++r) {
+    const int64_t i = from + r * 64 + lane;
+    if (i < a.N) token[r] = sort_input<I, FIRST>(a, i);
+  }
+#pragma unroll
+  for (int r = 0; r < ROUNDS; ++r) {
+    const bool here = from + r * 64 + lane < a.N;
+    const uint32_t digit = here ? token[r].key >> a.shift & (a.bins - 1) : 0;
+    uint64_t same = __builtin_amdgcn_ballot_w64(here);
+    for (int bit = 1; bit < a.bins; bit *= 2) {
+      const bool set = (digit & bit) != 0;
+      const uint64_t with = __builtin_amdgcn_ballot_w64(set);
+      same &= set ? with : ~with;
+    }
+    const uint32_t before = __builtin_amdgcn_mbcnt_hi((uint32_t)(same >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)same, 0));
+    if (here) rank[r] = bins[wave][digit] + before;
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    if (here && before == 0) bins[wave][digit] += (uint32_t)__builtin_popcountll(same);
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  }
+  __syncthreads();
+  // where each digit's tokens of this tile go: a thread has kOwn neighbouring digits
+  uint32_t total[kOwn], before[kOwn], sum = 0;
+#pragma unroll
+  for (int k = 0; k < kOwn; ++k) {
+    const int d = threadIdx.x * kOwn + k;
+    total[k] = before[k] = 0;
+    if (d >= a.bins) continue;
+    if (a.totals != nullptr) {
+      before[k] = a.counts[(int64_t)blockIdx.x * a.bins + d];
+      total[k] = a.totals[d];
+    }
+  }
+  if (a.totals == nullptr && threadIdx.x * kOwn < a.bins) {
+    for (int t = 0; t < a.tiles; ++t) {
+#pragma unroll
+      for (int k = 0; k < kOwn; ++k) {
+        if (threadIdx.x * kOwn + k >= a.bins) continue;
+        const uint32_t here = a.counts[(int64_t)t * a.bins + threadIdx.x * kOwn + k];
+        if (t < (int)blockIdx.x) before[k] += here;
+        total[k] += here;
       }
     }
-    if (c >= a.D || (a.accumulate && !named)) continue;
-    W* out = static_cast<W*>(a.dtable) + v * a.lddt + c;
-    *out = from_float<W>((a.accumulate ? to_float(*out) : 0.f) + a.scale * sum);
   }
+#pragma unroll
+  for (int k = 0; k < kOwn; ++k) sum += total[k];
+  uint32_t below = sum;   // of the digits up to this thread's, within the wavefront
+#pragma unroll
+  for (int k = 1; k < 64; k *= 2) {
+    const uint32_t o = __shfl_up(below, k);
+    if (lane >= k) below += o;
+  }
+  if (lane == 63) waves[wave] = below;
+  __syncthreads();
+  below -= sum;
+  for (int k = 0; k < wave; ++k) below += waves[k];
+#pragma unroll
+  for (int k = 0; k < kOwn; ++k) {
+    const int d = threadIdx.x * kOwn + k;
+    if (d >= a.bins) continue;
+    uint32_t at = below + before[k];
+    below += total[k];
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const uint32_t here = bins[w][d];
+      bins[w][d] = at;
+      at += here;
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int r = 0; r < ROUNDS; ++r)
+    if (from + r * 64 + lane < a.N) a.out[bins[wave][token[r].key >> a.shift & (a.bins - 1)] + rank[r]] = token[r];
+}
+
+// ---- sums --------------------------------------------------------------------------------------------------
+// A piece of a table's row: written, or added to what is there.  The last piece of a row is moved back to end with it; the columns that the piece before
+// has too are left to that one.
+template <typename W, int E>
+__device__ __forceinline__ void store_piece(const EmbeddingBackward& a, const uint32_t row, const int piece, const float (&sum)[E]) {
+  const int at = min(piece * E, a.D - E), skip = piece * E - at;
+  W* const out = static_cast<W*>(a.dtable) + row * a.lddt + at;
+  if (skip == 0) {
+    Pack<W, E> v;
+    if (a.accumulate) v = *reinterpret_cast<const Pack<W, E>*>(out);
+#pragma unroll
+    for (int j = 0; j < E; ++j) v.v[j] = from_float<W>((a.accumulate ? to_float(v.v[j]) : 0.f) + a.scale * sum[j]);
+    *reinterpret_cast<Pack<W, E>*>(out) = v;
+  } else {
+#pragma unroll
+    for (int j = 0; j < E; ++j)
+      if (j >= skip) out[j] = from_float<W>((a.accumulate ? to_float(out[j]) : 0.f) + a.scale * sum[j]);
+  }
+}
+
+constexpr int kSumThreads = 256, kSumAhead = 8;   // rows that a thread has in flight
+
+// The sums of a chunk of sorted tokens, of the columns of this thread's piece.  A token whose rows are all in the chunk is done; the first one's and the last
+// one's sums are parts if the chunks beside this one have rows of theirs.
+template <typename T, typename W, int E, bool WAVE>
+__device__ __forceinline__ void embedding_sum_chunk(const EmbeddingBackward& a, const int64_t chunk, const int piece) {
+  const int64_t from = chunk * a.chunk, to = min(from + a.chunk, a.N);
+  const int at = min(piece * E, a.D - E);
+  float sum[E];
+#pragma unroll
+  for (int j = 0; j < E; ++j) sum[j] = 0.f;
+  uint32_t key = a.sorted[from].key;
+  bool before = from > 0 && a.sorted[from - 1].key == key;   // the chunk in front has rows of this token
+  const auto finish = [&](const bool behind) {
+    if (piece >= a.pieces) return;
+    if (!before && !behind) {
+      store_piece<W, E>(a, key, piece, sum);
+    } else {
+      float* const part = a.parts + ((chunk * 2 + (before ? 0 : 1)) * a.pieces + piece) * E;
+#pragma unroll
+      for (int j = 0; j < E; ++j) part[j] = sum[j];
+    }
+  };
+  for (int64_t p = from; p < to; p += kSumAhead) {
+    SortedToken token[kSumAhead];
+    Pack<T, E> row[kSumAhead];
+#pragma unroll
+    for (int k = 0; k < kSumAhead; ++k) token[k] = a.sorted[min(p + k, to - 1)];
+#pragma unroll
+    for (int k = 0; k < kSumAhead; ++k)
+      if (token[k].key < (uint32_t)a.V && piece < a.pieces)
+        row[k] = *reinterpret_cast<const Pack<T, E>*>(static_cast<const T*>(a.dy) + token[k].place * a.lddy + at);
+#pragma unroll
+    for (int k = 0; k < kSumAhead; ++k) {
+      if (p + k >= to || token[k].key >= (uint32_t)a.V) continue;
+      if (token[k].key != key) {
+        finish(false);
+        key = token[k].key;
+        before = false;
+#pragma unroll
+        for (int j = 0; j < E; ++j) sum[j] = 0.f;
+      }
+#pragma unroll
+      for (int j = 0; j < E; ++j) sum[j] += to_float(row[k].v[j]);
+    }
+  }
+  if (key < (uint32_t)a.V) finish(to < a.N && a.sorted[to].key == key);
+}
+
+// First place among the sorted tokens whose key is not below this one.
+__device__ __forceinline__ int64_t lower_bound(const SortedToken* sorted, const int64_t N, const uint32_t key) {
+  int64_t low = 0, high = N;
+  while (low < high) {
+    const int64_t mid = (low + high) / 2;
+    if (sorted[mid].key < key) low = mid + 1; else high = mid;
+  }
+  return low;
+}
+
+// Zeros in those of 64 rows that no token names: a lane looks for a row, the wavefront writes it.
+template <typename W>
+__device__ __forceinline__ void embedding_clear_rows(const EmbeddingBackward& a, const int64_t first) {
+  constexpr int E = 16 / sizeof(W);
+  const int lane = threadIdx.x & 63;
+  const int64_t v = first + lane;
+  bool absent = false;
+  if (v < a.V) {
+    const int64_t at = lower_bound(a.sorted, a.N, (uint32_t)v);
+    absent = at == a.N || a.sorted[at].key != (uint32_t)v;
+  }
+  for (uint64_t rows = __builtin_amdgcn_ballot_w64(absent); rows != 0; rows &= rows - 1) {
+    W* const row = static_cast<W*>(a.dtable) + (first + __builtin_ctzll(rows)) * a.lddt;
+    Pack<W, E> zeros;
+#pragma unroll
+    for (int j = 0; j < E; ++j) zeros.v[j] = from_float<W>(0.f);
+    const int full = a.D / E;
+    for (int p = lane; p < full; p += 64) *reinterpret_cast<Pack<W, E>*>(row + p * E) = zeros;
+    if (full * E + lane < a.D) row[full * E + lane] = from_float<W>(0.f);
+  }
+}
+
+template <typename T, typename W, int E, bool WAVE>
+__global__ __launch_bounds__(kSumThreads) void embedding_sum_kernel(const EmbeddingBackward a) {
+  if (blockIdx.x >= a.sum_groups) {
+    const int64_t wave = (int64_t)(blockIdx.x - a.sum_groups) * (kSumThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (wave * 64 < a.V) embedding_clear_rows<W>(a, wave * 64);
+    return;
+  }
+  if (WAVE) {   // (uniform)
+    const int64_t unit = (int64_t)blockIdx.x * (kSumThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t chunk = unit / a.slabs;
+    if (chunk < a.chunks) embedding_sum_chunk<T, W, E, WAVE>(a, chunk, (int)(unit % a.slabs) * 64 + (threadIdx.x & 63));
+  } else {
+    const int64_t chunk = ((int64_t)blockIdx.x * kSumThreads + threadIdx.x) / a.lanes;
+    if (chunk < a.chunks) embedding_sum_chunk<T, W, E, WAVE>(a, chunk, threadIdx.x & (a.lanes - 1));
+  }
+}
+
+// A workgroup per chunk in which a token begins that goes on behind it, and 64 pieces: the parts of all chunks that have rows of it.
+constexpr int kJoinThreads = 256;
+template <typename W, int E>
+__global__ __launch_bounds__(kJoinThreads) void embedding_join_kernel(const EmbeddingBackward a) {
+  constexpr int kWaves = kJoinThreads / 64;
+  __shared__ float parts[kWaves][64][E];
+  const int64_t chunk = blockIdx.x / a.slabs, from = chunk * a.chunk, to = from + a.chunk;
+  if (to >= a.N) return;
+  const uint32_t key = a.sorted[to - 1].key;
+  if (key >= (uint32_t)a.V || a.sorted[to].key != key || (from > 0 && a.sorted[from - 1].key == key)) return;
+  const int64_t last = (lower_bound(a.sorted, a.N, key + 1) - 1) / a.chunk;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, piece = (int)(blockIdx.x % a.slabs) * 64 + lane;
+  float sum[E];
+#pragma unroll
+  for (int j = 0; j < E; ++j) sum[j] = 0.f;
+  if (piece < a.pieces) {
+#pragma unroll 4
+    for (int64_t c = chunk + wave; c <= last; c += kWaves) {
+      const Pack<float, E> part = *reinterpret_cast<const Pack<float, E>*>(a.parts + ((c * 2 + (c == chunk ? 1 : 0)) * a.pieces + piece) * E);
+#pragma unroll
+      for (int j = 0; j < E; ++j) sum[j] += part.v[j];
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < E; ++j) parts[wave][lane][j] = sum[j];
+  __syncthreads();
+  if (wave != 0 || piece >= a.pieces) return;
+#pragma unroll
+  for (int k = 1; k < kWaves; ++k)
+#pragma unroll
+    for (int j = 0; j < E; ++j) sum[j] += parts[k][lane][j];
+  store_piece<W, E>(a, key, piece, sum);
 }
 
 }  // namespace ngsgd

@@ -38,6 +38,112 @@ int launch_forward(EmbeddingForward a, hipStream_t s) {
   return NGSGD_OK;
 }
 
+// How a gradient is computed: all by sizes, so that a workspace for more tokens serves fewer.
+constexpr int64_t kRankMost = 8192;        // tokens whose ranks are counted
+constexpr int kSortSmallTile = 1024, kSortTile = 4096;
+constexpr int64_t kSumWaves = 8192;        // wavefronts that the sums are cut into, if there are as many
+constexpr int kLeastChunk = 16, kMostChunk = 512;
+
+int sort_tile(const int64_t N) { return N <= (int64_t)kSortSmallTile * kSortInline ? kSortSmallTile : kSortTile; }
+
+struct BackwardPlan {
+  int e, pieces, lanes, slabs, chunk;
+  int64_t chunks, most_chunks;             // most_chunks: of N tokens or fewer
+};
+BackwardPlan backward_plan(const int64_t N, const int D, const int element_bytes) {
+  BackwardPlan p;
+  p.e = D >= 16 / element_bytes ? 16 / element_bytes : 1;
+  p.pieces = (D + p.e - 1) / p.e;
+  for (p.lanes = 1; p.lanes < p.pieces && p.lanes < 64; p.lanes *= 2) {
+  }
+  p.slabs = (p.pieces + 63) / 64;
+  const int64_t units = std::max<int64_t>(1, kSumWaves * (64 / p.lanes) / p.slabs);   // chunks that fill the chip
+  for (p.chunk = kLeastChunk; p.chunk < kMostChunk && (N + p.chunk - 1) / p.chunk > units; p.chunk *= 2) {
+  }
+  p.chunks = (N + p.chunk - 1) / p.chunk;
+  p.most_chunks = std::max(std::min((N + kLeastChunk - 1) / kLeastChunk, units), (N + kMostChunk - 1) / kMostChunk);
+  return p;
+}
+
+struct Workspace {
+  SortedToken *sorted, *other;
+  uint32_t *counts, *totals;
+  float* parts;
+};
+Workspace layout(Carver& c, const int64_t N, const int D) {
+  Workspace w{};
+  size_t floats = 0;                       // of any type
+  for (const int bytes : {2, 4}) {
+    const BackwardPlan p = backward_plan(N, D, bytes);
+    floats = std::max(floats, (size_t)p.most_chunks * 2 * p.pieces * p.e);
+  }
+  w.sorted = c.take<SortedToken>(N);
+  w.parts = c.take<float>(floats);
+  if (N > kRankMost) {
+    const int64_t tiles = std::max((N + kSortTile - 1) / kSortTile, std::min<int64_t>((N + kSortSmallTile - 1) / kSortSmallTile, kSortInline));
+    w.other = c.take<SortedToken>(N);
+    w.counts = c.take<uint32_t>(tiles * kSortBins);
+    w.totals = c.take<uint32_t>(kSortBins);
+  }
+  return w;
+}
+
+template <typename I, bool FIRST>
+int sort_pass(const EmbeddingSort& a, hipStream_t s) {
+  hipLaunchKernelGGL((embedding_count_kernel<I, FIRST>), dim3((unsigned)a.tiles), dim3(kSortThreads), 0, s, a);
+  LAUNCH_CHECK();
+  if (a.totals != nullptr) {
+    hipLaunchKernelGGL(embedding_scan_kernel, dim3((unsigned)((a.bins + 63) / 64)), dim3(1024), 0, s, a);
+    LAUNCH_CHECK();
+  }
+  if (a.tile == kSortSmallTile)
+    hipLaunchKernelGGL((embedding_scatter_kernel<I, FIRST, kSortSmallTile / kSortThreads>), dim3((unsigned)a.tiles), dim3(kSortThreads), 0, s, a);
+  else
+    hipLaunchKernelGGL((embedding_scatter_kernel<I, FIRST, kSortTile / kSortThreads>), dim3((unsigned)a.tiles), dim3(kSortThreads), 0, s, a);
+  LAUNCH_CHECK();
+  return NGSGD_OK;
+}
+
+template <typename I>
+int sort_tokens(const void* tokens, const int64_t N, const int64_t V, const Workspace& w, hipStream_t s) {
+  if (N <= kRankMost) {
+    hipLaunchKernelGGL(embedding_rank_kernel<I>, dim3((unsigned)((N + 63) / 64)), dim3(kRankThreads), 0, s, static_cast<const I*>(tokens), (int)N, V,
+                       w.sorted);
+    LAUNCH_CHECK();
+    return NGSGD_OK;
+  }
+  int bits = 1;                            // of the keys 0 .. V
+  while ((int64_t)1 << bits <= V) ++bits;
+  const int passes = (bits + kSortBits - 1) / kSortBits, digit = (bits + passes - 1) / passes;
+  EmbeddingSort a{tokens, nullptr, nullptr, N, V, w.counts, nullptr, 0, sort_tile(N), 0, 1 << digit};
+  a.tiles = (int)((N + a.tile - 1) / a.tile);
+  if (a.tiles > kSortInline) a.totals = w.totals;
+  for (int pass = 0; pass < passes; ++pass, a.shift += digit) {
+    a.out = (passes - pass) % 2 == 1 ? w.sorted : w.other;   // the last one's
+    if (pass == 0)
+      NG_TRY((sort_pass<I, true>(a, s)));
+    else
+      NG_TRY((sort_pass<I, false>(a, s)));
+    a.in = a.out;
+  }
+  return NGSGD_OK;
+}
+
+template <typename T, typename W, int E>
+int launch_sums(const EmbeddingBackward& a, const unsigned grid, hipStream_t s) {
+  if (grid == 0) return NGSGD_OK;
+  if (a.lanes == 64)
+    hipLaunchKernelGGL((embedding_sum_kernel<T, W, E, true>), dim3(grid), dim3(kSumThreads), 0, s, a);
+  else
+    hipLaunchKernelGGL((embedding_sum_kernel<T, W, E, false>), dim3(grid), dim3(kSumThreads), 0, s, a);
+  LAUNCH_CHECK();
+  if (a.chunks > 1) {
+    hipLaunchKernelGGL((embedding_join_kernel<W, E>), dim3((unsigned)(a.chunks * a.slabs)), dim3(kJoinThreads), 0, s, a);
+    LAUNCH_CHECK();
+  }
+  return NGSGD_OK;
+}
+
 }  // namespace
 
 extern "C" int ngsgd_embedding_forward(const void* dev_tokens, int32_t index_type, int64_t N, const void* dev_table, int64_t ldt, int32_t table_type,
@@ -58,7 +164,9 @@ extern "C" int ngsgd_embedding_forward(const void* dev_tokens, int32_t index_typ
 
 extern "C" int ngsgd_embedding_workspace_bytes(int64_t max_tokens, int64_t V, int32_t D, size_t* out_bytes) {
   if (out_bytes == nullptr || max_tokens < 0 || max_tokens > kMostRows || V < 1 || V > kMostRows || D < 1 || D > kMostColumns) return NGSGD_EINVAL;
-  *out_bytes = 256;
+  Carver c(nullptr);
+  (void)layout(c, max_tokens, D);
+  *out_bytes = align_up(std::max<size_t>(c.off, 1), 256);
   return NGSGD_OK;
 }
 
@@ -72,11 +180,18 @@ extern "C" int ngsgd_embedding_backward(const void* dev_dy, int64_t lddy, int32_
   size_t need = 0;
   NG_TRY(ngsgd_embedding_workspace_bytes(N, V, D, &need));
   NG_TRY(check_workspace(dev_workspace, workspace_bytes, need));
-  const EmbeddingBackward a{dev_dy, lddy, dev_tokens, N, V, D, scale, dev_dtable, lddt, accumulate};
-  return with_types(type, table_type, index_type, [&](auto t, auto w, auto i) {
-    const dim3 grid((unsigned)((V + 3) / 4), (unsigned)std::min(D / 64 + 1, 64));
-    hipLaunchKernelGGL((embedding_backward_kernel<decltype(t), decltype(w), decltype(i)>), grid, dim3(256), 0, static_cast<hipStream_t>(hip_stream), a);
-    LAUNCH_CHECK();
-    return NGSGD_OK;
+  const BackwardPlan p = backward_plan(N, D, type_bytes(type));
+  if (p.chunks * p.slabs >= (int64_t)1 << 24) return NGSGD_EINVAL;   // a launch has less than 2^32 threads (no memory holds such rows)
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  Carver c(dev_workspace);
+  const Workspace w = layout(c, N, D);
+  if (N > 0) NG_TRY(index_type == NGSGD_INT32 ? sort_tokens<int32_t>(dev_tokens, N, V, w, s) : sort_tokens<int64_t>(dev_tokens, N, V, w, s));
+  EmbeddingBackward a{dev_dy, lddy, dev_tokens, N, V, D, scale, dev_dtable, lddt, accumulate, w.sorted, w.parts, p.chunk, p.chunks, p.pieces, p.lanes, p.slabs, 0};
+  a.sum_groups = (unsigned)((p.chunks * p.slabs * p.lanes + kSumThreads - 1) / kSumThreads);
+  const unsigned grid = a.sum_groups + (accumulate ? 0u : (unsigned)((V + kSumThreads - 1) / kSumThreads));
+  return with_types(type, table_type, NGSGD_INT32, [&](auto t, auto wt, auto) {
+    using T = decltype(t);
+    using W = decltype(wt);
+    return p.e == 1 ? launch_sums<T, W, 1>(a, grid, s) : launch_sums<T, W, 16 / sizeof(T)>(a, grid, s);
   });
 }
