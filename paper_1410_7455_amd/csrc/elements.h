@@ -16,11 +16,33 @@ struct __attribute__((packed, aligned(sizeof(T)))) Pack {
   T v[V];
 };
 
+// A store of 16 bytes as one, on any element's boundary: of zeros, and where another branch stores some of its elements, the compiler otherwise
+// makes several.
+typedef uint32_t U32x4 __attribute__((ext_vector_type(4)));
+typedef U32x4 U32x4On4 __attribute__((aligned(4)));
+typedef U32x4 U32x4On2 __attribute__((aligned(2)));
+template <typename T, int V>
+__device__ __forceinline__ void store_pack(T* p, const Pack<T, V>& v) {
+  if constexpr (sizeof(v) != 16)
+    *reinterpret_cast<Pack<T, V>*>(p) = v;
+  else if constexpr (sizeof(T) == 2)
+    *reinterpret_cast<U32x4On2*>(p) = __builtin_bit_cast(U32x4, v);
+  else
+    *reinterpret_cast<U32x4On4*>(p) = __builtin_bit_cast(U32x4, v);
+}
+
 // Arithmetic is in fp32.  A result is rounded once, to the nearest value of its type (ties to even), as it is stored.
 template <typename T>
 __device__ __forceinline__ float to_float(const T x) { return static_cast<float>(x); }
 template <typename T>
 __device__ __forceinline__ T from_float(const float x) { return static_cast<T>(x); }
+
+// A number in fp32 that the compiler does not merge with the conversion behind it: a product that is rounded to 16 bits in one instruction, without the
+// step over fp32, may differ by a step from one that is not, and it does so for some of a thread's elements only.
+__device__ __forceinline__ float as_f32(float x) {
+  asm("" : "+v"(x));
+  return x;
+}
 
 // Sum over the 64 lanes, to all of them: through the vector ALU's cross-lane path within rows of 16 lanes, then across them.
 template <int CTRL>

@@ -46,7 +46,8 @@ struct EmbeddingBackward {
   int chunk;          // sorted tokens that are added one after the other, a power of two
   int64_t chunks;
   int pieces, lanes, slabs;   // pieces of E columns of a row; threads that share a chunk, each with one of them; groups of so many pieces
-  unsigned sum_groups;   // workgroups that add; those behind them write the rows that no token names
+  unsigned sum_groups;   // workgroups that add; those behind them write the rows that no token names,
+  int clear_rows;        // so many rows (at most 64) to a wavefront
 };
 
 // -1 for padding
@@ -80,36 +81,45 @@ __global__ __launch_bounds__(kLookupThreads) void embedding_forward_kernel(const
       if (token[k] == -2) continue;
       Pack<T, E> y;
 #pragma unroll
-      for (int j = 0; j < E; ++j) y.v[j] = from_float<T>(token[k] >= 0 ? a.scale * to_float(w[k].v[j]) : 0.f);
-      *reinterpret_cast<Pack<T, E>*>(static_cast<T*>(a.y) + (first + k * per_round) * a.ldy + at) = y;
+      for (int j = 0; j < E; ++j) y.v[j] = from_float<T>(token[k] >= 0 ? as_f32(a.scale * to_float(w[k].v[j])) : 0.f);
+      store_pack(static_cast<T*>(a.y) + (first + k * per_round) * a.ldy + at, y);
     }
   }
 }
 
 // ---- sorting ----------------------------------------------------------------------------------------------
 template <typename I>
-__device__ __forceinline__ uint32_t key_of(const I* tokens, const int64_t i, const int64_t V) {
-  const int64_t t = tokens[i];
-  return t >= 0 && t < V ? (uint32_t)t : (uint32_t)V;
-}
+__device__ __forceinline__ uint32_t key_of(const I t, const int64_t V) { return (uint64_t)(int64_t)t < (uint64_t)V ? (uint32_t)t : (uint32_t)V; }
 
-// Few tokens: each one's rank is counted, sum_j [key_j < key_i or (key_j = key_i and j < i)].  A workgroup's 16 wavefronts share 64 tokens
-// and deal the others between them.
-constexpr int kRankThreads = 1024;
+// Few tokens: each one's rank is counted, sum_j [key_j < key_i or (key_j = key_i and j < i)].  A workgroup's 16 wavefronts share 64 tokens and deal the
+// others between them, 64 at a time.  Their keys come from LDS, four with one read that all lanes share: a wavefront's own copy, without a barrier.
+constexpr int kRankThreads = 1024, kRankRounds = 8, kRankMost = kRankThreads * kRankRounds;   // tokens
 template <typename I>
 __global__ __launch_bounds__(kRankThreads) void embedding_rank_kernel(const I* tokens, const int N, const int64_t V, SortedToken* sorted) {
+  __shared__ U32x4 keys[kRankThreads / 64][kRankRounds][16];
   __shared__ int counts[kRankThreads / 64][64];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = blockIdx.x * 64 + lane;
-  const uint32_t key = i < N ? key_of(tokens, i, V) : 0xffffffffu;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), first = blockIdx.x * 64, i = first + lane;
+  I others[kRankRounds];
+  const I own = tokens[min(i, N - 1)];
+#pragma unroll
+  for (int r = 0; r < kRankRounds; ++r) others[r] = tokens[min(r * kRankThreads + (int)threadIdx.x, N - 1)];
+  const uint32_t key = key_of(own, V);
+#pragma unroll
+  for (int r = 0; r < kRankRounds; ++r)
+    reinterpret_cast<uint32_t*>(keys[wave][r])[lane] = r * kRankThreads + (int)threadIdx.x < N ? key_of(others[r], V) : 0xffffffffu;
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
   int count = 0;
-  for (int base = wave * 64; base < N; base += kRankThreads) {
-    const uint32_t other = base + lane < N ? key_of(tokens, base + lane, V) : 0xffffffffu;
-    const uint32_t limit = base < (int)blockIdx.x * 64 ? key + 1 : key;   // those in front go first among equals
-#pragma unroll 16
-    for (int k = 0; k < 64; ++k) count += (uint32_t)__builtin_amdgcn_readlane(other, k) < limit;
-    if (base == (int)blockIdx.x * 64) {
-#pragma unroll 16
-      for (int k = 0; k < 64; ++k) count += (uint32_t)__builtin_amdgcn_readlane(other, k) == key && k < lane;
+  for (int r = 0, base = wave * 64; base < N; ++r, base += kRankThreads) {
+    const uint32_t limit = base < first ? key + 1 : key;   // those in front go first among equals
+#pragma unroll 4
+    for (int k = 0; k < 16; ++k) {
+      const U32x4 other = keys[wave][r][k];
+      count += (other.x < limit) + (other.y < limit) + (other.z < limit) + (other.w < limit);
+    }
+    if (base == first) {
+      for (int k = 0; k < 64; ++k) count += reinterpret_cast<const uint32_t*>(keys[wave][r])[k] == key && k < lane;
     }
   }
   counts[wave][lane] = count;
@@ -121,8 +131,8 @@ __global__ __launch_bounds__(kRankThreads) void embedding_rank_kernel(const I* t
   sorted[rank] = SortedToken{key, (uint32_t)i};
 }
 
-// More: a radix sort from the lowest digit, each pass stable.  A workgroup has a tile of tokens; counts[tile][digit].
-constexpr int kSortThreads = 256, kSortBits = 10, kSortBins = 1 << kSortBits;
+// More: a radix sort from the lowest digit, each pass stable.  A workgroup has a tile of kSortRounds tokens a thread; counts[tile][digit].
+constexpr int kSortBits = 10, kSortBins = 1 << kSortBits, kSortRounds = 4;
 constexpr int kSortInline = 64;   // tiles up to which a workgroup adds up the counts in front of it itself
 
 struct EmbeddingSort {
@@ -132,25 +142,30 @@ struct EmbeddingSort {
   int64_t N, V;
   uint32_t* counts;            // [tiles][bins]
   uint32_t* totals;            // [bins], where there are more tiles than kSortInline
-  int tiles, tile;             // tokens of a tile, a multiple of kSortThreads
-  int shift, bins;             // of this pass's digit; a power of two
+  int tiles;
+  int shift, bins;             // of this pass's digit; a power of two, at least 4
 };
 
 template <typename I, bool FIRST>
 __device__ __forceinline__ SortedToken sort_input(const EmbeddingSort& a, const int64_t i) {
-  if (FIRST) return SortedToken{key_of(static_cast<const I*>(a.tokens), i, a.V), (uint32_t)i};
+  if (FIRST) return SortedToken{key_of(static_cast<const I*>(a.tokens)[i], a.V), (uint32_t)i};
   return a.in[i];
 }
 
-template <typename I, bool FIRST>
-__global__ __launch_bounds__(kSortThreads) void embedding_count_kernel(const EmbeddingSort a) {
+template <typename I, bool FIRST, int THREADS>
+__global__ __launch_bounds__(THREADS) void embedding_count_kernel(const EmbeddingSort a) {
   __shared__ uint32_t bins[kSortBins];
-  for (int d = threadIdx.x; d < a.bins; d += kSortThreads) bins[d] = 0;
+  const int64_t from = (int64_t)blockIdx.x * THREADS * kSortRounds + threadIdx.x;
+  uint32_t key[kSortRounds];
+#pragma unroll
+  for (int r = 0; r < kSortRounds; ++r) key[r] = sort_input<I, FIRST>(a, min(from + r * THREADS, a.N - 1)).key;
+  for (int d = threadIdx.x; d < a.bins; d += THREADS) bins[d] = 0;
   __syncthreads();
-  const int64_t from = (int64_t)blockIdx.x * a.tile, to = min(from + a.tile, a.N);
-  for (int64_t i = from + threadIdx.x; i < to; i += kSortThreads) atomicAdd(&bins[sort_input<I, FIRST>(a, i).key >> a.shift & (a.bins - 1)], 1u);
+#pragma unroll
+  for (int r = 0; r < kSortRounds; ++r)
+    if (from + r * THREADS < a.N) atomicAdd(&bins[key[r] >> a.shift & (a.bins - 1)], 1u);
   __syncthreads();
-  for (int d = threadIdx.x; d < a.bins; d += kSortThreads) a.counts[(int64_t)blockIdx.x * a.bins + d] = bins[d];
+  for (int d = threadIdx.x; d < a.bins; d += THREADS) a.counts[(int64_t)blockIdx.x * a.bins + d] = bins[d];
 }
 
 // Many tiles: counts become those of the tiles in front.  A lane per digit; 16 wavefronts share the tiles.
@@ -159,8 +174,10 @@ __global__ __launch_bounds__(1024) void embedding_scan_kernel(const EmbeddingSor
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, d = blockIdx.x * 64 + lane;
   const int share = (a.tiles + 15) / 16, from = min(wave * share, a.tiles), to = min(from + share, a.tiles);
   uint32_t sum = 0;
-  if (d < a.bins)
+  if (d < a.bins) {
+#pragma unroll 8
     for (int t = from; t < to; ++t) sum += a.counts[(int64_t)t * a.bins + d];
+  }
   sums[wave][lane] = sum;
   __syncthreads();
   uint32_t before = 0, total = 0;
@@ -169,6 +186,7 @@ __global__ __launch_bounds__(1024) void embedding_scan_kernel(const EmbeddingSor
     total += sums[k][lane];
   }
   if (d >= a.bins) return;
+#pragma unroll 8
   for (int t = from; t < to; ++t) {
     uint32_t* const at = a.counts + (int64_t)t * a.bins + d;
     const uint32_t here = *at;
@@ -179,27 +197,52 @@ __global__ __launch_bounds__(1024) void embedding_scan_kernel(const EmbeddingSor
 }
 
 // Places: digits in order, tiles in order within a digit, a tile's tokens in order within that.  A wavefront ranks 64 tokens at a time: lanes
-// with the same digit find each other by one ballot a bit.
-template <typename I, bool FIRST, int ROUNDS>
-__global__ __launch_bounds__(kSortThreads) void embedding_scatter_kernel(const EmbeddingSort a) {
-  constexpr int kWaves = kSortThreads / 64, kOwn = kSortBins / kSortThreads;
-  __shared__ uint32_t bins[kWaves][kSortBins];   // of each wavefront: its count, then where its next token with that digit goes
+// with the same digit find each other by one ballot a bit.  Then four neighbouring digits belong to a thread.
+template <typename I, bool FIRST, int THREADS>
+__global__ __launch_bounds__(THREADS) void embedding_scatter_kernel(const EmbeddingSort a) {
+  constexpr int kWaves = THREADS / 64, kOwn = 4;
+  static_assert(THREADS * kOwn >= kSortBins);
+  __shared__ uint32_t bins[kWaves * kSortBins];   // of each wavefront: its count, then where its next token with that digit goes
   __shared__ uint32_t waves[kWaves];
+  using Counts = Pack<uint32_t, kOwn>;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int d = threadIdx.x; d < kWaves * a.bins; d += kSortThreads) bins[d / a.bins][d & (a.bins - 1)] = 0;
-  __syncthreads();
-  // counts within the wavefronts, and each token's rank within its wavefront
-  const int64_t from = (int64_t)blockIdx.x * a.tile + (int64_t)wave * ROUNDS * 64;
-  SortedToken token[ROUNDS];
-  uint32_t rank[ROUNDS];
+  const bool owns = threadIdx.x * kOwn < (unsigned)a.bins;
+  uint32_t* const mine = bins + wave * a.bins;
+  const int64_t from = ((int64_t)blockIdx.x * THREADS + wave * 64) * kSortRounds + lane;
+  SortedToken token[kSortRounds];
 #pragma unroll
-  for (int r = 0; r < ROUNDS; ++r) {
-    const int64_t i = from + r * 64 + lane;
-    if (i < a.N) token[r] = sort_input<I, FIRST>(a, i);
+  for (int r = 0; r < kSortRounds; ++r) token[r] = sort_input<I, FIRST>(a, min(from + r * 64, a.N - 1));
+  // tokens with this thread's digits: in all tiles, and in those in front
+  Counts total{}, before{};
+  if (owns) {
+    const Counts* const counts = reinterpret_cast<const Counts*>(a.counts) + threadIdx.x;
+    const int stride = a.bins / kOwn;
+    if (a.totals != nullptr) {
+      before = counts[(int64_t)blockIdx.x * stride];
+      total = reinterpret_cast<const Counts*>(a.totals)[threadIdx.x];
+    } else {
+      constexpr int kAhead = 16;
+      for (int t = 0; t < a.tiles; t += kAhead) {
+        Counts of[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) of[u] = counts[min(t + u, a.tiles - 1) * stride];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+          for (int k = 0; k < kOwn; ++k) {
+            const uint32_t here = t + u < a.tiles ? of[u].v[k] : 0u;
+            before.v[k] += t + u < (int)blockIdx.x ? here : 0u;
+            total.v[k] += here;
+          }
+      }
+    }
   }
+  for (int d = threadIdx.x; d < kWaves * a.bins; d += THREADS) bins[d] = 0;
+  __syncthreads();
+  uint32_t rank[kSortRounds];                     // within the wavefront
 #pragma unroll
-  for (int r = 0; r < ROUNDS; ++r) {
-    const bool here = from + r * 64 + lane < a.N;
+  for (int r = 0; r < kSortRounds; ++r) {
+    const bool here = from + r * 64 < a.N;
     const uint32_t digit = here ? token[r].key >> a.shift & (a.bins - 1) : 0;
     uint64_t same = __builtin_amdgcn_ballot_w64(here);
     for (int bit = 1; bit < a.bins; bit *= 2) {
@@ -207,43 +250,21 @@ __global__ __launch_bounds__(kSortThreads) void embedding_scatter_kernel(const E
       const uint64_t with = __builtin_amdgcn_ballot_w64(set);
       same &= set ? with : ~with;
     }
-    const uint32_t before = __builtin_amdgcn_mbcnt_hi((uint32_t)(same >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)same, 0));
-    if (here) rank[r] = bins[wave][digit] + before;
+    const uint32_t in_front = __builtin_amdgcn_mbcnt_hi((uint32_t)(same >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)same, 0));
+    if (here) rank[r] = mine[digit] + in_front;
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-    if (here && before == 0) bins[wave][digit] += (uint32_t)__builtin_popcountll(same);
+    if (here && in_front == 0) mine[digit] += (uint32_t)__builtin_popcountll(same);
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
   }
-  __syncthreads();
-  // where each digit's tokens of this tile go: a thread has kOwn neighbouring digits
-  uint32_t total[kOwn], before[kOwn], sum = 0;
+  // tokens with lower digits than this thread's
+  uint32_t sum = 0;
 #pragma unroll
-  for (int k = 0; k < kOwn; ++k) {
-    const int d = threadIdx.x * kOwn + k;
-    total[k] = before[k] = 0;
-    if (d >= a.bins) continue;
-    if (a.totals != nullptr) {
-      before[k] = a.counts[(int64_t)blockIdx.x * a.bins + d];
-      total[k] = a.totals[d];
-    }
-  }
-  if (a.totals == nullptr && threadIdx.x * kOwn < a.bins) {
-    for (int t = 0; t < a.tiles; ++t) {
-#pragma unroll
-      for (int k = 0; k < kOwn; ++k) {
-        if (threadIdx.x * kOwn + k >= a.bins) continue;
-        const uint32_t here = a.counts[(int64_t)t * a.bins + threadIdx.x * kOwn + k];
-        if (t < (int)blockIdx.x) before[k] += here;
-        total[k] += here;
-      }
-    }
-  }
-#pragma unroll
-  for (int k = 0; k < kOwn; ++k) sum += total[k];
-  uint32_t below = sum;   // of the digits up to this thread's, within the wavefront
+  for (int k = 0; k < kOwn; ++k) sum += total.v[k];
+  uint32_t below = sum;
 #pragma unroll
   for (int k = 1; k < 64; k *= 2) {
     const uint32_t o = __shfl_up(below, k);
@@ -253,42 +274,43 @@ __global__ __launch_bounds__(kSortThreads) void embedding_scatter_kernel(const E
   __syncthreads();
   below -= sum;
   for (int k = 0; k < wave; ++k) below += waves[k];
+  if (owns) {
 #pragma unroll
-  for (int k = 0; k < kOwn; ++k) {
-    const int d = threadIdx.x * kOwn + k;
-    if (d >= a.bins) continue;
-    uint32_t at = below + before[k];
-    below += total[k];
+    for (int k = 0; k < kOwn; ++k) {
+      uint32_t at = below + before.v[k];
+      below += total.v[k];
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      const uint32_t here = bins[w][d];
-      bins[w][d] = at;
-      at += here;
+      for (int w = 0; w < kWaves; ++w) {
+        uint32_t* const bin = bins + w * a.bins + threadIdx.x * kOwn + k;
+        const uint32_t here = *bin;
+        *bin = at;
+        at += here;
+      }
     }
   }
   __syncthreads();
 #pragma unroll
-  for (int r = 0; r < ROUNDS; ++r)
-    if (from + r * 64 + lane < a.N) a.out[bins[wave][token[r].key >> a.shift & (a.bins - 1)] + rank[r]] = token[r];
+  for (int r = 0; r < kSortRounds; ++r)
+    if (from + r * 64 < a.N) a.out[mine[token[r].key >> a.shift & (a.bins - 1)] + rank[r]] = token[r];
 }
 
 // ---- sums --------------------------------------------------------------------------------------------------
-// A piece of a table's row: written, or added to what is there.  The last piece of a row is moved back to end with it; the columns that the piece before
-// has too are left to that one.
+// A piece of a table's row: written, or added to what is there.  The last piece of a row is moved back to end with it.  The columns that the piece
+// before has too are written twice, with the same values, but added once.
 template <typename W, int E>
 __device__ __forceinline__ void store_piece(const EmbeddingBackward& a, const uint32_t row, const int piece, const float (&sum)[E]) {
-  const int at = min(piece * E, a.D - E), skip = piece * E - at;
+  const int at = min(piece * E, a.D - E);
   W* const out = static_cast<W*>(a.dtable) + row * a.lddt + at;
-  if (skip == 0) {
+  if (!a.accumulate) {
     Pack<W, E> v;
-    if (a.accumulate) v = *reinterpret_cast<const Pack<W, E>*>(out);
 #pragma unroll
-    for (int j = 0; j < E; ++j) v.v[j] = from_float<W>((a.accumulate ? to_float(v.v[j]) : 0.f) + a.scale * sum[j]);
-    *reinterpret_cast<Pack<W, E>*>(out) = v;
+    for (int j = 0; j < E; ++j) v.v[j] = from_float<W>(as_f32(a.scale * sum[j]));
+    store_pack(out, v);
   } else {
+    const int skip = piece * E - at;
 #pragma unroll
     for (int j = 0; j < E; ++j)
-      if (j >= skip) out[j] = from_float<W>((a.accumulate ? to_float(out[j]) : 0.f) + a.scale * sum[j]);
+      if (j >= skip) out[j] = from_float<W>(as_f32(to_float(out[j]) + a.scale * sum[j]));
   }
 }
 
@@ -341,34 +363,97 @@ __device__ __forceinline__ void embedding_sum_chunk(const EmbeddingBackward& a, 
   if (key < (uint32_t)a.V) finish(to < a.N && a.sorted[to].key == key);
 }
 
-// First place among the sorted tokens whose key is not below this one.
-__device__ __forceinline__ int64_t lower_bound(const SortedToken* sorted, const int64_t N, const uint32_t key) {
-  int64_t low = 0, high = N;
+// Very few tokens: no sorting.  A wavefront has all of them in its lanes, walks over rows of the table (and slabs of 64 pieces) and finds those that name
+// one by a ballot for each 64.
+constexpr int kFewRounds = 2, kFewTokens = kFewRounds * 64;
+template <typename T, typename W, typename I, int E>
+__global__ __launch_bounds__(kSumThreads) void embedding_few_kernel(const EmbeddingBackward a) {
+  const int lane = threadIdx.x & 63, N = (int)a.N;
+  I raw[kFewRounds];
+#pragma unroll
+  for (int r = 0; r < kFewRounds; ++r) raw[r] = static_cast<const I*>(a.tokens)[min(r * 64 + lane, N - 1)];
+  uint32_t key[kFewRounds];
+#pragma unroll
+  for (int r = 0; r < kFewRounds; ++r) key[r] = r * 64 + lane < N ? key_of(raw[r], a.V) : (uint32_t)a.V;
+  const int64_t units = a.V * a.slabs, step = (int64_t)gridDim.x * (kSumThreads / 64);
+  for (int64_t u = (int64_t)blockIdx.x * (kSumThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); u < units; u += step) {
+    const uint32_t v = (uint32_t)(u / a.slabs);
+    const int piece = (int)(u % a.slabs) * 64 + lane, at = min(piece * E, a.D - E);
+    float sum[E];
+#pragma unroll
+    for (int j = 0; j < E; ++j) sum[j] = 0.f;
+    bool named = false;
+#pragma unroll
+    for (int r = 0; r < kFewRounds; ++r) {
+      uint64_t mask = __builtin_amdgcn_ballot_w64(key[r] == v);
+      named |= mask != 0;
+      while (mask != 0) {
+        const int here = __builtin_popcountll(mask);
+        Pack<T, E> row[kSumAhead];
+#pragma unroll
+        for (int k = 0; k < kSumAhead; ++k) {
+          if (k >= here) break;
+          const int64_t i = r * 64 + __builtin_ctzll(mask);
+          mask &= mask - 1;
+          if (piece < a.pieces) row[k] = *reinterpret_cast<const Pack<T, E>*>(static_cast<const T*>(a.dy) + i * a.lddy + at);
+        }
+#pragma unroll
+        for (int k = 0; k < kSumAhead; ++k) {
+          if (k >= here) break;
+#pragma unroll
+          for (int j = 0; j < E; ++j) sum[j] += to_float(row[k].v[j]);
+        }
+      }
+    }
+    if (piece < a.pieces && (named || !a.accumulate)) store_piece<W, E>(a, v, piece, sum);
+  }
+}
+
+// First place in [low, high) of the sorted tokens whose key is not below this one (high, if there is none): a lane for each of 64 places at a time.
+__device__ __forceinline__ int64_t wave_lower_bound(const SortedToken* sorted, int64_t low, int64_t high, const uint32_t key) {
+  const int lane = threadIdx.x & 63;
   while (low < high) {
-    const int64_t mid = (low + high) / 2;
-    if (sorted[mid].key < key) low = mid + 1; else high = mid;
+    const int64_t step = (high - low + 63) / 64, at = low + (lane + 1) * step - 1;   // the last place of the lane's share
+    const int below = __builtin_popcountll(__builtin_amdgcn_ballot_w64(at < high && sorted[at].key < key));
+    low += below * step;
+    high = min(high, low + step - 1);                                                // (that share's last place is not below)
   }
   return low;
 }
 
-// Zeros in those of 64 rows that no token names: a lane looks for a row, the wavefront writes it.
+// Zeros in those of a.clear_rows rows that no token names.
 template <typename W>
 __device__ __forceinline__ void embedding_clear_rows(const EmbeddingBackward& a, const int64_t first) {
   constexpr int E = 16 / sizeof(W);
   const int lane = threadIdx.x & 63;
+  // the tokens that name these rows: looked for among few, or each row's for itself among many
+  const int64_t from = wave_lower_bound(a.sorted, 0, a.N, (uint32_t)first), to = wave_lower_bound(a.sorted, from, a.N, (uint32_t)(first + a.clear_rows));
   const int64_t v = first + lane;
-  bool absent = false;
-  if (v < a.V) {
-    const int64_t at = lower_bound(a.sorted, a.N, (uint32_t)v);
-    absent = at == a.N || a.sorted[at].key != (uint32_t)v;
+  bool named = false;
+  if (to - from <= 64) {
+    const uint32_t at = from + lane < to ? a.sorted[from + lane].key - (uint32_t)first : 64u;
+    uint32_t low = at < 32 ? 1u << at : 0u, high = at >= 32 && at < 64 ? 1u << (at - 32) : 0u;
+#pragma unroll
+    for (int k = 1; k < 64; k *= 2) {
+      low |= __shfl_xor(low, k);
+      high |= __shfl_xor(high, k);
+    }
+    named = ((lane < 32 ? low : high) >> (lane & 31) & 1u) != 0;
+  } else {
+    int64_t low = from, high = to;
+    while (low < high) {
+      const int64_t mid = (low + high) / 2;
+      if (a.sorted[mid].key < (uint32_t)v) low = mid + 1; else high = mid;
+    }
+    named = low < to && a.sorted[low].key == (uint32_t)v;
   }
-  for (uint64_t rows = __builtin_amdgcn_ballot_w64(absent); rows != 0; rows &= rows - 1) {
+  for (uint64_t rows = __builtin_amdgcn_ballot_w64(lane < a.clear_rows && v < a.V && !named); rows != 0; rows &= rows - 1) {
     W* const row = static_cast<W*>(a.dtable) + (first + __builtin_ctzll(rows)) * a.lddt;
     Pack<W, E> zeros;
 #pragma unroll
     for (int j = 0; j < E; ++j) zeros.v[j] = from_float<W>(0.f);
     const int full = a.D / E;
-    for (int p = lane; p < full; p += 64) *reinterpret_cast<Pack<W, E>*>(row + p * E) = zeros;
+    for (int p = lane; p < full; p += 64) store_pack(row + p * E, zeros);
     if (full * E + lane < a.D) row[full * E + lane] = from_float<W>(0.f);
   }
 }
@@ -377,7 +462,7 @@ template <typename T, typename W, int E, bool WAVE>
 __global__ __launch_bounds__(kSumThreads) void embedding_sum_kernel(const EmbeddingBackward a) {
   if (blockIdx.x >= a.sum_groups) {
     const int64_t wave = (int64_t)(blockIdx.x - a.sum_groups) * (kSumThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (wave * 64 < a.V) embedding_clear_rows<W>(a, wave * 64);
+    if (wave * a.clear_rows < a.V) embedding_clear_rows<W>(a, wave * a.clear_rows);
     return;
   }
   if (WAVE) {   // (uniform)
@@ -390,18 +475,28 @@ __global__ __launch_bounds__(kSumThreads) void embedding_sum_kernel(const Embedd
   }
 }
 
-// A workgroup per chunk in which a token begins that goes on behind it, and 64 pieces: the parts of all chunks that have rows of it.
-constexpr int kJoinThreads = 256;
+// A workgroup per chunk in which a token begins that goes on behind it, and 64 pieces: the parts of all chunks that have rows of it, dealt to
+// its wavefronts.
+constexpr int kJoinThreads = 512;
 template <typename W, int E>
 __global__ __launch_bounds__(kJoinThreads) void embedding_join_kernel(const EmbeddingBackward a) {
   constexpr int kWaves = kJoinThreads / 64;
   __shared__ float parts[kWaves][64][E];
   const int64_t chunk = blockIdx.x / a.slabs, from = chunk * a.chunk, to = from + a.chunk;
   if (to >= a.N) return;
-  const uint32_t key = a.sorted[to - 1].key;
-  if (key >= (uint32_t)a.V || a.sorted[to].key != key || (from > 0 && a.sorted[from - 1].key == key)) return;
-  const int64_t last = (lower_bound(a.sorted, a.N, key + 1) - 1) / a.chunk;
+  const uint32_t key = a.sorted[to - 1].key, behind = a.sorted[to].key, in_front = from > 0 ? a.sorted[from - 1].key : ~key;
+  if (key >= (uint32_t)a.V || behind != key || in_front == key) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, piece = (int)(blockIdx.x % a.slabs) * 64 + lane;
+  int64_t last = chunk + 1;              // the chunk with its last row: a lane looks where each of the next ones ends
+  for (;;) {
+    const int64_t end = (last + lane + 1) * a.chunk;
+    const uint64_t goes_on = __builtin_amdgcn_ballot_w64(end < a.N && a.sorted[end].key == key);
+    if (~goes_on != 0) {
+      last += __builtin_ctzll(~goes_on);
+      break;
+    }
+    last += 64;
+  }
   float sum[E];
 #pragma unroll
   for (int j = 0; j < E; ++j) sum[j] = 0.f;

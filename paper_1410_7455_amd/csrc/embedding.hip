@@ -39,12 +39,11 @@ int launch_forward(EmbeddingForward a, hipStream_t s) {
 }
 
 // How a gradient is computed: all by sizes, so that a workspace for more tokens serves fewer.
-constexpr int64_t kRankMost = 8192;        // tokens whose ranks are counted
-constexpr int kSortSmallTile = 1024, kSortTile = 4096;
-constexpr int64_t kSumWaves = 8192;        // wavefronts that the sums are cut into, if there are as many
+constexpr int kSortSmall = 256, kSortLarge = 1024;   // threads
+constexpr int64_t kSortSmallTile = kSortSmall * kSortRounds, kSortTile = kSortLarge * kSortRounds;
+constexpr int64_t kSumWaves = 4096;        // wavefronts that the sums are cut into, if there are as many
+constexpr int64_t kFewGroups = 4096;       // workgroups that walk over a table
 constexpr int kLeastChunk = 16, kMostChunk = 512;
-
-int sort_tile(const int64_t N) { return N <= (int64_t)kSortSmallTile * kSortInline ? kSortSmallTile : kSortTile; }
 
 struct BackwardPlan {
   int e, pieces, lanes, slabs, chunk;
@@ -88,18 +87,15 @@ Workspace layout(Carver& c, const int64_t N, const int D) {
   return w;
 }
 
-template <typename I, bool FIRST>
+template <typename I, bool FIRST, int THREADS>
 int sort_pass(const EmbeddingSort& a, hipStream_t s) {
-  hipLaunchKernelGGL((embedding_count_kernel<I, FIRST>), dim3((unsigned)a.tiles), dim3(kSortThreads), 0, s, a);
+  hipLaunchKernelGGL((embedding_count_kernel<I, FIRST, THREADS>), dim3((unsigned)a.tiles), dim3(THREADS), 0, s, a);
   LAUNCH_CHECK();
   if (a.totals != nullptr) {
     hipLaunchKernelGGL(embedding_scan_kernel, dim3((unsigned)((a.bins + 63) / 64)), dim3(1024), 0, s, a);
     LAUNCH_CHECK();
   }
-  if (a.tile == kSortSmallTile)
-    hipLaunchKernelGGL((embedding_scatter_kernel<I, FIRST, kSortSmallTile / kSortThreads>), dim3((unsigned)a.tiles), dim3(kSortThreads), 0, s, a);
-  else
-    hipLaunchKernelGGL((embedding_scatter_kernel<I, FIRST, kSortTile / kSortThreads>), dim3((unsigned)a.tiles), dim3(kSortThreads), 0, s, a);
+  hipLaunchKernelGGL((embedding_scatter_kernel<I, FIRST, THREADS>), dim3((unsigned)a.tiles), dim3(THREADS), 0, s, a);
   LAUNCH_CHECK();
   return NGSGD_OK;
 }
@@ -114,16 +110,17 @@ int sort_tokens(const void* tokens, const int64_t N, const int64_t V, const Work
   }
   int bits = 1;                            // of the keys 0 .. V
   while ((int64_t)1 << bits <= V) ++bits;
-  const int passes = (bits + kSortBits - 1) / kSortBits, digit = (bits + passes - 1) / passes;
-  EmbeddingSort a{tokens, nullptr, nullptr, N, V, w.counts, nullptr, 0, sort_tile(N), 0, 1 << digit};
-  a.tiles = (int)((N + a.tile - 1) / a.tile);
+  const int passes = (bits + kSortBits - 1) / kSortBits, digit = std::max(2, (bits + passes - 1) / passes);
+  const bool small = N <= kSortSmallTile * kSortInline;
+  const int64_t tile = small ? kSortSmallTile : kSortTile;
+  EmbeddingSort a{tokens, nullptr, nullptr, N, V, w.counts, nullptr, (int)((N + tile - 1) / tile), 0, 1 << digit};
   if (a.tiles > kSortInline) a.totals = w.totals;
   for (int pass = 0; pass < passes; ++pass, a.shift += digit) {
     a.out = (passes - pass) % 2 == 1 ? w.sorted : w.other;   // the last one's
     if (pass == 0)
-      NG_TRY((sort_pass<I, true>(a, s)));
+      NG_TRY(small ? (sort_pass<I, true, kSortSmall>(a, s)) : (sort_pass<I, true, kSortLarge>(a, s)));
     else
-      NG_TRY((sort_pass<I, false>(a, s)));
+      NG_TRY(small ? (sort_pass<I, false, kSortSmall>(a, s)) : (sort_pass<I, false, kSortLarge>(a, s)));
     a.in = a.out;
   }
   return NGSGD_OK;
@@ -141,6 +138,14 @@ int launch_sums(const EmbeddingBackward& a, const unsigned grid, hipStream_t s) 
     hipLaunchKernelGGL((embedding_join_kernel<W, E>), dim3((unsigned)(a.chunks * a.slabs)), dim3(kJoinThreads), 0, s, a);
     LAUNCH_CHECK();
   }
+  return NGSGD_OK;
+}
+
+template <typename T, typename W, typename I, int E>
+int launch_few(const EmbeddingBackward& a, hipStream_t s) {
+  const int64_t groups = std::min<int64_t>((a.V * a.slabs + kSumThreads / 64 - 1) / (kSumThreads / 64), kFewGroups);
+  hipLaunchKernelGGL((embedding_few_kernel<T, W, I, E>), dim3((unsigned)groups), dim3(kSumThreads), 0, s, a);
+  LAUNCH_CHECK();
   return NGSGD_OK;
 }
 
@@ -183,12 +188,23 @@ extern "C" int ngsgd_embedding_backward(const void* dev_dy, int64_t lddy, int32_
   const BackwardPlan p = backward_plan(N, D, type_bytes(type));
   if (p.chunks * p.slabs >= (int64_t)1 << 24) return NGSGD_EINVAL;   // a launch has less than 2^32 threads (no memory holds such rows)
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  EmbeddingBackward a{dev_dy, lddy, dev_tokens, N, V, D, scale, dev_dtable, lddt, accumulate, nullptr, nullptr, p.chunk, p.chunks, p.pieces, p.lanes, p.slabs, 0, 1};
+  if (N > 0 && N <= kFewTokens)
+    return with_types(type, table_type, index_type, [&](auto t, auto wt, auto i) {
+      using T = decltype(t);
+      using W = decltype(wt);
+      using I = decltype(i);
+      return p.e == 1 ? launch_few<T, W, I, 1>(a, s) : launch_few<T, W, I, 16 / sizeof(T)>(a, s);
+    });
   Carver c(dev_workspace);
   const Workspace w = layout(c, N, D);
   if (N > 0) NG_TRY(index_type == NGSGD_INT32 ? sort_tokens<int32_t>(dev_tokens, N, V, w, s) : sort_tokens<int64_t>(dev_tokens, N, V, w, s));
-  EmbeddingBackward a{dev_dy, lddy, dev_tokens, N, V, D, scale, dev_dtable, lddt, accumulate, w.sorted, w.parts, p.chunk, p.chunks, p.pieces, p.lanes, p.slabs, 0};
+  a.sorted = w.sorted;
+  a.parts = w.parts;
   a.sum_groups = (unsigned)((p.chunks * p.slabs * p.lanes + kSumThreads - 1) / kSumThreads);
-  const unsigned grid = a.sum_groups + (accumulate ? 0u : (unsigned)((V + kSumThreads - 1) / kSumThreads));
+  while (a.clear_rows < 64 && a.clear_rows * 8192ll < V) a.clear_rows *= 2;
+  const int64_t clear_waves = accumulate ? 0 : (V + a.clear_rows - 1) / a.clear_rows;
+  const unsigned grid = a.sum_groups + (unsigned)((clear_waves + kSumThreads / 64 - 1) / (kSumThreads / 64));
   return with_types(type, table_type, NGSGD_INT32, [&](auto t, auto wt, auto) {
     using T = decltype(t);
     using W = decltype(wt);
