@@ -269,7 +269,7 @@ int ngsgd_embedding_backward(const void* dev_dy, int64_t lddy, int32_t type, con
  * the loss and the label's gradient of a row that is as good as decided keep their digits; the gradient is rounded once.  A logit of -infinity is
  * a class that is not there: its probability is 0, and as the label's it gives a loss of infinity.  A row with a NaN or
  * +infinity, or with -infinity alone, has a loss and a gradient of NaN.  Sums are in an order that depends on the sizes alone.  Leading dimensions are
- * at least V.  N and V are at most 2^30.  dev_workspace (256-byte aligned) holds nothing between calls; calls that may run at the
+ * at least V.  N is at most 2^30 and V 2^29.  dev_workspace (256-byte aligned) holds nothing between calls; calls that may run at the
  * same time need one each. */
 int ngsgd_cross_entropy_workspace_bytes(int64_t max_rows, int32_t V, size_t* out_bytes);
 int ngsgd_cross_entropy(const void* dev_logits, int64_t ld, int32_t type, const void* dev_labels, int32_t index_type,

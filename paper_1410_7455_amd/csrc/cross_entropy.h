@@ -2,6 +2,13 @@
 //   m = max_j x_j;  e_j = exp(x_j - m);  S = sum_{j != y} e_j
 //   loss = log(S + e_y) - (x_y - m);  d_j = scale e_j / (S + e_y),  d_y = -scale S / (S + e_y)
 // The label's term is kept out of the sum: where it is almost all of it, S is what the loss and the label's gradient are made of.
+//
+// Exponentials are powers of two of x L - M, L = log2(e) in fp32 and M = m L rounded: one multiply-add, which rounds once, and the hardware's power.  What
+// M's rounding adds is the same for all of a row, and the quotients do not see it; the loss takes the m that M stands for.  Where m L could overflow,
+// numbers that differ do so by 10^31: there L = 2^-20, which gives 1 for m and 0 for all others.
+//
+// Rows of up to 16384 pieces of 16 bytes are held in registers: read once, written once.  Wider ones are read a second time for the gradient.  Few wide
+// rows are cut into parts, whose statistics a second kernel joins.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -11,74 +18,333 @@
 
 namespace ngsgd {
 
-constexpr int kLossThreads = 256;
-
 struct CrossEntropy {
   const void* logits;
   int64_t ld;
   const void* labels;
+  int index_bytes;          // of a label: 4 or 8
   int64_t N;
   int V;
-  float* loss;          // optional
+  float* loss;              // optional
   float scale;
   const float* dev_scale;   // optional
-  void* dlogits;        // optional
+  void* dlogits;            // optional
   int64_t ldd;
+  struct LossStats* stats;  // [N][parts + 1], of rows in parts; the last one's m is the label's logit
+  int parts;
 };
 
-__device__ __forceinline__ float wave_max_f32(float v) {
-#pragma unroll
-  for (int k = 1; k < 64; k *= 2) {
-    const float o = __shfl_xor(v, k);
-    v = v != v || v > o ? v : o;   // (a NaN stays)
+__device__ __forceinline__ int64_t label_of(const CrossEntropy& a, const int64_t row) {
+  return a.index_bytes == 4 ? static_cast<const int32_t*>(a.labels)[row] : static_cast<const int64_t*>(a.labels)[row];
+}
+
+constexpr float kLog2e = 1.44269504088896341f;
+constexpr double kLog2eMore = 1.44269504088896341 / (double)kLog2e;   // what one power of L is short of
+constexpr float kLowest = -3.4028234663852886e38f;
+
+// S of some columns: the sum of their powers, in units that go with their largest logit.
+struct LossStats {
+  float m, S;
+};
+struct PowerBase {
+  float m, L, M;
+  __device__ __forceinline__ explicit PowerBase(const float m) : m(m) {
+    L = far() ? 0x1p-20f : kLog2e;
+    M = m * L;
   }
-  return v;
+  __device__ __forceinline__ bool far() const { return fabsf(m) > 1e38f; }
+  __device__ __forceinline__ float power(const float x) const { return __builtin_amdgcn_exp2f(fmaf(x, L, -M)); }
+  // What a sum in the units of a lower base is in these; the bases may be far apart, and all of the sum sees the error of this.
+  __device__ __forceinline__ float share(const PowerBase& other) const {
+    if (other.m == m) return 1.f;
+    if (far() || other.far()) return 0.f;
+    const double t = fmax(((double)other.M - (double)M) * kLog2eMore, -1000.0);
+    const float high = (float)t;
+    return __builtin_amdgcn_exp2f(high) * fmaf((float)(t - (double)high), 0.693147180559945309f, 1.f);
+  }
+};
+
+// What a row's statistics make of its loss and gradient.
+struct LossRow {
+  PowerBase base;
+  float f, label_gradient, loss;
+  __device__ __forceinline__ LossRow(const CrossEntropy& a, const LossStats& others, const float label) : base(fmaxf(others.m, label)) {
+    const float S = others.S * base.share(PowerBase(others.m)), e = base.power(label), total = S + e;
+    f = (a.dev_scale != nullptr ? a.scale * *a.dev_scale : a.scale) / total;
+    label_gradient = -f * S;
+    if (label >= others.m)
+      loss = log1pf(S / e);
+    else
+      loss = (float)((double)logf(total) + ((double)base.M / (double)base.L - (double)label));
+  }
+};
+
+// A row's columns in pieces of E; the last one is moved back to end with the row, and its first elements, which the piece before has too, do not count.
+template <typename T, int E>
+struct LossPieces {
+  const T* x;
+  int V, pieces, label_piece, label_at;
+  __device__ __forceinline__ LossPieces(const T* row, const int V, const int label) : x(row), V(V), pieces((V - 1) / E + 1) {
+    label_piece = label / E;
+    label_at = label - start(label_piece);
+  }
+  __device__ __forceinline__ int start(const int piece) const { return min(piece * E, V - E); }   // (V is at most 2^30)
+  __device__ __forceinline__ int skip(const int piece) const { return piece * E - start(piece); }
+  // (offsets in bytes, without a sign and below 2^32, are added to a scalar address as they are)
+  __device__ __forceinline__ uint32_t offset(const int at) const { return (uint32_t)at * (uint32_t)sizeof(T); }
+  __device__ __forceinline__ Pack<T, E> load(const int piece) const {
+    return *reinterpret_cast<const Pack<T, E>*>(reinterpret_cast<const char*>(x) + offset(start(piece)));
+  }
+  // -infinity in the place of the label and of what does not count
+  __device__ __forceinline__ void mask(Pack<T, E>& v, const int piece) const {
+    if (piece != label_piece && piece != pieces - 1) return;
+#pragma unroll
+    for (int j = 0; j < E; ++j)
+      if (j < skip(piece) || (piece == label_piece && j == label_at)) v.v[j] = from_float<T>(-INFINITY);
+  }
+  __device__ __forceinline__ void store(T* d, const Pack<T, E>& v, const int piece, const LossRow& row) const {
+    Pack<T, E> out;
+#pragma unroll
+    for (int j = 0; j < E; ++j) out.v[j] = from_float<T>(row.f * row.base.power(to_float(v.v[j])));
+    if (piece != label_piece && piece != pieces - 1) {
+      store_pack(reinterpret_cast<T*>(reinterpret_cast<char*>(d) + offset(start(piece))), out);
+    } else {
+#pragma unroll
+      for (int j = 0; j < E; ++j)
+        if (j >= skip(piece)) d[start(piece) + j] = piece == label_piece && j == label_at ? from_float<T>(row.label_gradient) : out.v[j];
+    }
+  }
+};
+// Keeps a piece as it was loaded: the compiler would hold the numbers that it has unpacked from it, twice the registers, for the next time that they are
+// used.
+template <typename T, int E>
+__device__ __forceinline__ void keep_packed(Pack<T, E>& v) {
+  if constexpr (sizeof(v) == 16) {
+    U32x4 bits = __builtin_bit_cast(U32x4, v);
+    asm("" : "+v"(bits));
+    v = __builtin_bit_cast(Pack<T, E>, bits);
+  }
+}
+template <typename T, int E>
+__device__ __forceinline__ float largest_of(const Pack<T, E>& v) {
+  float m = to_float(v.v[0]);
+#pragma unroll
+  for (int j = 1; j < E; ++j) m = fmaxf(m, to_float(v.v[j]));
+  return m;
 }
 
-// log(S + e) - (x_y - m)
-__device__ __forceinline__ float loss_of(const float S, const float e, const float label, const float m) {
-  // the label's is the largest logit: e = 1, and S may be far below it
-  return label == m ? log1pf(S) : logf(S + e) - (label - m);
+// Over G lanes, or with G > 64 over a workgroup of G threads.
+template <int CTRL>
+__device__ __forceinline__ float dpp_max_f32(const float v) {
+  return fmaxf(v, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true)));
+}
+__device__ __forceinline__ float row16_max_f32(float v) {
+  v = dpp_max_f32<0xB1>(v);    // quad_perm [1,0,3,2]
+  v = dpp_max_f32<0x4E>(v);    // quad_perm [2,3,0,1]
+  v = dpp_max_f32<0x141>(v);   // row_half_mirror
+  return dpp_max_f32<0x140>(v);   // row_mirror
+}
+__device__ __forceinline__ float wave_max_f32(float v) {
+  v = row16_max_f32(v);
+  const auto a = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+  v = fmaxf(__builtin_bit_cast(float, (uint32_t)a[0]), __builtin_bit_cast(float, (uint32_t)a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+  return fmaxf(__builtin_bit_cast(float, (uint32_t)b[0]), __builtin_bit_cast(float, (uint32_t)b[1]));
+}
+template <int G>
+__device__ __forceinline__ float group_max(float v, BlockScratch& red) {
+  if constexpr (G == 16) {
+    return row16_max_f32(v);
+  } else if constexpr (G == 64) {
+    return wave_max_f32(v);
+  } else {
+    v = wave_max_f32(v);
+    if ((threadIdx.x & 63) == 0) red[0][threadIdx.x >> 6].v[0] = v;
+    __syncthreads();
+    return row16_max_f32(red[0][min((int)(threadIdx.x & 15), G / 64 - 1)].v[0]);
+  }
+}
+template <int G>
+__device__ __forceinline__ float group_sum(const float v, BlockScratch& red) {
+  if constexpr (G == 16) return row16_sum_f32(v);
+  else if constexpr (G == 64) return wave_sum_f32(v);
+  else return block_sum_f32(v, red, 1);
 }
 
-// A workgroup per row: three passes over it.
-template <typename T, typename I>
-__global__ __launch_bounds__(kLossThreads) void cross_entropy_kernel(const CrossEntropy a) {
+template <typename T>
+__device__ __forceinline__ void clear_row(T* d, const int V, const int thread, const int threads) {
+  constexpr int E = 16 / sizeof(T);
+  Pack<T, E> zeros;
+#pragma unroll
+  for (int j = 0; j < E; ++j) zeros.v[j] = from_float<T>(0.f);
+  for (int p = thread; p < V / E; p += threads) store_pack(d + p * E, zeros);
+  if (V / E * E + thread < V) d[V / E * E + thread] = from_float<T>(0.f);   // (there are at least E threads)
+}
+
+// G threads hold a row, P pieces each; a workgroup has THREADS / G rows.
+template <typename T, int E, int G, int P, int THREADS>
+__global__ __launch_bounds__(THREADS, P <= 8 ? 8 : 4) void cross_entropy_kernel(const CrossEntropy a) {
   __shared__ BlockScratch red;
-  __shared__ float top[kLossThreads / 64];
-  const int64_t row = blockIdx.x;
-  const int64_t label = static_cast<const I*>(a.labels)[row];
-  const T* x = static_cast<const T*>(a.logits) + row * a.ld;
-  T* d = static_cast<T*>(a.dlogits) + row * a.ldd;
+  int row_in_group = threadIdx.x / G;
+  if constexpr (G >= 64) row_in_group = __builtin_amdgcn_readfirstlane(row_in_group);   // (so that addresses are a scalar and an offset)
+  const int64_t row = (int64_t)blockIdx.x * (THREADS / G) + row_in_group;
+  int thread = threadIdx.x % G;
+  if (row >= a.N) return;
+  const int64_t label = label_of(a, row);
+  const T* const x = static_cast<const T*>(a.logits) + row * a.ld;
+  T* const d = static_cast<T*>(a.dlogits) + row * a.ldd;
   if (label < 0 || label >= a.V) {
-    if (a.loss != nullptr && threadIdx.x == 0) a.loss[row] = 0.f;
-    if (a.dlogits != nullptr)
-      for (int j = threadIdx.x; j < a.V; j += kLossThreads) d[j] = from_float<T>(0.f);
+    if (a.loss != nullptr && thread == 0) a.loss[row] = 0.f;
+    if (a.dlogits != nullptr) clear_row(d, a.V, thread, G);
     return;
   }
-  float m = -INFINITY;
-  for (int j = threadIdx.x; j < a.V; j += kLossThreads) {
-    const float v = to_float(x[j]);
-    m = m != m || m > v ? m : v;
-  }
-  m = wave_max_f32(m);
-  if ((threadIdx.x & 63) == 0) top[threadIdx.x >> 6] = m;
-  __syncthreads();
+  const LossPieces<T, E> pieces(x, a.V, (int)label);
+  Pack<T, E> v[P];
 #pragma unroll
-  for (int k = 0; k < kLossThreads / 64; ++k) {
-    const float o = top[k];
-    m = m != m || m > o ? m : o;
+  for (int p = 0; p < P; ++p) {
+    if (p * G + thread < pieces.pieces) {
+      v[p] = pieces.load(p * G + thread);
+    } else {
+#pragma unroll
+      for (int j = 0; j < E; ++j) v[p].v[j] = from_float<T>(-INFINITY);
+    }
   }
+  const float own = to_float(x[label]);
+  float m = kLowest;
+#pragma unroll
+  for (int p = 0; p < P; ++p) {
+    if (p * G < pieces.pieces) {   // (uniform)
+      pieces.mask(v[p], p * G + thread);
+      keep_packed(v[p]);
+      m = fmaxf(m, largest_of(v[p]));
+      keep_packed(v[p]);
+    }
+  }
+  m = group_max<G>(m, red);
+  const PowerBase base(m);
   float S = 0.f;
-  for (int j = threadIdx.x; j < a.V; j += kLossThreads) S += j == label ? 0.f : expf(to_float(x[j]) - m);
-  S = block_sum_f32(S, red, 0);
-  if (!(fabsf(m) < INFINITY)) S = NAN;   // a largest logit that is the label's and infinite would leave zeros
-  const float xl = to_float(x[label]), e = expf(xl - m);
-  if (a.loss != nullptr && threadIdx.x == 0) a.loss[row] = loss_of(S, e, xl, m);
+#pragma unroll
+  for (int p = 0; p < P; ++p) {
+    if (p * G < pieces.pieces) {
+#pragma unroll
+      for (int j = 0; j < E; ++j) S += base.power(to_float(v[p].v[j]));
+      keep_packed(v[p]);
+    }
+  }
+  S = group_sum<G>(S, red);
+  const LossRow out(a, LossStats{m, S}, own);
+  if (a.loss != nullptr && thread == 0) a.loss[row] = out.loss;
   if (a.dlogits == nullptr) return;
-  __syncthreads();   // the label's logit has been read: dlogits may be logits
-  const float f = (a.dev_scale != nullptr ? a.scale * *a.dev_scale : a.scale) / (S + e);
-  for (int j = threadIdx.x; j < a.V; j += kLossThreads) d[j] = from_float<T>(j == label ? -S * f : f * expf(to_float(x[j]) - m));
+  asm("" : "+v"(thread));   // the offsets are formed anew: kept, they would take a register a piece
+#pragma unroll
+  for (int p = 0; p < P; ++p)
+    if (p * G + thread < pieces.pieces) pieces.store(d, v[p], p * G + thread, out);
+}
+
+// ---- rows that are read twice --------------------------------------------------------------------------
+constexpr int kWideThreads = 1024, kPartThreads = 256, kStreamAhead = 4;
+
+// Statistics of pieces [from, to), by all threads of a workgroup: each has its own largest logit, and its sum in units of that.
+template <typename T, int E, int THREADS>
+__device__ __forceinline__ LossStats stream_stats(const LossPieces<T, E>& pieces, const int from, const int to, BlockScratch& red) {
+  LossStats mine{kLowest, 0.f};
+  for (int p = from + threadIdx.x; p < to; p += THREADS * kStreamAhead) {
+    Pack<T, E> v[kStreamAhead];
+#pragma unroll
+    for (int k = 0; k < kStreamAhead; ++k) v[k] = pieces.load(min(p + k * THREADS, to - 1));
+    float m = mine.m;
+#pragma unroll
+    for (int k = 0; k < kStreamAhead; ++k) {
+      if (p + k * THREADS >= to) {
+#pragma unroll
+        for (int j = 0; j < E; ++j) v[k].v[j] = from_float<T>(-INFINITY);
+      }
+      pieces.mask(v[k], p + k * THREADS);
+      m = fmaxf(m, largest_of(v[k]));
+    }
+    const PowerBase base(m);
+    if (m != mine.m) mine = LossStats{m, mine.S * base.share(PowerBase(mine.m))};
+#pragma unroll
+    for (int k = 0; k < kStreamAhead; ++k)
+#pragma unroll
+      for (int j = 0; j < E; ++j) mine.S += base.power(to_float(v[k].v[j]));
+  }
+  const float m = group_max<THREADS>(mine.m, red);
+  return LossStats{m, group_sum<THREADS>(mine.S * PowerBase(m).share(PowerBase(mine.m)), red)};
+}
+template <typename T, int E, int THREADS>
+__device__ __forceinline__ void stream_gradient(const LossPieces<T, E>& pieces, const int from, const int to, T* d, const LossRow& row) {
+  for (int p = from + threadIdx.x; p < to; p += THREADS * kStreamAhead) {
+    Pack<T, E> v[kStreamAhead];
+#pragma unroll
+    for (int k = 0; k < kStreamAhead; ++k) v[k] = pieces.load(min(p + k * THREADS, to - 1));
+#pragma unroll
+    for (int k = 0; k < kStreamAhead; ++k)
+      if (p + k * THREADS < to) pieces.store(d, v[k], p + k * THREADS, row);
+  }
+}
+
+// A workgroup per row.
+template <typename T>
+__global__ __launch_bounds__(kWideThreads) void cross_entropy_wide_kernel(const CrossEntropy a) {
+  constexpr int E = 16 / sizeof(T);
+  __shared__ BlockScratch red;
+  const int64_t row = blockIdx.x, label = label_of(a, row);
+  const T* const x = static_cast<const T*>(a.logits) + row * a.ld;
+  T* const d = static_cast<T*>(a.dlogits) + row * a.ldd;
+  if (label < 0 || label >= a.V) {
+    if (a.loss != nullptr && threadIdx.x == 0) a.loss[row] = 0.f;
+    if (a.dlogits != nullptr) clear_row(d, a.V, threadIdx.x, kWideThreads);
+    return;
+  }
+  const LossPieces<T, E> pieces(x, a.V, (int)label);
+  const float own = to_float(x[label]);
+  const LossStats others = stream_stats<T, E, kWideThreads>(pieces, 0, pieces.pieces, red);
+  const LossRow out(a, others, own);
+  if (a.loss != nullptr && threadIdx.x == 0) a.loss[row] = out.loss;
+  if (a.dlogits != nullptr) stream_gradient<T, E, kWideThreads>(pieces, 0, pieces.pieces, d, out);
+}
+
+// Few wide rows: a workgroup per part of a row, which leaves its statistics; then one that joins a row's and writes its part of the gradient.  (The label's
+// logit comes from the first kernel too: the gradient may be written in its place.)
+constexpr int kMostParts = 64;   // a lane for each
+
+template <typename T>
+__global__ __launch_bounds__(kPartThreads) void cross_entropy_part_kernel(const CrossEntropy a) {
+  constexpr int E = 16 / sizeof(T);
+  __shared__ BlockScratch red;
+  const int64_t row = blockIdx.x / a.parts, label = label_of(a, row);
+  const int part = (int)(blockIdx.x % a.parts);
+  if (label < 0 || label >= a.V) return;
+  const LossPieces<T, E> pieces(static_cast<const T*>(a.logits) + row * a.ld, a.V, (int)label);
+  const int share = (pieces.pieces + a.parts - 1) / a.parts, from = min(part * share, pieces.pieces), to = min(from + share, pieces.pieces);
+  LossStats* const stats = a.stats + row * (a.parts + 1);
+  const LossStats mine = stream_stats<T, E, kPartThreads>(pieces, from, to, red);
+  if (threadIdx.x != 0) return;
+  stats[part] = mine;
+  if (part == 0) stats[a.parts].m = to_float(pieces.x[label]);
+}
+
+template <typename T>
+__global__ __launch_bounds__(kPartThreads) void cross_entropy_join_kernel(const CrossEntropy a) {
+  constexpr int E = 16 / sizeof(T);
+  const int64_t row = blockIdx.x / a.parts, label = label_of(a, row);
+  const int part = (int)(blockIdx.x % a.parts), lane = threadIdx.x & 63;
+  const bool counts = label >= 0 && label < a.V;
+  const LossPieces<T, E> pieces(static_cast<const T*>(a.logits) + row * a.ld, a.V, counts ? (int)label : 0);
+  const int share = (pieces.pieces + a.parts - 1) / a.parts, from = min(part * share, pieces.pieces), to = min(from + share, pieces.pieces);
+  T* const d = static_cast<T*>(a.dlogits) + row * a.ldd;
+  if (!counts) {
+    if (part == 0 && threadIdx.x == 0 && a.loss != nullptr) a.loss[row] = 0.f;
+    if (a.dlogits != nullptr && from < to) clear_row(d + pieces.start(from), (to == pieces.pieces ? a.V : to * E) - pieces.start(from), threadIdx.x, kPartThreads);
+    return;
+  }
+  const LossStats* const stats = a.stats + row * (a.parts + 1);
+  const LossStats mine = lane < a.parts ? stats[lane] : LossStats{kLowest, 0.f};
+  const float m = wave_max_f32(mine.m);
+  const LossRow out(a, LossStats{m, wave_sum_f32(mine.S * PowerBase(m).share(PowerBase(mine.m)))}, stats[a.parts].m);
+  if (part == 0 && threadIdx.x == 0 && a.loss != nullptr) a.loss[row] = out.loss;
+  if (a.dlogits != nullptr) stream_gradient<T, E, kPartThreads>(pieces, from, to, d, out);
 }
 
 }  // namespace ngsgd

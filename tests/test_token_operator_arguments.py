@@ -64,7 +64,7 @@ def loss(lib, x=A, ld=8, type=F32, labels=A, index=I32, N=4, V=8, out=A, scale=1
 
 
 @pytest.mark.parametrize("bad", [
-    dict(type=I32), dict(type=-1), dict(index=F32), dict(index=5), dict(N=-1), dict(N=(1 << 30) + 1), dict(V=0), dict(V=(1 << 30) + 1, ld=1 << 31, ldd=1 << 31),
+    dict(type=I32), dict(type=-1), dict(index=F32), dict(index=5), dict(N=-1), dict(N=(1 << 30) + 1), dict(V=0), dict(V=(1 << 29) + 1, ld=1 << 31, ldd=1 << 31),
     dict(x=None), dict(labels=None), dict(out=None, d=None), dict(x=A + 2), dict(type=BF16, x=A + 1), dict(labels=A + 2), dict(index=I64, labels=A + 4),
     dict(out=A + 2), dict(dev_scale=A + 1), dict(d=2 * A + 2), dict(ld=7), dict(ldd=7, d=2 * A), dict(ld=-1), dict(ldd=1 << 62), dict(ldd=9), dict(ws=None),
     dict(ws=A + 64)])
@@ -78,7 +78,7 @@ def test_cross_entropy_of_no_rows(lib):
 
 def test_cross_entropy_workspace(lib):
     n = c_size_t(0)
-    for classes in (1, 2, 100, 5000, 32768, 65537, 131072, 262144, 10 ** 6, 1 << 30):
+    for classes in (1, 2, 100, 5000, 32768, 65537, 131072, 262144, 10 ** 6, 1 << 29):
         sizes = []
         for rows in (0, 1, 2, 15, 16, 17, 63, 64, 255, 256, 257, 1000, 10 ** 5, 10 ** 7, 1 << 30):
             assert lib.ngsgd_cross_entropy_workspace_bytes(rows, classes, byref(n)) == 0 and n.value % 256 == 0
@@ -86,7 +86,7 @@ def test_cross_entropy_workspace(lib):
             if rows > 0 and n.value > 0 and rows * classes < 1 << 56:
                 assert loss(lib, N=rows, V=classes, ld=classes, ldd=classes, nbytes=n.value - 1) == ng.NGSGD_ENOMEM
         assert sizes == sorted(sizes)                 # fewer rows never need more
-    for rows, classes in ((-1, 8), ((1 << 30) + 1, 8), (4, 0), (4, -1), (4, (1 << 30) + 1)):
+    for rows, classes in ((-1, 8), ((1 << 30) + 1, 8), (4, 0), (4, -1), (4, (1 << 29) + 1)):
         assert lib.ngsgd_cross_entropy_workspace_bytes(rows, classes, byref(n)) == ng.NGSGD_EINVAL
     assert lib.ngsgd_cross_entropy_workspace_bytes(4, 8, None) == ng.NGSGD_EINVAL
 
