@@ -11,8 +11,10 @@ from __future__ import annotations
 
 import ctypes
 import os
+from array import array
 from contextlib import nullcontext
 from ctypes import POINTER, byref, c_char_p, c_double, c_float, c_int, c_int32, c_int64, c_size_t, c_void_p
+from operator import attrgetter
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libngsgd.so")
@@ -97,9 +99,9 @@ _SIGNATURES = {
     "ngsgd_cross_entropy": (c_int, [c_void_p, c_int64, c_int32, c_void_p, c_int32, c_int64, c_int32, c_void_p, c_float, c_void_p,
                                     c_void_p, c_int64, c_void_p, c_size_t, c_void_p]),
     "ngsgd_grad_norm_workspace_bytes": (c_int, [c_int32, POINTER(c_size_t)]),
-    "ngsgd_grad_norm": (c_int, [c_int32, POINTER(c_int64), POINTER(c_void_p), c_int32, c_double, c_void_p, c_void_p, c_void_p,
+    "ngsgd_grad_norm": (c_int, [c_int32, c_void_p, c_void_p, c_int32, c_double, c_void_p, c_void_p, c_void_p,
                                 c_size_t, c_void_p]),
-    "ngsgd_grad_clip": (c_int, [c_int32, POINTER(c_int64), POINTER(c_void_p), c_int32, c_double, POINTER(c_void_p), c_void_p,
+    "ngsgd_grad_clip": (c_int, [c_int32, c_void_p, c_void_p, c_int32, c_double, c_void_p, c_void_p,
                                 c_void_p, c_void_p, c_size_t, c_void_p]),
     "ngsgd_adamw_workspace_bytes": (c_int, [POINTER(ngsgd_adamw_config), POINTER(c_size_t)]),
     "ngsgd_adamw_create": (c_int, [POINTER(ngsgd_adamw_config), c_void_p, c_size_t, POINTER(c_void_p)]),
@@ -309,13 +311,18 @@ def _check_dense(t, name, device, dtype=None, numel=None):
         raise ValueError(f"{name} has {t.numel()} elements, not {numel}")
 
 
+def _current_raw_stream(index):
+    """hipStream_t of the device's current stream, without an object for it where torch has a call for that."""
+    get = getattr(_torch._C, "_cuda_getCurrentRawStream", None)
+    return _torch.cuda.current_stream(index).cuda_stream if get is None else get(index)
+
+
 def _raw_stream(stream, device, workspace=None, home=None):
     """The stream's hipStream_t.  A workspace that is used on another stream than the one it was allocated on (`home`) is not given to
     anybody else before that stream is done with it, though its owner may be gone."""
-    stream = _torch.cuda.current_stream(device.index) if stream is None else stream
-    raw = stream.cuda_stream
+    raw = _current_raw_stream(device.index) if stream is None else stream.cuda_stream
     if workspace is not None and raw != home:
-        workspace.record_stream(stream)
+        workspace.record_stream(_torch.cuda.current_stream(device.index) if stream is None else stream)
     return raw
 
 
@@ -323,9 +330,12 @@ def _address(t):
     return None if t is None else t.data_ptr()
 
 
+_HERE_AND_NOW = nullcontext()
+
+
 def _allocate_on(stream):
     """Outputs are allocated on the stream that writes them."""
-    return nullcontext() if stream is None else _torch.cuda.stream(stream)
+    return _HERE_AND_NOW if stream is None else _torch.cuda.stream(stream)
 
 
 class LayerNorm:
@@ -608,6 +618,14 @@ class CrossEntropy:
         return self._call(logits, labels, scale, loss, dlogits, True, stream)
 
 
+_DTYPE = attrgetter("dtype")
+
+
+def _host(numbers):
+    """Address of an array.array's numbers."""
+    return numbers.buffer_info()[0]
+
+
 class GradientNorm:
     """ngsgd_grad_norm / ngsgd_grad_clip: the norm of many gradients as one vector, and clipping, on the current device.
 
@@ -633,28 +651,35 @@ class GradientNorm:
         self.grad_dtype = like[0].dtype if grad_dtype is None else grad_dtype
         self.type = _type_of(self.grad_dtype)
         self.sizes = [p.numel() for p in like]
-        self._sizes = (c_int64 * n)(*self.sizes)
-        self._grads, self._out = (c_void_p * n)(), (c_void_p * n)()
+        self._sizes = array("q", self.sizes)
         nbytes = c_size_t(0)
         _check(self.lib.ngsgd_grad_norm_workspace_bytes(n, byref(nbytes)), "ngsgd_grad_norm_workspace_bytes")
         self.workspace_bytes = nbytes.value
         self.workspace = torch.empty(nbytes.value, dtype=torch.uint8, device=self.device)
         self._home = _raw_stream(None, self.device)
 
-    def _addresses(self, tensors, name, array):
-        dtype, index, sizes, addresses = self.grad_dtype, self.device.index, self.sizes, []
+    def _addresses(self, tensors, name):
+        """The tensors' addresses (0: does not count)."""
+        dtype, index, sizes = self.grad_dtype, self.device.index, self.sizes
         if len(tensors) != len(sizes):
             raise ValueError(f"{len(tensors)} {name}s for {len(sizes)} tensors")
+        tensor = _torch.Tensor
+        try:      # all at once: half the time of one by one
+            if (list(map(tensor.numel, tensors)) == sizes and all(map(tensor.is_contiguous, tensors)) and set(map(_DTYPE, tensors)) == {dtype}
+                    and set(map(tensor.get_device, tensors)) == {index}):
+                return array("Q", map(tensor.data_ptr, tensors))
+        except TypeError:
+            pass  # None among them
+        addresses = array("Q")
         for t, size in zip(tensors, sizes):
             if t is None or size == 0:
-                addresses.append(None)
+                addresses.append(0)
                 continue
             if t.dtype != dtype or t.numel() != size or t.get_device() != index or not t.is_contiguous():
                 raise ValueError(f"{name} {len(addresses)}: {t.dtype}, {t.numel()} elements on {t.device}, for {dtype}, {size} on "
                                  f"{self.device}, dense")
             addresses.append(t.data_ptr())
-        array[:] = addresses
-        return array
+        return addresses
 
     def _results(self, norm, factor, stream):
         for name, t in (("norm", norm), ("factor", factor)):
@@ -672,9 +697,9 @@ class GradientNorm:
         """(norm, factor), float32 tensors of one element: the norm of all gradients, and max_norm / norm where the norm is above max_norm, else 1, which
         AdamW.step takes as grad_scale.  grads: a dense tensor of grad_dtype for each size, or None for one that does not count."""
         _current_device(self.device)
-        grads = self._addresses(grads, "gradient", self._grads)
+        grads = self._addresses(grads, "gradient")
         norm, factor = self._results(norm, factor, stream)
-        _check(self.lib.ngsgd_grad_norm(len(self.sizes), self._sizes, grads, self.type, max_norm, norm.data_ptr(), factor.data_ptr(),
+        _check(self.lib.ngsgd_grad_norm(len(self.sizes), _host(self._sizes), _host(grads), self.type, max_norm, norm.data_ptr(), factor.data_ptr(),
                                         self.workspace.data_ptr(), self.workspace_bytes,
                                         _raw_stream(stream, self.device, self.workspace, self._home)), "ngsgd_grad_norm")
         return norm, factor
@@ -683,12 +708,13 @@ class GradientNorm:
         """(norm, factor); every gradient is multiplied by the factor, in place or into `out` (a tensor for each gradient, which may be it)."""
         _current_device(self.device)
         if out is not None:
-            if any(g is not None and size != 0 and o is None for g, o, size in zip(grads, out, self.sizes)):
-                raise ValueError("out has no tensor for a gradient")
-            out = self._addresses(out, "output", self._out)
-        grads = self._addresses(grads, "gradient", self._grads)
+            out = self._addresses(out, "output")
+        grads = self._addresses(grads, "gradient")
+        if out is not None and 0 in out and any(g and not o for g, o in zip(grads, out)):
+            raise ValueError("out has no tensor for a gradient")
         norm, factor = self._results(norm, factor, stream)
-        _check(self.lib.ngsgd_grad_clip(len(self.sizes), self._sizes, grads, self.type, max_norm, out, norm.data_ptr(), factor.data_ptr(),
+        _check(self.lib.ngsgd_grad_clip(len(self.sizes), _host(self._sizes), _host(grads), self.type, max_norm,
+                                        None if out is None else _host(out), norm.data_ptr(), factor.data_ptr(),
                                         self.workspace.data_ptr(), self.workspace_bytes,
                                         _raw_stream(stream, self.device, self.workspace, self._home)), "ngsgd_grad_clip")
         return norm, factor

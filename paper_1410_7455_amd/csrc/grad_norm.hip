@@ -12,10 +12,7 @@ namespace {
 constexpr int32_t kMostTensors = 1 << 20;
 constexpr int64_t kMostElements = (int64_t)1 << 40;
 
-// Sums of the pieces of all launches: one launch has at most kNormPieces full ones, and one more for each tensor.
-size_t most_parts(const int32_t n_tensors) {
-  return (size_t)((n_tensors + kNormTensors - 1) / kNormTensors) * kNormPieces + (size_t)n_tensors;
-}
+size_t most_parts(const int32_t n_tensors) { return (size_t)((n_tensors + kNormTensors - 1) / kNormTensors) * kNormParts; }
 
 struct Workspace {
   NormResult* result;
@@ -29,23 +26,24 @@ Workspace layout(Carver& c, const int32_t n_tensors) {
 }
 
 // The tensors from `first` on that one launch takes; returns where the next one goes on.  Empty ones are left out.
-int fill(NormTensors& a, int& pieces, int first, const int32_t n_tensors, const int64_t* sizes, const void* const* grads, void* const* out) {
-  a.count = 0;
+int fill(NormTensors& a, int first, const int32_t n_tensors, const int64_t* sizes, const void* const* grads, void* const* out) {
+  int count = 0;
   int64_t total = 0;
-  for (; first < n_tensors && a.count < kNormTensors; ++first) {
+  for (; first < n_tensors && count < kNormTensors; ++first) {
     if (sizes[first] == 0 || grads[first] == nullptr) continue;
-    a.g[a.count] = grads[first];
-    a.out[a.count] = out != nullptr ? out[first] : const_cast<void*>(grads[first]);
-    a.n[a.count++] = sizes[first];
+    a.g[count] = grads[first];
+    a.out[count] = out != nullptr ? out[first] : const_cast<void*>(grads[first]);
+    a.n[count++] = sizes[first];
     total += sizes[first];
   }
   const int64_t share = (total + kNormPieces - 1) / kNormPieces;
   a.piece = std::max<int64_t>(kNormLeast, (share + kNormThreads * 8 - 1) / (kNormThreads * 8) * (kNormThreads * 8));
-  pieces = 0;
-  for (int i = 0; i < a.count; ++i) {
-    a.first[i] = pieces;
-    pieces += (int)((a.n[i] + a.piece - 1) / a.piece);
+  a.pieces = 0;
+  for (int i = 0; i < count; ++i) {
+    a.first[i] = a.pieces;
+    a.pieces += (int)((a.n[i] + a.piece - 1) / a.piece);
   }
+  for (int i = count; i < kNormTensors; ++i) a.first[i] = INT32_MAX;
   return first;
 }
 
@@ -65,28 +63,40 @@ int run(int32_t n_tensors, const int64_t* sizes, const void* const* grads, int32
   NG_TRY(check_workspace(dev_workspace, workspace_bytes, need));
   Carver c(dev_workspace);
   const Workspace w = layout(c, n_tensors);
+  const NormOut to{dev_norm, dev_factor};
   NormTensors a;
-  int pieces = 0, parts = 0;
+  int parts = 0, launches = 0;
   for (int first = 0; first < n_tensors;) {
-    first = fill(a, pieces, first, n_tensors, sizes, grads, out);
-    if (pieces == 0) continue;
-    with_type(type, [&](auto t) {
-      hipLaunchKernelGGL(grad_norm_kernel<decltype(t)>, dim3(pieces), dim3(kNormThreads), 0, s, a, w.parts + parts);
-      return 0;
-    });
-    LAUNCH_CHECK();
-    parts += pieces;
+    first = fill(a, first, n_tensors, sizes, grads, out);
+    if (first == n_tensors && launches == 0 && a.pieces <= kNormSmallPieces)
+      return with_type(type, [&](auto t) {
+        hipLaunchKernelGGL(grad_small_kernel<decltype(t)>, dim3(1), dim3(kNormSmallThreads), 0, s, a, clip, max_norm, to);
+        LAUNCH_CHECK();
+        return NGSGD_OK;
+      });
+    if (a.pieces == 0) continue;
+    NG_TRY(with_type(type, [&](auto t) {
+      hipLaunchKernelGGL(grad_norm_kernel<decltype(t)>, dim3(a.pieces), dim3(kNormThreads), 0, s, a, w.parts + parts);
+      LAUNCH_CHECK();
+      return NGSGD_OK;
+    }));
+    parts += a.pieces;
+    ++launches;
   }
-  hipLaunchKernelGGL(grad_norm_finish_kernel, dim3(1), dim3(1024), 0, s, w.parts, parts, max_norm, w.result, dev_norm, dev_factor);
-  LAUNCH_CHECK();
-  for (int first = 0; clip && first < n_tensors;) {
-    first = fill(a, pieces, first, n_tensors, sizes, grads, out);
-    if (pieces == 0) continue;
-    with_type(type, [&](auto t) {
-      hipLaunchKernelGGL(grad_clip_kernel<decltype(t)>, dim3(pieces), dim3(kNormThreads), 0, s, a, w.result);
-      return 0;
-    });
+  // the sums of one launch are joined by every workgroup that clips (2048 of them: 2 us, a launch for it 4)
+  const bool join = clip && launches == 1;
+  if (!join) {
+    hipLaunchKernelGGL(grad_norm_finish_kernel, dim3(1), dim3(1024), 0, s, w.parts, parts, max_norm, w.result, to);
     LAUNCH_CHECK();
+  }
+  for (int first = 0; clip && first < n_tensors;) {
+    first = fill(a, first, n_tensors, sizes, grads, out);
+    if (a.pieces == 0) continue;
+    NG_TRY(with_type(type, [&](auto t) {
+      hipLaunchKernelGGL(grad_clip_kernel<decltype(t)>, dim3(a.pieces), dim3(kNormThreads), 0, s, a, w.parts, join ? parts : 0, max_norm, w.result, to);
+      LAUNCH_CHECK();
+      return NGSGD_OK;
+    }));
   }
   return NGSGD_OK;
 }

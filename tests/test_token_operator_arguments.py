@@ -152,7 +152,7 @@ def test_binding_refuses_tensors_off_the_device(monkeypatch):
         ng.GradientNorm([])
     e = made(torch, ng.Embedding, max_tokens=4, vocabulary=8, dim=8, scale=1.0)
     c = made(torch, ng.CrossEntropy, max_rows=4, classes=8)
-    g = made(torch, ng.GradientNorm, sizes=[4], grad_dtype=torch.float32, _grads=(c_void_p * 1)(), _out=(c_void_p * 1)())
+    g = made(torch, ng.GradientNorm, sizes=[4], grad_dtype=torch.float32)
     tokens, x = torch.zeros(4, dtype=torch.int32), torch.zeros(4, 8)
     for call in (lambda: e.forward(tokens, x), lambda: e.backward(x, tokens), lambda: c.forward(x, tokens), lambda: c.gradient(x, tokens),
                  lambda: g.norm([torch.zeros(4)]), lambda: g.clip([torch.zeros(4)], 1.0), lambda: g.norm([])):
