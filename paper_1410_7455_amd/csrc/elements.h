@@ -37,6 +37,17 @@ __device__ __forceinline__ float to_float(const T x) { return static_cast<float>
 template <typename T>
 __device__ __forceinline__ T from_float(const float x) { return static_cast<T>(x); }
 
+// The same for what no kernel reads soon: it does not displace what the caches hold.
+template <typename T, int V>
+__device__ __forceinline__ void store_pack_past(T* p, const Pack<T, V>& v) {
+  if constexpr (sizeof(v) != 16)
+    *reinterpret_cast<Pack<T, V>*>(p) = v;
+  else if constexpr (sizeof(T) == 2)
+    __builtin_nontemporal_store(__builtin_bit_cast(U32x4, v), reinterpret_cast<U32x4On2*>(p));
+  else
+    __builtin_nontemporal_store(__builtin_bit_cast(U32x4, v), reinterpret_cast<U32x4On4*>(p));
+}
+
 // A number in fp32 that the compiler does not merge with the conversion behind it: a product that is rounded to 16 bits in one instruction, without the
 // step over fp32, may differ by a step from one that is not, and it does so for some of a thread's elements only.
 __device__ __forceinline__ float as_f32(float x) {

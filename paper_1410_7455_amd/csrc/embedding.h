@@ -23,7 +23,9 @@ struct EmbeddingForward {
   float scale;
   void* y;
   int64_t ldy;
-  int lanes;         // threads that share a row, a power of two
+  int slabs;         // a row is cut into so many slabs,
+  int slab;          // of so many pieces;
+  int lanes;         // threads that share one, a power of two
 };
 
 // A token that is sorted: its row of the table (V: padding, which goes last) and its place among the tokens.
@@ -58,31 +60,33 @@ __device__ __forceinline__ int64_t token_of(const I* tokens, const int64_t i, co
 }
 
 // A thread has pieces of E elements of kLookupRows rows in flight: their tokens first, then the table's rows.  The last piece of a row is
-// moved back to end with it (its first elements are written twice, with the same values).
-template <typename W, typename T, typename I, int E>
+// moved back to end with it (its first elements are written twice, with the same values).  PAST: y is written past the caches.  (The compiler would make
+// one ordinary store of the two kinds behind a condition.)
+template <typename W, typename T, typename I, int E, bool PAST>
 __global__ __launch_bounds__(kLookupThreads) void embedding_forward_kernel(const EmbeddingForward a) {
   const int lane = threadIdx.x & (a.lanes - 1), per_round = kLookupThreads / a.lanes;
-  const int64_t first = (int64_t)blockIdx.x * per_round * kLookupRows + threadIdx.x / a.lanes;
-  int64_t token[kLookupRows];
+  const int64_t first = (int64_t)(blockIdx.x / a.slabs) * per_round * kLookupRows + threadIdx.x / a.lanes;
+  I raw[kLookupRows];
 #pragma unroll
-  for (int k = 0; k < kLookupRows; ++k) {
-    const int64_t row = first + k * per_round;
-    token[k] = row < a.N ? token_of(static_cast<const I*>(a.tokens), row, a.V) : -2;
-  }
-  const int pieces = (a.D + E - 1) / E;
-  for (int p = lane; p < pieces; p += a.lanes) {
+  for (int k = 0; k < kLookupRows; ++k) raw[k] = static_cast<const I*>(a.tokens)[min(first + k * per_round, a.N - 1)];
+  const int pieces = (a.D + E - 1) / E, from = (int)(blockIdx.x % a.slabs) * a.slab, to = min(from + a.slab, pieces);
+  for (int p = from + lane; p < to; p += a.lanes) {
     const int at = min(p * E, a.D - E);
     Pack<W, E> w[kLookupRows];
 #pragma unroll
-    for (int k = 0; k < kLookupRows; ++k)
-      if (token[k] >= 0) w[k] = *reinterpret_cast<const Pack<W, E>*>(static_cast<const W*>(a.table) + token[k] * a.ldt + at);
+    for (int k = 0; k < kLookupRows; ++k) {
+      const bool named = (uint64_t)(int64_t)raw[k] < (uint64_t)a.V;
+      w[k] = *reinterpret_cast<const Pack<W, E>*>(static_cast<const W*>(a.table) + (named ? (int64_t)raw[k] : 0) * a.ldt + at);
+    }
 #pragma unroll
     for (int k = 0; k < kLookupRows; ++k) {
-      if (token[k] == -2) continue;
+      const bool named = (uint64_t)(int64_t)raw[k] < (uint64_t)a.V;
+      if (first + k * per_round >= a.N) continue;
       Pack<T, E> y;
 #pragma unroll
-      for (int j = 0; j < E; ++j) y.v[j] = from_float<T>(token[k] >= 0 ? as_f32(a.scale * to_float(w[k].v[j])) : 0.f);
-      store_pack(static_cast<T*>(a.y) + (first + k * per_round) * a.ldy + at, y);
+      for (int j = 0; j < E; ++j) y.v[j] = from_float<T>(named ? as_f32(a.scale * to_float(w[k].v[j])) : 0.f);
+      T* const to = static_cast<T*>(a.y) + (first + k * per_round) * a.ldy + at;
+      if constexpr (PAST) store_pack_past(to, y); else store_pack(to, y);
     }
   }
 }
@@ -197,11 +201,10 @@ __global__ __launch_bounds__(1024) void embedding_scan_kernel(const EmbeddingSor
 }
 
 // Places: digits in order, tiles in order within a digit, a tile's tokens in order within that.  A wavefront ranks 64 tokens at a time: lanes
-// with the same digit find each other by one ballot a bit.  Then four neighbouring digits belong to a thread.
+// with the same digit find each other by one ballot a bit.  Then the digits are dealt to the threads, neighbours to each.
 template <typename I, bool FIRST, int THREADS>
 __global__ __launch_bounds__(THREADS) void embedding_scatter_kernel(const EmbeddingSort a) {
-  constexpr int kWaves = THREADS / 64, kOwn = 4;
-  static_assert(THREADS * kOwn >= kSortBins);
+  constexpr int kWaves = THREADS / 64, kOwn = kSortBins / THREADS;
   __shared__ uint32_t bins[kWaves * kSortBins];   // of each wavefront: its count, then where its next token with that digit goes
   __shared__ uint32_t waves[kWaves];
   using Counts = Pack<uint32_t, kOwn>;
@@ -277,14 +280,15 @@ __global__ __launch_bounds__(THREADS) void embedding_scatter_kernel(const Embedd
   if (owns) {
 #pragma unroll
     for (int k = 0; k < kOwn; ++k) {
-      uint32_t at = below + before.v[k];
+      uint32_t at = below + before.v[k], here[kWaves];
       below += total.v[k];
+      uint32_t* const bin = bins + threadIdx.x * kOwn + k;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) here[w] = bin[w * a.bins];
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) {
-        uint32_t* const bin = bins + w * a.bins + threadIdx.x * kOwn + k;
-        const uint32_t here = *bin;
-        *bin = at;
-        at += here;
+        bin[w * a.bins] = at;
+        at += here[w];
       }
     }
   }
