@@ -244,15 +244,33 @@ __global__ __launch_bounds__(THREADS, P <= 8 ? 8 : 4) void cross_entropy_kernel(
 // ---- rows that are read twice --------------------------------------------------------------------------
 constexpr int kWideThreads = 1024, kPartThreads = 256, kStreamAhead = 4;
 
-// Statistics of pieces [from, to), by all threads of a workgroup: each has its own largest logit, and its sum in units of that.
+// Adds K pieces to a thread's statistics: it has its own largest logit, and its sum in units of that.
+template <typename T, int E, int K>
+__device__ __forceinline__ void add_pieces(LossStats& mine, Pack<T, E> (&v)[K]) {
+  float m = mine.m;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    keep_packed(v[k]);
+    m = fmaxf(m, largest_of(v[k]));
+    keep_packed(v[k]);
+  }
+  const PowerBase base(m);
+  if (m != mine.m) mine = LossStats{m, mine.S * base.share(PowerBase(mine.m))};
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+#pragma unroll
+    for (int j = 0; j < E; ++j) mine.S += base.power(to_float(v[k].v[j]));
+    keep_packed(v[k]);
+  }
+}
+// Statistics of pieces [from, to) of a thread of a workgroup, and of all of them.
 template <typename T, int E, int THREADS>
-__device__ __forceinline__ LossStats stream_stats(const LossPieces<T, E>& pieces, const int from, const int to, BlockScratch& red) {
+__device__ __forceinline__ LossStats stream_stats(const LossPieces<T, E>& pieces, const int from, const int to) {
   LossStats mine{kLowest, 0.f};
   for (int p = from + threadIdx.x; p < to; p += THREADS * kStreamAhead) {
     Pack<T, E> v[kStreamAhead];
 #pragma unroll
     for (int k = 0; k < kStreamAhead; ++k) v[k] = pieces.load(min(p + k * THREADS, to - 1));
-    float m = mine.m;
 #pragma unroll
     for (int k = 0; k < kStreamAhead; ++k) {
       if (p + k * THREADS >= to) {
@@ -260,15 +278,13 @@ __device__ __forceinline__ LossStats stream_stats(const LossPieces<T, E>& pieces
         for (int j = 0; j < E; ++j) v[k].v[j] = from_float<T>(-INFINITY);
       }
       pieces.mask(v[k], p + k * THREADS);
-      m = fmaxf(m, largest_of(v[k]));
     }
-    const PowerBase base(m);
-    if (m != mine.m) mine = LossStats{m, mine.S * base.share(PowerBase(mine.m))};
-#pragma unroll
-    for (int k = 0; k < kStreamAhead; ++k)
-#pragma unroll
-      for (int j = 0; j < E; ++j) mine.S += base.power(to_float(v[k].v[j]));
+    add_pieces(mine, v);
   }
+  return mine;
+}
+template <int THREADS>
+__device__ __forceinline__ LossStats join_stats(const LossStats& mine, BlockScratch& red) {
   const float m = group_max<THREADS>(mine.m, red);
   return LossStats{m, group_sum<THREADS>(mine.S * PowerBase(m).share(PowerBase(mine.m)), red)};
 }
@@ -284,7 +300,8 @@ __device__ __forceinline__ void stream_gradient(const LossPieces<T, E>& pieces, 
   }
 }
 
-// A workgroup per row.
+// A workgroup per row, which holds the last kHeld pieces a thread and reads the others twice, the second time from a cache.
+constexpr int kHeld = 12, kHeldPieces = kHeld * kWideThreads;
 template <typename T>
 __global__ __launch_bounds__(kWideThreads) void cross_entropy_wide_kernel(const CrossEntropy a) {
   constexpr int E = 16 / sizeof(T);
@@ -292,17 +309,29 @@ __global__ __launch_bounds__(kWideThreads) void cross_entropy_wide_kernel(const 
   const int64_t row = blockIdx.x, label = label_of(a, row);
   const T* const x = static_cast<const T*>(a.logits) + row * a.ld;
   T* const d = static_cast<T*>(a.dlogits) + row * a.ldd;
+  int thread = threadIdx.x;
   if (label < 0 || label >= a.V) {
-    if (a.loss != nullptr && threadIdx.x == 0) a.loss[row] = 0.f;
-    if (a.dlogits != nullptr) clear_row(d, a.V, threadIdx.x, kWideThreads);
+    if (a.loss != nullptr && thread == 0) a.loss[row] = 0.f;
+    if (a.dlogits != nullptr) clear_row(d, a.V, thread, kWideThreads);
     return;
   }
   const LossPieces<T, E> pieces(x, a.V, (int)label);
   const float own = to_float(x[label]);
-  const LossStats others = stream_stats<T, E, kWideThreads>(pieces, 0, pieces.pieces, red);
-  const LossRow out(a, others, own);
-  if (a.loss != nullptr && threadIdx.x == 0) a.loss[row] = out.loss;
-  if (a.dlogits != nullptr) stream_gradient<T, E, kWideThreads>(pieces, 0, pieces.pieces, d, out);
+  const int first = pieces.pieces - kHeldPieces;   // (there are more than that)
+  Pack<T, E> v[kHeld];
+#pragma unroll
+  for (int p = 0; p < kHeld; ++p) v[p] = pieces.load(first + p * kWideThreads + thread);
+  LossStats mine = stream_stats<T, E, kWideThreads>(pieces, 0, first);
+#pragma unroll
+  for (int p = 0; p < kHeld; ++p) pieces.mask(v[p], first + p * kWideThreads + thread);
+  add_pieces(mine, v);
+  const LossRow out(a, join_stats<kWideThreads>(mine, red), own);
+  if (a.loss != nullptr && thread == 0) a.loss[row] = out.loss;
+  if (a.dlogits == nullptr) return;
+  asm("" : "+v"(thread));
+#pragma unroll
+  for (int p = 0; p < kHeld; ++p) pieces.store(d, v[p], first + p * kWideThreads + thread, out);
+  stream_gradient<T, E, kWideThreads>(pieces, 0, first, d, out);
 }
 
 // Few wide rows: a workgroup per part of a row, which leaves its statistics; then one that joins a row's and writes its part of the gradient.  (The label's
@@ -319,7 +348,7 @@ __global__ __launch_bounds__(kPartThreads) void cross_entropy_part_kernel(const 
   const LossPieces<T, E> pieces(static_cast<const T*>(a.logits) + row * a.ld, a.V, (int)label);
   const int share = (pieces.pieces + a.parts - 1) / a.parts, from = min(part * share, pieces.pieces), to = min(from + share, pieces.pieces);
   LossStats* const stats = a.stats + row * (a.parts + 1);
-  const LossStats mine = stream_stats<T, E, kPartThreads>(pieces, from, to, red);
+  const LossStats mine = join_stats<kPartThreads>(stream_stats<T, E, kPartThreads>(pieces, from, to), red);
   if (threadIdx.x != 0) return;
   stats[part] = mine;
   if (part == 0) stats[a.parts].m = to_float(pieces.x[label]);

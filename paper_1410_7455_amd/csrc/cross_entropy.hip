@@ -13,7 +13,8 @@ constexpr int64_t kMostRows = (int64_t)1 << 30;
 constexpr int32_t kMostClasses = 1 << 29;   // (offsets in a row are 32 bits of bytes)
 constexpr int64_t kLaunchRows = (int64_t)1 << 21;
 
-constexpr int kRegisterPieces = 16384;     // of 16 bytes: wider rows are read twice
+constexpr int kRegisterPieces = 16384;     // of 16 bytes: of wider rows some are read twice
+static_assert(kRegisterPieces >= kHeldPieces);
 constexpr int kPartPieces = 4096;          // rows of more are cut into parts
 constexpr int kPartRows = 128;             // if there are fewer than so many,
 constexpr int kPartGroups = 1024;          // into about so many workgroups' worth
