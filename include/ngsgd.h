@@ -293,8 +293,8 @@ int ngsgd_grad_norm(int32_t n_tensors, const int64_t* sizes, const void* const* 
                     float* dev_norm, float* dev_factor, void* dev_workspace, size_t workspace_bytes, void* hip_stream);
 
 /* The same, and every element times the factor, rounded once, to dev_out[i] (of the same type and size; NULL only where dev_grads[i] is or the
- * size is 0); dev_out NULL: in place, where with a factor of 1 nothing is read again or written.  dev_out[i] may be dev_grads[i]; other
- * overlaps are not allowed. */
+ * size is 0); dev_out NULL: in place, where with a factor of 1 nothing is read again or written.  dev_out[i] may be dev_grads[i]; where
+ * outputs share memory with each other or with another gradient the call is refused (NGSGD_EINVAL). */
 int ngsgd_grad_clip(int32_t n_tensors, const int64_t* sizes, const void* const* dev_grads, int32_t type, double max_norm,
                     void* const* dev_out, float* dev_norm, float* dev_factor, void* dev_workspace,
                     size_t workspace_bytes, void* hip_stream);

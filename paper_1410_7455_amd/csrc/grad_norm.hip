@@ -2,6 +2,8 @@
 #include "grad_norm.h"
 
 #include <algorithm>
+#include <new>
+#include <vector>
 
 #include "host.h"
 
@@ -47,6 +49,32 @@ int fill(NormTensors& a, int first, const int32_t n_tensors, const int64_t* size
   return first;
 }
 
+// Outputs share memory with nothing but their own gradients: otherwise a factor would be applied twice, or to what another workgroup has written.
+bool outputs_apart(const int32_t n_tensors, const int64_t* sizes, const void* const* grads, const int type, void* const* out) {
+  struct Span {
+    uintptr_t from, to;
+    int index;
+  };
+  const auto span = [&](const void* p, const int i) {
+    const uintptr_t from = reinterpret_cast<uintptr_t>(p);
+    return Span{from, from + (uintptr_t)(sizes[i] * type_bytes(type)), i};
+  };
+  std::vector<Span> outs;
+  for (int i = 0; i < n_tensors; ++i)
+    if (sizes[i] > 0 && grads[i] != nullptr) outs.push_back(span(out != nullptr ? out[i] : grads[i], i));
+  std::sort(outs.begin(), outs.end(), [](const Span& a, const Span& b) { return a.from < b.from; });
+  for (size_t k = 1; k < outs.size(); ++k)
+    if (outs[k].from < outs[k - 1].to) return false;
+  for (int i = 0; out != nullptr && i < n_tensors; ++i) {
+    if (sizes[i] == 0 || grads[i] == nullptr) continue;
+    const Span g = span(grads[i], i);
+    for (auto o = std::upper_bound(outs.begin(), outs.end(), g.from, [](const uintptr_t at, const Span& b) { return at < b.to; });
+         o != outs.end() && o->from < g.to; ++o)
+      if (o->index != i || o->from != g.from) return false;
+  }
+  return true;
+}
+
 template <typename F>
 int with_type(const int type, F f) { return type == NGSGD_FLOAT32 ? f(float()) : type == NGSGD_BFLOAT16 ? f(bf16()) : f(fp16()); }
 
@@ -61,6 +89,13 @@ int run(int32_t n_tensors, const int64_t* sizes, const void* const* grads, int32
     if (out != nullptr && sizes[i] > 0 && grads[i] != nullptr && (out[i] == nullptr || !on_element(out[i], type))) return NGSGD_EINVAL;
   }
   NG_TRY(check_workspace(dev_workspace, workspace_bytes, need));
+  if (clip) {
+    try {
+      if (!outputs_apart(n_tensors, sizes, grads, type, out)) return NGSGD_EINVAL;
+    } catch (const std::bad_alloc&) {   // no host memory for the addresses
+      return NGSGD_ENOMEM;
+    }
+  }
   Carver c(dev_workspace);
   const Workspace w = layout(c, n_tensors);
   const NormOut to{dev_norm, dev_factor};

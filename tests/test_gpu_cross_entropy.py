@@ -132,14 +132,60 @@ def test_rows(ngsgd, N, V):
     check(torch, x, y, 2.0, loss, d)
 
 
+@pytest.mark.parametrize("V,dtype", [(32769, "float16"), (65536, "bfloat16"), (65537, "float16"), (100003, "bfloat16"), (131072, "bfloat16"), (131073, "float16"),
+                                     (150001, "bfloat16"), (32769, "float32"), (65536, "float32"), (65537, "float32"), (90001, "float32")])
+def test_wide_rows_of_a_workgroup(ngsgd, V, dtype):
+    """As many rows as are not cut into parts: held in registers, and wider than those.  Among them rows that are decided, masked, empty or not numbers."""
+    import torch
+    dtype = getattr(torch, dtype)
+    rng = np.random.default_rng(V)
+    N, low = 130, float(torch.finfo(dtype).min)
+    labels, y = make_labels(torch, rng, N, V, "int64")
+    y[:10] = rng.integers(0, V, 10)
+    y[3], y[4] = V - 1, 0
+    labels[:10] = torch.from_numpy(y[:10])
+    x = logits_of(rng, N, V, y)
+    x[0, y[0]] = 50.0
+    x[1] = -np.inf
+    x[2, ::2] = -np.inf
+    x[2, y[2]] = 1.0
+    x[3, V // 2], x[4, V - 1] = np.nan, np.inf
+    x[5] = low
+    x[6, np.arange(V) != y[6]] = low
+    x[7, y[7]] = -np.inf
+    pad = V % 2 + 1
+    x = matrix(torch, x, dtype, pad, 1)
+    ce = ngsgd.CrossEntropy(N, V)
+    loss, d = ce.gradient(x, labels, scale=1.5)
+    check(torch, x, y, 1.5, loss, d)
+    assert bool(loss[[1, 3, 4]].isnan().all()) and float(loss[5]) == pytest.approx(np.log(V), rel=1e-6) and float(loss[0]) > 0
+    assert torch.equal(torch.nan_to_num(ce.forward(x, labels), nan=-5.0), torch.nan_to_num(loss, nan=-5.0))
+    kept = x.clone()
+    again, _ = ce.gradient(x, labels, scale=1.5, dlogits=x)
+    assert torch.equal(x.nan_to_num(), d.nan_to_num()) and torch.equal(again.nan_to_num(), loss.nan_to_num())
+    assert bool((between_rows(x, pad) == 77).all())
+    few = ngsgd.CrossEntropy(20, V).gradient(kept[:20], labels[:20], scale=1.5)          # the same rows in parts
+    check(torch, kept[:20], y[:20], 1.5, *few)
+
+
+def test_very_wide_rows(ngsgd):
+    import torch
+    rng = np.random.default_rng(4)
+    for N, V in ((1, 3_000_001), (2, 2_500_000)):
+        labels, y = make_labels(torch, rng, N, V, "int64", ignored=0.0)
+        x = matrix(torch, logits_of(rng, N, V, y), torch.bfloat16)
+        loss, d = ngsgd.CrossEntropy(N, V).gradient(x, labels)
+        check(torch, x, y, 1.0, loss, d)
+
+
 def test_many_rows(ngsgd):
     import torch
     rng = np.random.default_rng(1)
-    N, V = 200003, 11
-    labels, y = make_labels(torch, rng, N, V, "int32")
-    x = matrix(torch, logits_of(rng, N, V, y), torch.float32)
-    loss, d = ngsgd.CrossEntropy(N, V).gradient(x, labels)
-    check(torch, x, y, 1.0, loss, d)
+    for N, V in ((200003, 11), (2 ** 21 + 100, 3)):      # the second one: more than a launch takes
+        labels, y = make_labels(torch, rng, N, V, "int32")
+        x = matrix(torch, logits_of(rng, N, V, y), torch.float32)
+        loss, d = ngsgd.CrossEntropy(N, V).gradient(x, labels)
+        check(torch, x, y, 1.0, loss, d)
 
 
 @pytest.mark.parametrize("V", [9, 300, 5000, 40000, 140000])

@@ -126,6 +126,38 @@ def test_counts(ngsgd, N, V, law):
         check_backward(torch, dy, t, V, 0.5, e.backward(dy, tokens, dtype=torch.float32))
 
 
+@pytest.mark.parametrize("N,V,D", [(262144, 5000, 8), (262145, 131072, 8), (300007, 70, 12), (1000003, 2 ** 20 + 1, 5), (20000, 3, 8), (9000, 2 ** 21 + 5, 4),
+                                   (129, 600011, 8), (128, 600011, 8), (500, 1500007, 3)])
+def test_many_tokens_and_large_tables(ngsgd, N, V, D):
+    """More tiles than a workgroup adds up itself; digits of one to three passes; wavefronts that clear 64 rows and more."""
+    import torch
+    rng = np.random.default_rng(N)
+    e = ngsgd.Embedding(N, V, D)
+    for law in ("zipf", "uniform", "last"):
+        tokens, t = make_tokens(torch, rng, N, V, "int64", law, 0.05)
+        dy = matrix(torch, rng.standard_normal((N, D)), torch.float32)
+        check_backward(torch, dy, t, V, 1.0, e.backward(dy, tokens))
+
+
+@pytest.mark.parametrize("N,D,types", [(3000, 8192, ("float32", "float32")), (4099, 4097, ("bfloat16", "float32")), (2100, 8192, ("bfloat16", "bfloat16")),
+                                       (5003, 5001, ("float16", "float32")), (16411, 1024, ("bfloat16", "bfloat16")), (40000, 257, ("float32", "float32"))])
+def test_lookups_of_large_rows(ngsgd, N, D, types):
+    """Rows in slabs, and outputs that are written past the caches."""
+    import torch
+    rng = np.random.default_rng(D)
+    V = 333
+    dtype, ttype = (getattr(torch, t) for t in types)
+    e = ngsgd.Embedding(N, V, D, scale=0.3)
+    tokens, t = make_tokens(torch, rng, N, V, "int32")
+    for pad in (0, 3):
+        table = matrix(torch, rng.standard_normal((V, D)), ttype, pad, pad)
+        y = e.forward(tokens, table, dtype=dtype)
+        named = torch.from_numpy((t >= 0) & (t < V)).cuda()
+        want = table.double()[torch.where(named, tokens.long(), 0)] * float(np.float32(0.3)) * named[:, None]
+        h = half_step(torch, dtype)
+        assert bool(((y.double() - want).abs() <= (U + h * (1 + U)) * want.abs() + tiny(torch, dtype)).all())
+
+
 @pytest.mark.parametrize("N,V,D", [(5000, 700, 1000), (4096, 40, 2050), (60000, 900, 129), (9000, 20000, 77), (33000, 5, 260)])
 @pytest.mark.parametrize("types", COMBOS, ids="-".join)
 def test_long_sums(ngsgd, N, V, D, types):

@@ -101,6 +101,40 @@ def test_large_tensors(ngsgd, dtype):
     assert all(torch.equal(o, (t.float() * factor).to(dtype)) for o, t in zip(out, grads))
 
 
+@pytest.mark.parametrize("sizes", [[4096 * 32], [4096 * 32 + 1], [4096] * 32, [4096] * 33, [1] * 32, [1] * 33, [4097] * 16, [4097] * 17])
+def test_one_workgroup_and_more(ngsgd, sizes):
+    """32 pieces of 4096 elements are one workgroup's, 33 are not."""
+    import torch
+    rng = np.random.default_rng(len(sizes))
+    for dtype in (torch.float32, torch.bfloat16):
+        grads = make(torch, rng, sizes, dtype)
+        g = ngsgd.GradientNorm(grads)
+        expect = norm_and_factor([f64(t) for t in grads], 1.0)[0]
+        out = [torch.empty_like(t) for t in grads]
+        for bound in (0.4 * expect, 3.0 * expect):
+            check(torch, grads, bound, *g.norm(grads, bound))
+            check(torch, grads, bound, *g.clip(grads, bound, out=out), out)
+
+
+def test_gradients_next_to_each_other(ngsgd):
+    """Views of one buffer: clipped in place, and one buffer into another; in another order or over each other it is refused."""
+    import torch
+    flat, other = torch.randn(3000, device="cuda"), torch.zeros(3000, device="cuda")
+    cut = lambda t: [t[:1000], t[1000:1700], t[1700:]]
+    g = ngsgd.GradientNorm(cut(flat))
+    want = flat.clone()
+    norm, factor = g.clip(cut(flat), 5.0, out=cut(other))
+    assert torch.equal(flat, want) and torch.equal(other, want * factor)
+    g.clip(cut(flat), 5.0)
+    assert torch.equal(flat, other)
+    one, two = torch.ones(1000, device="cuda"), torch.ones(1000, device="cuda")
+    pair = ngsgd.GradientNorm([one, two])
+    for grads, out in (([one, one], None), ([one, two], [two, one]), ([one, two], [other[:1000], other[999:1999]])):
+        with pytest.raises(ngsgd.NgsgdError):
+            pair.clip(grads, 1.0, out=out)
+    assert [float(t) for t in pair.norm([one, one], 1.0)] == pytest.approx([2000 ** 0.5, 2000 ** -0.5], rel=1e-7)
+
+
 def test_squares_beyond_fp32(ngsgd):
     """Numbers whose squares overflow or vanish in fp32; the norm does too where it is above what fp32 holds."""
     import torch

@@ -115,6 +115,16 @@ def test_grad_clip_refuses(lib, bad):
     assert norm(lib, clip=True, **bad) == ng.NGSGD_EINVAL
 
 
+@pytest.mark.parametrize("bad", [
+    dict(grads=(A, A)), dict(grads=(A, A + 16)), dict(grads=(A + 24, A)), dict(out=(3 * A, 3 * A)), dict(out=(3 * A, 3 * A + 16)), dict(out=(2 * A, A)),
+    dict(out=(A, A)), dict(out=(A + 4, 2 * A)), dict(out=(2 * A + 24, 2 * A)), dict(out=(3 * A, 2 * A - 4)), dict(sizes=(5, 0, 9), grads=(A, A, A + 12)),
+    dict(sizes=(100, 100, 100), grads=(A, A, A), out=(2 * A, 3 * A, A))])
+def test_grad_clip_refuses_shared_memory(lib, bad):
+    """Refused, while everything else about the call is right: with a workspace that is too small the same call is refused for that."""
+    assert norm(lib, clip=True, **bad) == ng.NGSGD_EINVAL
+    assert norm(lib, clip=True, nbytes=16, **bad) == ng.NGSGD_ENOMEM
+
+
 def test_grad_norm_without_arrays(lib):
     s, g = (c_int64 * 2)(5, 7), (c_void_p * 2)(A, A)
     assert lib.ngsgd_grad_norm(2, None, g, F32, 1.0, None, None, A, 1 << 30, None) == ng.NGSGD_EINVAL
