@@ -479,21 +479,19 @@ __global__ __launch_bounds__(kSumThreads) void embedding_sum_kernel(const Embedd
   }
 }
 
-// A workgroup per chunk in which a token begins that goes on behind it, and 64 pieces: the parts of all chunks that have rows of it, dealt to
-// its wavefronts.
-constexpr int kJoinThreads = 512;
+// A workgroup per chunk in which a token begins that goes on behind it, and slab of pieces: the parts of all chunks that have rows of it, dealt to groups of
+// a.lanes threads, whose sums are added two by two.
+constexpr int kJoinThreads = 512, kJoinAhead = 4;
 template <typename W, int E>
 __global__ __launch_bounds__(kJoinThreads) void embedding_join_kernel(const EmbeddingBackward a) {
-  constexpr int kWaves = kJoinThreads / 64;
-  __shared__ float parts[kWaves][64][E];
+  __shared__ float parts[E][kJoinThreads];
   const int64_t chunk = blockIdx.x / a.slabs, from = chunk * a.chunk, to = from + a.chunk;
   if (to >= a.N) return;
   const uint32_t key = a.sorted[to - 1].key, behind = a.sorted[to].key, in_front = from > 0 ? a.sorted[from - 1].key : ~key;
   if (key >= (uint32_t)a.V || behind != key || in_front == key) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, piece = (int)(blockIdx.x % a.slabs) * 64 + lane;
   int64_t last = chunk + 1;              // the chunk with its last row: a lane looks where each of the next ones ends
   for (;;) {
-    const int64_t end = (last + lane + 1) * a.chunk;
+    const int64_t end = (last + (threadIdx.x & 63) + 1) * a.chunk;
     const uint64_t goes_on = __builtin_amdgcn_ballot_w64(end < a.N && a.sorted[end].key == key);
     if (~goes_on != 0) {
       last += __builtin_ctzll(~goes_on);
@@ -501,26 +499,45 @@ __global__ __launch_bounds__(kJoinThreads) void embedding_join_kernel(const Embe
     }
     last += 64;
   }
+  const int lane = threadIdx.x & (a.lanes - 1), group = threadIdx.x / a.lanes, groups = kJoinThreads / a.lanes;
+  const int piece = (int)(blockIdx.x % a.slabs) * 64 + lane;
   float sum[E];
 #pragma unroll
   for (int j = 0; j < E; ++j) sum[j] = 0.f;
   if (piece < a.pieces) {
-#pragma unroll 4
-    for (int64_t c = chunk + wave; c <= last; c += kWaves) {
-      const Pack<float, E> part = *reinterpret_cast<const Pack<float, E>*>(a.parts + ((c * 2 + (c == chunk ? 1 : 0)) * a.pieces + piece) * E);
+    for (int64_t c = chunk + group; c <= last; c += groups * kJoinAhead) {
+      Pack<float, E> part[kJoinAhead];
 #pragma unroll
-      for (int j = 0; j < E; ++j) sum[j] += part.v[j];
+      for (int k = 0; k < kJoinAhead; ++k) {
+        const int64_t of = min(c + k * groups, last);
+        part[k] = *reinterpret_cast<const Pack<float, E>*>(a.parts + ((of * 2 + (of == chunk ? 1 : 0)) * a.pieces + piece) * E);
+      }
+#pragma unroll
+      for (int k = 0; k < kJoinAhead; ++k) {
+        const bool here = c + k * groups <= last;   // (behind a condition, the compiler would load one after the other)
+#pragma unroll
+        for (int j = 0; j < E; ++j) sum[j] += here ? part[k].v[j] : 0.f;
+      }
     }
   }
+  int half = groups;
+  while (half / 2 > last - chunk) half /= 2;   // (the groups behind these have nothing)
+  if (group < half) {
 #pragma unroll
-  for (int j = 0; j < E; ++j) parts[wave][lane][j] = sum[j];
-  __syncthreads();
-  if (wave != 0 || piece >= a.pieces) return;
+    for (int j = 0; j < E; ++j) parts[j][threadIdx.x] = sum[j];
+  }
+  while (half > 1) {
+    half /= 2;
+    __syncthreads();
+    if (group < half) {
 #pragma unroll
-  for (int k = 1; k < kWaves; ++k)
-#pragma unroll
-    for (int j = 0; j < E; ++j) sum[j] += parts[k][lane][j];
-  store_piece<W, E>(a, key, piece, sum);
+      for (int j = 0; j < E; ++j) {
+        sum[j] += parts[j][threadIdx.x + half * a.lanes];
+        parts[j][threadIdx.x] = sum[j];
+      }
+    }
+  }
+  if (group == 0 && piece < a.pieces) store_piece<W, E>(a, key, piece, sum);
 }
 
 }  // namespace ngsgd
