@@ -14,7 +14,6 @@ import os
 from array import array
 from contextlib import nullcontext
 from ctypes import POINTER, byref, c_char_p, c_double, c_float, c_int, c_int32, c_int64, c_size_t, c_void_p
-from operator import attrgetter
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libngsgd.so")
@@ -154,6 +153,11 @@ def load_library():
         _torch = torch
     except ImportError:
         pass
+    if _torch is not None:
+        try:
+            from . import _tensors   # noqa: F401  (addresses of many tensors at once; from here on a name of this package)
+        except ImportError as e:
+            raise ImportError(f"{_HERE}/_tensors.so is missing or of another torch: build it with `python -m paper_1410_7455_amd.build`") from e
     lib = ctypes.CDLL(LIB_PATH)
     for name, (restype, argtypes) in _SIGNATURES.items():
         fn = getattr(lib, name)          # AttributeError if the symbol is not exported
@@ -618,14 +622,6 @@ class CrossEntropy:
         return self._call(logits, labels, scale, loss, dlogits, True, stream)
 
 
-_DTYPE = attrgetter("dtype")
-
-
-def _host(numbers):
-    """Address of an array.array's numbers."""
-    return numbers.buffer_info()[0]
-
-
 class GradientNorm:
     """ngsgd_grad_norm / ngsgd_grad_clip: the norm of many gradients as one vector, and clipping, on the current device.
 
@@ -651,7 +647,8 @@ class GradientNorm:
         self.grad_dtype = like[0].dtype if grad_dtype is None else grad_dtype
         self.type = _type_of(self.grad_dtype)
         self.sizes = [p.numel() for p in like]
-        self._sizes = array("q", self.sizes)
+        self._sizes = array("q", self.sizes).tobytes()
+        self._like = torch.empty(0, dtype=self.grad_dtype)
         nbytes = c_size_t(0)
         _check(self.lib.ngsgd_grad_norm_workspace_bytes(n, byref(nbytes)), "ngsgd_grad_norm_workspace_bytes")
         self.workspace_bytes = nbytes.value
@@ -659,27 +656,19 @@ class GradientNorm:
         self._home = _raw_stream(None, self.device)
 
     def _addresses(self, tensors, name):
-        """The tensors' addresses (0: does not count)."""
-        dtype, index, sizes = self.grad_dtype, self.device.index, self.sizes
-        if len(tensors) != len(sizes):
-            raise ValueError(f"{len(tensors)} {name}s for {len(sizes)} tensors")
-        tensor = _torch.Tensor
-        try:      # all at once: half the time of one by one
-            if (list(map(tensor.numel, tensors)) == sizes and all(map(tensor.is_contiguous, tensors)) and set(map(_DTYPE, tensors)) == {dtype}
-                    and set(map(tensor.get_device, tensors)) == {index}):
-                return array("Q", map(tensor.data_ptr, tensors))
-        except TypeError:
-            pass  # None among them
-        addresses = array("Q")
-        for t, size in zip(tensors, sizes):
-            if t is None or size == 0:
-                addresses.append(0)
-                continue
-            if t.dtype != dtype or t.numel() != size or t.get_device() != index or not t.is_contiguous():
-                raise ValueError(f"{name} {len(addresses)}: {t.dtype}, {t.numel()} elements on {t.device}, for {dtype}, {size} on "
-                                 f"{self.device}, dense")
-            addresses.append(t.data_ptr())
-        return addresses
+        """The tensors' addresses as bytes (0: does not count)."""
+        if len(tensors) != len(self.sizes):
+            raise ValueError(f"{len(tensors)} {name}s for {len(self.sizes)} tensors")
+        found = _tensors.addresses(tensors, self._sizes, self._like, self.device.index)
+        if found is None:
+            for i, (t, size) in enumerate(zip(tensors, self.sizes)):
+                if t is None or size == 0:
+                    continue
+                if t.dtype != self.grad_dtype or t.numel() != size or t.get_device() != self.device.index or not t.is_contiguous():
+                    raise ValueError(f"{name} {i}: {t.dtype}, {t.numel()} elements on {t.device}, for {self.grad_dtype}, {size} on "
+                                     f"{self.device}, dense")
+            raise ValueError(f"a {name} has no memory of its own")
+        return found
 
     def _results(self, norm, factor, stream):
         for name, t in (("norm", norm), ("factor", factor)):
@@ -699,7 +688,7 @@ class GradientNorm:
         _current_device(self.device)
         grads = self._addresses(grads, "gradient")
         norm, factor = self._results(norm, factor, stream)
-        _check(self.lib.ngsgd_grad_norm(len(self.sizes), _host(self._sizes), _host(grads), self.type, max_norm, norm.data_ptr(), factor.data_ptr(),
+        _check(self.lib.ngsgd_grad_norm(len(self.sizes), self._sizes, grads, self.type, max_norm, norm.data_ptr(), factor.data_ptr(),
                                         self.workspace.data_ptr(), self.workspace_bytes,
                                         _raw_stream(stream, self.device, self.workspace, self._home)), "ngsgd_grad_norm")
         return norm, factor
@@ -708,13 +697,13 @@ class GradientNorm:
         """(norm, factor); every gradient is multiplied by the factor, in place or into `out` (a tensor for each gradient, which may be it)."""
         _current_device(self.device)
         if out is not None:
+            if len(out) != len(grads) or any(o is None and g is not None for o, g in zip(out, grads)):
+                raise ValueError("out has no tensor for a gradient")
             out = self._addresses(out, "output")
         grads = self._addresses(grads, "gradient")
-        if out is not None and 0 in out and any(g and not o for g, o in zip(grads, out)):
-            raise ValueError("out has no tensor for a gradient")
         norm, factor = self._results(norm, factor, stream)
-        _check(self.lib.ngsgd_grad_clip(len(self.sizes), _host(self._sizes), _host(grads), self.type, max_norm,
-                                        None if out is None else _host(out), norm.data_ptr(), factor.data_ptr(),
+        _check(self.lib.ngsgd_grad_clip(len(self.sizes), self._sizes, grads, self.type, max_norm,
+                                        out, norm.data_ptr(), factor.data_ptr(),
                                         self.workspace.data_ptr(), self.workspace_bytes,
                                         _raw_stream(stream, self.device, self.workspace, self._home)), "ngsgd_grad_clip")
         return norm, factor

@@ -1,15 +1,19 @@
-"""Builds libngsgd.so (HIP, gfx950) in-tree with hipcc."""
+"""Builds libngsgd.so (HIP, gfx950) in-tree with hipcc, and the binding's helper _tensors.so (host code) with g++."""
 from __future__ import annotations
 
 import os
 import shutil
 import subprocess
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 LIB_PATH = os.path.join(HERE, "libngsgd.so")
 SOURCES = [os.path.join(HERE, "csrc", name) for name in ("ngsgd.hip", "layer_norm.hip", "adamw.hip", "embedding.hip", "cross_entropy.hip", "grad_norm.hip")]
+
+BINDING_PATH = os.path.join(HERE, "_tensors.so")
+BINDING_SOURCE = os.path.join(HERE, "csrc", "tensors.cpp")
 
 HIPCC_FLAGS = [
     "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC",
@@ -26,8 +30,22 @@ def find_hipcc() -> str:
     raise RuntimeError("hipcc not found: the ngsgd library needs the ROCm toolchain to build")
 
 
+def binding_command() -> list:
+    """g++ on the binding's helper, against the Python and the torch that run this."""
+    import torch
+    from torch.utils import cpp_extension
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           "-I", sysconfig.get_paths()["include"]]
+    for path in cpp_extension.include_paths():
+        cmd += ["-isystem", path]
+    cmd += ["-o", BINDING_PATH, BINDING_SOURCE]
+    for path in cpp_extension.library_paths():
+        cmd += ["-L", path, f"-Wl,-rpath,{path}"]
+    return cmd + ["-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10"]
+
+
 def build(verbose: bool = False) -> str:
-    """Compiles every source (side by side) and links them; raises with the compiler's output if one fails."""
+    """Compiles every source (side by side) and links them, and the binding's helper; raises with the compiler's output if one fails."""
     hipcc = find_hipcc()
     objects = os.path.join(HERE, "_build")
     os.makedirs(objects, exist_ok=True)
@@ -41,14 +59,15 @@ def build(verbose: bool = False) -> str:
     def compile_one(source):
         return run([hipcc, *HIPCC_FLAGS, *include, "-c", "-o", os.path.join(objects, os.path.basename(source) + ".o"), source])
 
-    with ThreadPoolExecutor(max_workers=min(len(SOURCES), os.cpu_count() or 1)) as pool:
-        results = list(pool.map(compile_one, SOURCES))
+    with ThreadPoolExecutor(max_workers=min(len(SOURCES) + 1, os.cpu_count() or 1)) as pool:
+        binding = pool.submit(lambda: run(binding_command()))
+        results = list(pool.map(compile_one, SOURCES)) + [binding.result()]
     if all(r.returncode == 0 for r in results):
         results.append(run([hipcc, "-shared", "-fPIC", "--offload-arch=gfx950", "-o", LIB_PATH,
                             *(os.path.join(objects, os.path.basename(s) + ".o") for s in SOURCES)]))
     for proc in results:
         if proc.returncode != 0:
-            raise RuntimeError("hipcc failed:\n" + proc.stdout + proc.stderr)
+            raise RuntimeError(f"{os.path.basename(proc.args[0])} failed:\n" + proc.stdout + proc.stderr)
         if verbose and proc.stderr.strip():
             print(proc.stderr)
     return LIB_PATH

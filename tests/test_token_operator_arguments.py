@@ -162,7 +162,7 @@ def test_binding_refuses_tensors_off_the_device(monkeypatch):
         ng.GradientNorm([])
     e = made(torch, ng.Embedding, max_tokens=4, vocabulary=8, dim=8, scale=1.0)
     c = made(torch, ng.CrossEntropy, max_rows=4, classes=8)
-    g = made(torch, ng.GradientNorm, sizes=[4], grad_dtype=torch.float32)
+    g = made(torch, ng.GradientNorm, sizes=[4], grad_dtype=torch.float32, _sizes=(4).to_bytes(8, "little"), _like=torch.empty(0))
     tokens, x = torch.zeros(4, dtype=torch.int32), torch.zeros(4, 8)
     for call in (lambda: e.forward(tokens, x), lambda: e.backward(x, tokens), lambda: c.forward(x, tokens), lambda: c.gradient(x, tokens),
                  lambda: g.norm([torch.zeros(4)]), lambda: g.clip([torch.zeros(4)], 1.0), lambda: g.norm([])):
@@ -179,3 +179,18 @@ def test_binding_refuses_another_current_device(monkeypatch):
                  lambda: g.norm([None]), lambda: g.clip([None], 1.0)):
         with pytest.raises(ValueError):
             call()
+
+
+def test_addresses_of_many_tensors():
+    """What the helper takes, and what it does not (the binding then says why); it looks at the device, so on a CPU only what has no address is taken."""
+    torch = pytest.importorskip("torch")
+    ng.load_library()
+    like, size = torch.empty(0), lambda *n: b"".join(k.to_bytes(8, "little") for k in n)
+    assert ng._tensors.addresses([], b"", like, 0) == b""
+    assert ng._tensors.addresses([None, torch.zeros(0)], size(5, 0), like, 0) == bytes(16)
+    assert ng._tensors.addresses((None,), size(5), like, 0) == bytes(8)
+    for tensors, sizes in (([torch.zeros(5)], size(5)), ([None], size(5, 5)), ([None, None], size(5)), ([3], size(5)), (["x"], size(1))):
+        assert ng._tensors.addresses(tensors, sizes, like, 0) is None
+    for bad in ((5, size(5), like, 0), ([None], [5], like, 0), ([None], size(5), torch.float32, 0), ([None], size(5), like, "0"), ([None], size(5), like)):
+        with pytest.raises(TypeError):
+            ng._tensors.addresses(*bad)
