@@ -17,6 +17,8 @@ Modules
   network              forward / objective / backward / precondition / update
                        (Sec. 2, Sec. 4.5-4.6).
   averaging            parameter averaging across replicas (Sec. 3.1).
+  layer_norm, adamw, embedding, cross_entropy, clipping
+                       the operators beside the paper's method, from their definitions.
 
 Parity pins: every function here is pinned by tests/test_oracle_*.py against
 brute-force dense algebra, closed forms and invariants fixed by the paper.

@@ -56,8 +56,8 @@ struct EmbeddingBackward {
 // Bound by memory: y is written once, and of the table what the dies' caches do not hold is read.  A thread has pieces of E elements of kLookupRows rows in
 // flight: their tokens first, then the table's rows (8 rows: 4 % slower; 8-byte stores for fp32 tables, so that loads are dense: the same).  The last piece
 // of a row is moved back to end with it (its first elements are written twice, with the same values).  PAST: y is written past the caches.  (The compiler would
-// make one ordinary store of the two kinds behind a condition.)  196613 x 4096 fp32 to bf16, a Zipf law over 50021 rows: 532 us, 1.6 GB written and
-// 0.41 GB fetched, 3.8 TB/s; 131072 x 4096 bf16 over 32000: 280 us, 4.8 TB/s.
+// make one ordinary store of the two kinds behind a condition.)  196613 x 4096 fp32 to bf16, a Zipf law over 50021 rows: 532 us, 1.61 GB written and
+// 0.85 GB of the 3.0 GB read fetched, 4.6 TB/s, near what a copy reaches; 131072 x 4096 bf16 over 32000: 280 us, 4.8 TB/s.
 template <typename W, typename T, typename I, int E, bool PAST>
 __global__ __launch_bounds__(kLookupThreads) void embedding_forward_kernel(const EmbeddingForward a) {
   const int lane = threadIdx.x & (a.lanes - 1), per_round = kLookupThreads / a.lanes;

@@ -28,8 +28,8 @@ int with_types(const int type, const int table_type, const int index_type, F f) 
 }
 
 // Rows of the table from here on are cut into eight slabs, one for each die (workgroups go to them in turn), whose cache then holds eight times as many rows'
-// parts: 65536 x 8192 fp32 of a Zipf law 623 -> 535 us, 196613 x 4096 fp32 to bf16 543 -> 537 (0.67 -> 0.41 GB fetched); narrower rows lose (131072 x 4096
-// bf16 281 -> 300).
+// parts: 65536 x 8192 fp32 of a Zipf law 623 -> 535 us, 196613 x 4096 fp32 to bf16 543 -> 537 (1.37 -> 0.85 GB fetched); narrower rows lose (131072 x 4096
+// bf16 281 -> 300), and so do two or more slabs of a die one after the other (530 -> 550 and more: pieces of y that are written together get short).
 constexpr size_t kSlabBytes = 16384;
 constexpr int kDies = 8;
 // What is larger than all dies' caches is written past them, which leaves them to the table (65536 x 1024 bf16 29 -> 26 us, 131072 x 4096 309 -> 281).
