@@ -1,5 +1,6 @@
 """CPU-side checks of the embedding's, the cross-entropy's and the gradient norm's entry points: sizes, refusals.  Every call here is refused,
 or has nothing to do, before any device work."""
+import sys
 from ctypes import byref, c_int64, c_size_t, c_void_p
 
 import pytest
@@ -179,6 +180,16 @@ def test_binding_refuses_another_current_device(monkeypatch):
                  lambda: g.norm([None]), lambda: g.clip([None], 1.0)):
         with pytest.raises(ValueError):
             call()
+
+
+def test_missing_helper_fails_loudly(monkeypatch):
+    pytest.importorskip("torch")
+    ng.load_library()
+    monkeypatch.setattr(ng, "_lib", None)
+    monkeypatch.delattr(ng, "_tensors")
+    monkeypatch.setitem(sys.modules, ng.__name__ + "._tensors", None)
+    with pytest.raises(ImportError, match="_tensors.so"):
+        ng.load_library()
 
 
 def test_addresses_of_many_tensors():
