@@ -91,36 +91,46 @@ __global__ __launch_bounds__(kLookupThreads) void embedding_forward_kernel(const
 template <typename I>
 __device__ __forceinline__ uint32_t key_of(const I t, const int64_t V) { return (uint64_t)(int64_t)t < (uint64_t)V ? (uint32_t)t : (uint32_t)V; }
 
-// Few tokens: each one's rank is counted, sum_j [key_j < key_i or (key_j = key_i and j < i)].  A workgroup's 16 wavefronts share 64 tokens and deal the
-// others between them, 64 at a time.  Their keys come from LDS, four with one read that all lanes share: a wavefront's own copy, without a barrier.  Two
-// instructions a pair: 8192 tokens 13.6 us, 4096 8.5, 1024 4.5 (by v_readlane in 512 unrolled steps 22: the instructions came from memory).
-constexpr int kRankThreads = 1024, kRankRounds = 8, kRankMost = kRankThreads * kRankRounds;   // tokens
-template <typename I>
+// Few tokens: each one's rank is counted, sum_j [key_j < key_i or (key_j = key_i and j < i)], among all (TILES = 0, up to kRankMost) or among the 1024 of its
+// tile.  A workgroup's 16 wavefronts share 64 tokens and deal the others between them, 64 at a time.  Their keys come from LDS, four with one read that all lanes
+// share: a wavefront's own copy, without a barrier.  Two instructions a pair: 4096 tokens 8.2 us, 1024 4.7 (8192 13.6, in tiles 4.7 and 4.6 to merge them; by
+// v_readlane in 512 unrolled steps 22: the instructions came from memory).
+constexpr int kRankThreads = 1024, kRankRounds = 4, kRankMost = kRankThreads * kRankRounds;   // tokens
+template <typename I, bool TILES>
 __global__ __launch_bounds__(kRankThreads) void embedding_rank_kernel(const I* tokens, const int N, const int64_t V, SortedToken* sorted) {
-  __shared__ U32x4 keys[kRankThreads / 64][kRankRounds][16];
+  constexpr int kRounds = TILES ? 1 : kRankRounds;
+  __shared__ U32x4 keys[kRankThreads / 64][kRounds][16];
   __shared__ int counts[kRankThreads / 64][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), first = blockIdx.x * 64, i = first + lane;
-  I others[kRankRounds];
+  const int start = TILES ? first / kRankThreads * kRankThreads : 0, end = TILES ? min(start + kRankThreads, N) : N;   // of those that are compared
+  I others[kRounds];
   const I own = tokens[min(i, N - 1)];
 #pragma unroll
-  for (int r = 0; r < kRankRounds; ++r) others[r] = tokens[min(r * kRankThreads + (int)threadIdx.x, N - 1)];
+  for (int r = 0; r < kRounds; ++r) others[r] = tokens[min(start + r * kRankThreads + (int)threadIdx.x, N - 1)];
   const uint32_t key = key_of(own, V);
 #pragma unroll
-  for (int r = 0; r < kRankRounds; ++r)
-    reinterpret_cast<uint32_t*>(keys[wave][r])[lane] = r * kRankThreads + (int)threadIdx.x < N ? key_of(others[r], V) : 0xffffffffu;
+  for (int r = 0; r < kRounds; ++r)
+    reinterpret_cast<uint32_t*>(keys[wave][r])[lane] = start + r * kRankThreads + (int)threadIdx.x < end ? key_of(others[r], V) : 0xffffffffu;
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
   __builtin_amdgcn_wave_barrier();
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
   int count = 0;
-  for (int r = 0, base = wave * 64; base < N; ++r, base += kRankThreads) {
-    const uint32_t limit = base < first ? key + 1 : key;   // those in front go first among equals
+  for (int r = 0, base = start + wave * 64; base < end; ++r, base += kRankThreads) {
+    // those in front go first among equals
+    const uint32_t limit = base < first ? key + 1 : key;
+    if (base != first) {
 #pragma unroll 4
-    for (int k = 0; k < 16; ++k) {
-      const U32x4 other = keys[wave][r][k];
-      count += (other.x < limit) + (other.y < limit) + (other.z < limit) + (other.w < limit);
-    }
-    if (base == first) {
-      for (int k = 0; k < 64; ++k) count += reinterpret_cast<const uint32_t*>(keys[wave][r])[k] == key && k < lane;
+      for (int k = 0; k < 16; ++k) {
+        const U32x4 other = keys[wave][r][k];
+        count += (other.x < limit) + (other.y < limit) + (other.z < limit) + (other.w < limit);
+      }
+    } else {
+#pragma unroll 4
+      for (int k = 0; k < 16; ++k) {
+        const U32x4 other = keys[wave][r][k];
+        count += (other.x < key + (4 * k < lane)) + (other.y < key + (4 * k + 1 < lane)) + (other.z < key + (4 * k + 2 < lane)) +
+                 (other.w < key + (4 * k + 3 < lane));
+      }
     }
   }
   counts[wave][lane] = count;
@@ -129,12 +139,60 @@ __global__ __launch_bounds__(kRankThreads) void embedding_rank_kernel(const I* t
   int rank = 0;
 #pragma unroll
   for (int k = 0; k < kRankThreads / 64; ++k) rank += counts[k][lane];
-  sorted[rank] = SortedToken{key, (uint32_t)i};
+  sorted[start + rank] = SortedToken{key, (uint32_t)i};
+}
+
+// Up to 32 sorted tiles into one list: a token goes behind those of the tiles in front whose keys are not above its own, and of the tiles behind whose keys are
+// below.  A workgroup has 64 neighbours of a tile; a wavefront looks for them in every 16th tile, whose keys it copies to LDS while it looks in the one before
+// (by reading the tiles from the cache in every step: 20011 tokens 8.6 us instead of 7.7).  The work grows with the square of the tiles: 32768 tokens 11.8, ranks in
+// the tiles 5.6, where sorting by digits takes 25 in four launches; 65536 34, where it takes 25 too.
+constexpr int kMergeTiles = 32, kMergeMost = kMergeTiles * kRankThreads, kMergeLoads = kRankThreads / 64;
+__global__ __launch_bounds__(kRankThreads) void embedding_merge_kernel(const SortedToken* tiles, const int N, SortedToken* sorted) {
+  constexpr int kWaves = kRankThreads / 64;
+  __shared__ uint32_t keys[kWaves][kRankThreads];
+  __shared__ int counts[kWaves][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = blockIdx.x * 64 + lane;
+  const int own = blockIdx.x * 64 / kRankThreads, n_tiles = (N + kRankThreads - 1) / kRankThreads;
+  uint32_t next[kMergeLoads];
+  const auto ask = [&](const int tile) {
+#pragma unroll
+    for (int r = 0; r < kMergeLoads; ++r) next[r] = tiles[min(tile * kRankThreads + r * 64 + lane, N - 1)].key;
+  };
+  if (wave < n_tiles) ask(wave);
+  const SortedToken token = tiles[min(i, N - 1)];
+  int count = 0;
+  for (int tile = wave; tile < n_tiles; tile += kWaves) {
+#pragma unroll
+    for (int r = 0; r < kMergeLoads; ++r)
+      keys[wave][r * 64 + lane] = tile * kRankThreads + r * 64 + lane < N ? next[r] : 0xffffffffu;
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    if (tile + kWaves < n_tiles) ask(tile + kWaves);
+    if (tile != own) {
+      const uint32_t limit = tile < own ? token.key + 1 : token.key;
+      int at = 0;
+#pragma unroll
+      for (int step = kRankThreads / 2; step > 0; step /= 2)
+        if (keys[wave][at + step - 1] < limit) at += step;
+      count += at + (keys[wave][at] < limit);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  }
+  counts[wave][lane] = count;
+  __syncthreads();
+  if (wave != 0 || i >= N) return;
+  int rank = i - own * kRankThreads;
+#pragma unroll
+  for (int k = 0; k < kWaves; ++k) rank += counts[k][lane];
+  sorted[rank] = token;
 }
 
 // More: a radix sort from the lowest digit, each pass stable, as few passes as digits of 10 bits allow.  Latency bounds it (few workgroups, one step behind the
-// other): a pass over 20011 tokens takes 9.5 us, over 262144 17.  A workgroup has a tile of kSortRounds tokens a thread; counts[tile][digit].
-constexpr int kSortBits = 10, kSortBins = 1 << kSortBits, kSortRounds = 4;
+// other): a pass over 32769 tokens takes 12.4 us, over 262144 17.  A workgroup has a tile of kSortRounds tokens a thread; counts[tile][digit].
+constexpr int kSortThreads = 1024, kSortBits = 10, kSortBins = 1 << kSortBits, kSortRounds = 4;
 constexpr int kSortInline = 64;   // tiles up to which a workgroup adds up the counts in front of it itself
 
 struct EmbeddingSort {
@@ -154,20 +212,20 @@ __device__ __forceinline__ SortedToken sort_input(const EmbeddingSort& a, const 
   return a.in[i];
 }
 
-template <typename I, bool FIRST, int THREADS>
-__global__ __launch_bounds__(THREADS) void embedding_count_kernel(const EmbeddingSort a) {
+template <typename I, bool FIRST>
+__global__ __launch_bounds__(kSortThreads) void embedding_count_kernel(const EmbeddingSort a) {
   __shared__ uint32_t bins[kSortBins];
-  const int64_t from = (int64_t)blockIdx.x * THREADS * kSortRounds + threadIdx.x;
+  const int64_t from = (int64_t)blockIdx.x * kSortThreads * kSortRounds + threadIdx.x;
   uint32_t key[kSortRounds];
 #pragma unroll
-  for (int r = 0; r < kSortRounds; ++r) key[r] = sort_input<I, FIRST>(a, min(from + r * THREADS, a.N - 1)).key;
-  for (int d = threadIdx.x; d < a.bins; d += THREADS) bins[d] = 0;
+  for (int r = 0; r < kSortRounds; ++r) key[r] = sort_input<I, FIRST>(a, min(from + r * kSortThreads, a.N - 1)).key;
+  for (int d = threadIdx.x; d < a.bins; d += kSortThreads) bins[d] = 0;
   __syncthreads();
 #pragma unroll
   for (int r = 0; r < kSortRounds; ++r)
-    if (from + r * THREADS < a.N) atomicAdd(&bins[key[r] >> a.shift & (a.bins - 1)], 1u);
+    if (from + r * kSortThreads < a.N) atomicAdd(&bins[key[r] >> a.shift & (a.bins - 1)], 1u);
   __syncthreads();
-  for (int d = threadIdx.x; d < a.bins; d += THREADS) a.counts[(int64_t)blockIdx.x * a.bins + d] = bins[d];
+  for (int d = threadIdx.x; d < a.bins; d += kSortThreads) a.counts[(int64_t)blockIdx.x * a.bins + d] = bins[d];
 }
 
 // Many tiles: counts become those of the tiles in front.  A lane per digit; 16 wavefronts share the tiles.
@@ -200,16 +258,16 @@ __global__ __launch_bounds__(1024) void embedding_scan_kernel(const EmbeddingSor
 
 // Places: digits in order, tiles in order within a digit, a tile's tokens in order within that.  A wavefront ranks 64 tokens at a time: lanes
 // with the same digit find each other by one ballot a bit.  Then the digits are dealt to the threads, neighbours to each.
-template <typename I, bool FIRST, int THREADS>
-__global__ __launch_bounds__(THREADS) void embedding_scatter_kernel(const EmbeddingSort a) {
-  constexpr int kWaves = THREADS / 64, kOwn = kSortBins / THREADS;
+template <typename I, bool FIRST>
+__global__ __launch_bounds__(kSortThreads) void embedding_scatter_kernel(const EmbeddingSort a) {
+  constexpr int kWaves = kSortThreads / 64, kOwn = kSortBins / kSortThreads;
   __shared__ uint32_t bins[kWaves * kSortBins];   // of each wavefront: its count, then where its next token with that digit goes
   __shared__ uint32_t waves[kWaves];
   using Counts = Pack<uint32_t, kOwn>;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const bool owns = threadIdx.x * kOwn < (unsigned)a.bins;
   uint32_t* const mine = bins + wave * a.bins;
-  const int64_t from = ((int64_t)blockIdx.x * THREADS + wave * 64) * kSortRounds + lane;
+  const int64_t from = ((int64_t)blockIdx.x * kSortThreads + wave * 64) * kSortRounds + lane;
   SortedToken token[kSortRounds];
 #pragma unroll
   for (int r = 0; r < kSortRounds; ++r) token[r] = sort_input<I, FIRST>(a, min(from + r * 64, a.N - 1));
@@ -238,7 +296,7 @@ __global__ __launch_bounds__(THREADS) void embedding_scatter_kernel(const Embedd
       }
     }
   }
-  for (int d = threadIdx.x; d < kWaves * a.bins; d += THREADS) bins[d] = 0;
+  for (int d = threadIdx.x; d < kWaves * a.bins; d += kSortThreads) bins[d] = 0;
   __syncthreads();
   uint32_t rank[kSortRounds];                     // within the wavefront
 #pragma unroll

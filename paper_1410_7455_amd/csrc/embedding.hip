@@ -59,8 +59,7 @@ int launch_forward(EmbeddingForward a, hipStream_t s) {
 }
 
 // How a gradient is computed: all by sizes, so that a workspace for more tokens serves fewer.
-constexpr int kSortSmall = 256, kSortLarge = 1024;   // threads
-constexpr int64_t kSortSmallTile = kSortSmall * kSortRounds, kSortTile = kSortLarge * kSortRounds;
+constexpr int64_t kSortTile = kSortThreads * kSortRounds;
 constexpr int64_t kSumWaves = 4096;        // wavefronts that the sums are cut into, if there are as many
 constexpr int64_t kFewGroups = 4096;       // workgroups that walk over a table
 constexpr int kLeastChunk = 16, kMostChunk = 512;
@@ -98,49 +97,53 @@ Workspace layout(Carver& c, const int64_t N, const int D) {
   }
   w.sorted = c.take<SortedToken>(N);
   w.parts = c.take<float>(floats);
-  if (N > kRankMost) {
-    const int64_t tiles = std::max((N + kSortTile - 1) / kSortTile, std::min<int64_t>((N + kSortSmallTile - 1) / kSortSmallTile, kSortInline));
-    w.other = c.take<SortedToken>(N);
-    w.counts = c.take<uint32_t>(tiles * kSortBins);
+  if (N > kRankMost) w.other = c.take<SortedToken>(N);
+  if (N > kMergeMost) {
+    w.counts = c.take<uint32_t>((N + kSortTile - 1) / kSortTile * kSortBins);
     w.totals = c.take<uint32_t>(kSortBins);
   }
   return w;
 }
 
-template <typename I, bool FIRST, int THREADS>
+template <typename I, bool FIRST>
 int sort_pass(const EmbeddingSort& a, hipStream_t s) {
-  hipLaunchKernelGGL((embedding_count_kernel<I, FIRST, THREADS>), dim3((unsigned)a.tiles), dim3(THREADS), 0, s, a);
+  hipLaunchKernelGGL((embedding_count_kernel<I, FIRST>), dim3((unsigned)a.tiles), dim3(kSortThreads), 0, s, a);
   LAUNCH_CHECK();
   if (a.totals != nullptr) {
     hipLaunchKernelGGL(embedding_scan_kernel, dim3((unsigned)((a.bins + 63) / 64)), dim3(1024), 0, s, a);
     LAUNCH_CHECK();
   }
-  hipLaunchKernelGGL((embedding_scatter_kernel<I, FIRST, THREADS>), dim3((unsigned)a.tiles), dim3(THREADS), 0, s, a);
+  hipLaunchKernelGGL((embedding_scatter_kernel<I, FIRST>), dim3((unsigned)a.tiles), dim3(kSortThreads), 0, s, a);
   LAUNCH_CHECK();
   return NGSGD_OK;
 }
 
 template <typename I>
 int sort_tokens(const void* tokens, const int64_t N, const int64_t V, const Workspace& w, hipStream_t s) {
-  if (N <= kRankMost) {
-    hipLaunchKernelGGL(embedding_rank_kernel<I>, dim3((unsigned)((N + 63) / 64)), dim3(kRankThreads), 0, s, static_cast<const I*>(tokens), (int)N, V,
-                       w.sorted);
+  if (N <= kMergeMost) {
+    const dim3 grid((unsigned)((N + 63) / 64)), threads(kRankThreads);
+    if (N <= kRankMost) {
+      hipLaunchKernelGGL((embedding_rank_kernel<I, false>), grid, threads, 0, s, static_cast<const I*>(tokens), (int)N, V, w.sorted);
+      LAUNCH_CHECK();
+      return NGSGD_OK;
+    }
+    hipLaunchKernelGGL((embedding_rank_kernel<I, true>), grid, threads, 0, s, static_cast<const I*>(tokens), (int)N, V, w.other);
+    LAUNCH_CHECK();
+    hipLaunchKernelGGL(embedding_merge_kernel, grid, threads, 0, s, w.other, (int)N, w.sorted);
     LAUNCH_CHECK();
     return NGSGD_OK;
   }
   int bits = 1;                            // of the keys 0 .. V
   while ((int64_t)1 << bits <= V) ++bits;
   const int passes = (bits + kSortBits - 1) / kSortBits, digit = std::max(2, (bits + passes - 1) / passes);
-  const bool small = N <= kSortSmallTile * kSortInline;
-  const int64_t tile = small ? kSortSmallTile : kSortTile;
-  EmbeddingSort a{tokens, nullptr, nullptr, N, V, w.counts, nullptr, (int)((N + tile - 1) / tile), 0, 1 << digit};
+  EmbeddingSort a{tokens, nullptr, nullptr, N, V, w.counts, nullptr, (int)((N + kSortTile - 1) / kSortTile), 0, 1 << digit};
   if (a.tiles > kSortInline) a.totals = w.totals;
   for (int pass = 0; pass < passes; ++pass, a.shift += digit) {
     a.out = (passes - pass) % 2 == 1 ? w.sorted : w.other;   // the last one's
     if (pass == 0)
-      NG_TRY(small ? (sort_pass<I, true, kSortSmall>(a, s)) : (sort_pass<I, true, kSortLarge>(a, s)));
+      NG_TRY((sort_pass<I, true>(a, s)));
     else
-      NG_TRY(small ? (sort_pass<I, false, kSortSmall>(a, s)) : (sort_pass<I, false, kSortLarge>(a, s)));
+      NG_TRY((sort_pass<I, false>(a, s)));
     a.in = a.out;
   }
   return NGSGD_OK;

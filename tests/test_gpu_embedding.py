@@ -110,7 +110,7 @@ def test_widths(ngsgd, D, types):
 @pytest.mark.parametrize("law", ["zipf", "uniform", "first", "last"])
 @pytest.mark.parametrize("N,V", [(1, 1), (1, 1000), (2, 1), (3, 70000), (15, 4), (16, 5000), (63, 64), (64, 2), (65, 300), (127, 1), (128, 7), (129, 9),
                                  (1000, 50), (1024, 255), (1025, 256), (2048, 257), (4095, 3), (4096, 4096), (4097, 65535), (8192, 65536), (8193, 65537),
-                                 (10007, 1), (16384, 100), (20011, 511), (30000, 131073), (65537, 1023), (100003, 3000)])
+                                 (5120, 33), (5121, 900), (10007, 1), (16384, 100), (31745, 2), (32767, 40000), (32768, 5), (32769, 12000), (20011, 511), (30000, 131073), (65537, 1023), (100003, 3000)])
 def test_counts(ngsgd, N, V, law):
     """From one token to many, every kind of vocabulary: spread, equal, all one."""
     import torch
