@@ -52,12 +52,15 @@ int launch(CrossEntropy a, hipStream_t s) {
     LAUNCH_CHECK();
     return NGSGD_OK;
   }
+  // The fewest threads that hold a row in up to 8 pieces each, while wavefronts of their own rows fill the chip.  bf16, this and the next larger or smaller group, us:
+  // 65536 x 100 15 (16 lanes), 42 (64); 65536 x 256 21, 42; 32768 x 1000 34 (64 lanes), 77 (256 threads); 16384 x 2048 30, 61; 16384 x 4096 49, 62; 8192 x 8192 50
+  // (256), 59 (512), 81 (1024); 8192 x 16384 95 (512), 99 (256), 117 (1024); 8192 x 32000 180 (1024), 195 (512).
   if (pieces <= 16) return launch_rows<T, E, 16, 1, 256>(a, s);
   if (pieces <= 32) return launch_rows<T, E, 16, 2, 256>(a, s);
   if (pieces <= 64) return launch_rows<T, E, 64, 1, 256>(a, s);
   if (pieces <= 128) return launch_rows<T, E, 64, 2, 256>(a, s);
   if (pieces <= 256) return launch_rows<T, E, 64, 4, 256>(a, s);
-  if (pieces <= 512) return launch_rows<T, E, 256, 2, 256>(a, s);
+  if (pieces <= 512) return launch_rows<T, E, 64, 8, 256>(a, s);
   if (pieces <= 1024) return launch_rows<T, E, 256, 4, 256>(a, s);
   if (pieces <= 2048) return launch_rows<T, E, 512, 4, 512>(a, s);
   if (pieces <= 4096) return launch_rows<T, E, 1024, 4, 1024>(a, s);

@@ -425,7 +425,8 @@ __device__ __forceinline__ void embedding_sum_chunk(const EmbeddingBackward& a, 
 }
 
 // Very few tokens: no sorting.  A wavefront has all of them in its lanes, walks over rows of the table (and slabs of 64 pieces) and finds those that name
-// one by a ballot for each 64: one launch instead of three.  50000 x 1024 bf16 with 64 tokens 16 us (6.4 TB/s of zeros; sorted 25), with 128 that are all the same 17.
+// one by a ballot for each 64: one launch instead of three.  50000 x 1024 bf16 with 64 tokens 16 us (6.4 TB/s of zeros; sorted 25), two rows
+// with 128 tokens 17 (sorted 16 in three launches).
 constexpr int kFewRounds = 2, kFewTokens = kFewRounds * 64;
 template <typename T, typename W, typename I, int E>
 __global__ __launch_bounds__(kSumThreads) void embedding_few_kernel(const EmbeddingBackward a) {
