@@ -368,9 +368,16 @@ __device__ __forceinline__ void store_piece(const EmbeddingBackward& a, const ui
     store_pack(out, v);
   } else {
     const int skip = piece * E - at;
+    Pack<W, E> v = *reinterpret_cast<const Pack<W, E>*>(out);
 #pragma unroll
-    for (int j = 0; j < E; ++j)
-      if (j >= skip) out[j] = from_float<W>(as_f32(to_float(out[j]) + a.scale * sum[j]));
+    for (int j = 0; j < E; ++j) v.v[j] = from_float<W>(as_f32(to_float(v.v[j]) + a.scale * sum[j]));
+    if (skip == 0) {
+      store_pack(out, v);
+    } else {
+#pragma unroll
+      for (int j = 0; j < E; ++j)
+        if (j >= skip) out[j] = v.v[j];
+    }
   }
 }
 
