@@ -268,7 +268,8 @@ int ngsgd_embedding_backward(const void* dev_dy, int64_t lddy, int32_t type, con
  * One of loss and gradient at least.  Statistics are in fp32, and what the label's own term leaves of the sum is kept apart from it, so that
  * the loss and the label's gradient of a row that is as good as decided keep their digits; the gradient is rounded once.  A logit of -infinity is
  * a class that is not there: its probability is 0, and as the label's it gives a loss of infinity.  A row with a NaN or
- * +infinity, or with -infinity alone, has a loss and a gradient of NaN.  Sums are in an order that depends on the sizes alone.  Leading dimensions are
+ * +infinity, or with -infinity alone, has a loss and a gradient of NaN; finite logits of any size never do (where the largest of a row is
+ * beyond 2^27, a term that is less than 2^-60 of its own may count as 0).  Sums are in an order that depends on the sizes alone.  Leading dimensions are
  * at least V.  N is at most 2^30 and V 2^29.  dev_workspace (256-byte aligned) holds nothing between calls; calls that may run at the
  * same time need one each. */
 int ngsgd_cross_entropy_workspace_bytes(int64_t max_rows, int32_t V, size_t* out_bytes);

@@ -4,8 +4,10 @@
 // The label's term is kept out of the sum: where it is almost all of it, S is what the loss and the label's gradient are made of.
 //
 // Exponentials are powers of two of x L - M, L = log2(e) in fp32 and M = m L rounded: one multiply-add, which rounds once, and the hardware's power.  What
-// M's rounding adds is the same for all of a row, and the quotients do not see it; the loss takes the m that M stands for.  Where m L could overflow,
-// numbers that differ do so by 10^31: there L = 2^-20, which gives 1 for m and 0 for all others.
+// M's rounding adds, r = m L - M, is the same for all of a row, and the quotients do not see it; the loss takes the m that M stands for.  That needs 2^r to be a
+// number: half a step of M is at most 64 up to |m| = 2^30 (2^93 for a sum of 2^29 of them), and 2^128 beyond 2^31.  Farther out L = 1: M is m itself, m gives 1,
+// and any other number of fp32 lies at least 128 below, where the power and the definition's exponential are both 0 in fp32.  (Beyond 2^27 r is felt at the other
+// end: a term that is less than 2^-60 of the row's largest may count as 0.)
 //
 // Rows of up to 16384 pieces of 16 bytes are held in registers: read once, written once.  Wider ones are read a second time for the gradient.  Few wide
 // rows are cut into parts, whose statistics a second kernel joins.
@@ -49,10 +51,10 @@ struct LossStats {
 struct PowerBase {
   float m, L, M;
   __device__ __forceinline__ explicit PowerBase(const float m) : m(m) {
-    L = far() ? 0x1p-20f : kLog2e;
+    L = far() ? 1.f : kLog2e;
     M = m * L;
   }
-  __device__ __forceinline__ bool far() const { return fabsf(m) > 1e38f; }
+  __device__ __forceinline__ bool far() const { return fabsf(m) > 0x1p30f; }
   __device__ __forceinline__ float power(const float x) const { return __builtin_amdgcn_exp2f(fmaf(x, L, -M)); }
   // What a sum in the units of a lower base is in these; the bases may be far apart, and all of the sum sees the error of this.
   __device__ __forceinline__ float share(const PowerBase& other) const {

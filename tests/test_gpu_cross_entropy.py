@@ -454,3 +454,41 @@ def test_refusals(ngsgd):
     for bad in ((-1, 10), (8, 0), (8, -3)):
         with pytest.raises(ngsgd.NgsgdError):
             ngsgd.CrossEntropy(*bad)
+
+
+MASKS = [1e9, 2.0 ** 30, 2.0 ** 30 + 128, 2.0 ** 31, 1e10, 1e12, 1e20, 1e30, 1e38]
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])      # (fp16 has no such numbers)
+@pytest.mark.parametrize("N,V", [(63, 6), (63, 300), (63, 5001), (63, 33000), (63, 70001), (63, 140001), (130, 70001), (130, 140001)])
+def test_large_finite_logits(ngsgd, N, V, dtype):
+    """Masks that are finite and not the type's lowest value, and classes far above the rest: rows of 16 lanes to a workgroup, in parts, and wider than the registers."""
+    import torch
+    torch_type = getattr(torch, dtype)
+    rng = np.random.default_rng(14)
+    y = rng.integers(0, V, N)
+    x = 2.0 * rng.standard_normal((N, V))
+    for k, mask in enumerate(MASKS):
+        i = 7 * k
+        others = np.arange(V) != y[i]
+        x[i, others] = -mask                           # the label alone is left
+        x[i + 1, V // 4:V // 4 + max(1, V // 2)] = -mask      # a range of classes
+        x[i + 1, y[i + 1]] = 1.0
+        x[i + 2, rng.random(V) < 0.5] = -mask          # half of them
+        x[i + 2, y[i + 2]] = 1.0
+        x[i + 3] = -mask                               # all of them
+        x[i + 4, y[i + 4]] = -mask                     # the label
+        x[i + 5, (y[i + 5] + 1) % V] = mask            # another class far above
+        x[i + 6, y[i + 6]] = mask                      # the label far above
+    x = matrix(torch, x, torch_type, 1, 1)
+    ce, labels = ngsgd.CrossEntropy(N, V), torch.from_numpy(y).cuda()
+    loss, d = ce.gradient(x, labels, scale=0.5)
+    assert bool(loss.isfinite().all()) and bool(d.isfinite().all())
+    check(torch, x, y, 0.5, loss, d)
+    assert torch.equal(ce.forward(x, labels), loss)
+    for k in range(len(MASKS)):
+        i = 7 * k
+        assert float(loss[i]) == 0 and not bool(d[i].any()) and float(loss[i + 6]) == 0 and not bool(d[i + 6].any())
+        assert float(loss[i + 3]) == pytest.approx(np.log(V), rel=1e-6)
+    ce.gradient(x, labels, scale=0.5, dlogits=x)
+    assert torch.equal(x, d)
