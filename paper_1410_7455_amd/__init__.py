@@ -17,6 +17,7 @@ from ctypes import POINTER, byref, c_char_p, c_double, c_float, c_int, c_int32, 
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libngsgd.so")
+HELPER_PATH = os.path.join(_HERE, "_tensors.so")
 
 NGSGD_OK = 0
 NGSGD_EINVAL = -1
@@ -137,7 +138,7 @@ _lib = None
 _torch = None   # for calls that are short enough for an import statement to count
 
 
-def load_library():
+def _library():
     """Loads libngsgd.so and binds every declared entry point; raises if the library is missing."""
     global _lib, _torch
     if _lib is not None:
@@ -153,17 +154,29 @@ def load_library():
         _torch = torch
     except ImportError:
         pass
-    if _torch is not None:
-        try:
-            from . import _tensors   # noqa: F401  (addresses of many tensors at once; from here on a name of this package)
-        except ImportError as e:
-            raise ImportError(f"{_HERE}/_tensors.so is missing or of another torch: build it with `python -m paper_1410_7455_amd.build`") from e
     lib = ctypes.CDLL(LIB_PATH)
     for name, (restype, argtypes) in _SIGNATURES.items():
         fn = getattr(lib, name)          # AttributeError if the symbol is not exported
         fn.restype = restype
         fn.argtypes = argtypes
     _lib = lib
+    return lib
+
+
+def _load_helper():
+    """Loads _tensors.so (addresses of many tensors at once), which GradientNorm needs; from then on it is a name of this package."""
+    try:
+        from . import _tensors   # noqa: F401
+    except ImportError as e:
+        raise ImportError(f"{HELPER_PATH} is missing or of another torch: build it with `python -m paper_1410_7455_amd.build`") from e
+
+
+def load_library():
+    """Loads libngsgd.so, binds every declared entry point and loads the helper of GradientNorm, if it was built; raises if the library is missing,
+    or if the helper is of another torch."""
+    lib = _library()
+    if _torch is not None and "_tensors" not in globals() and os.path.exists(HELPER_PATH):
+        _load_helper()
     return lib
 
 
@@ -188,7 +201,7 @@ class Preconditioner:
     def __init__(self, dim, rank, max_batch, alpha=4.0, num_samples_history=2000.0, epsilon=1e-10,
                  update_period=4, always_update_first=10, _borrowed=None):
         import torch
-        self.lib = load_library()
+        self.lib = _library()
         self.dim, self.rank, self.max_batch = dim, rank, max_batch
         self._owner = None
         if _borrowed is not None:
@@ -256,7 +269,7 @@ class SimplePreconditioner:
 
     def __init__(self, max_rows, dim, alpha=4.0, epsilon=1e-20):
         import torch
-        self.lib = load_library()
+        self.lib = _library()
         self.max_rows, self.dim, self.alpha, self.epsilon = max_rows, dim, alpha, epsilon
         nbytes = c_size_t(0)
         _check(self.lib.ngsgd_simple_workspace_bytes(max_rows, dim, byref(nbytes)), "ngsgd_simple_workspace_bytes")
@@ -275,7 +288,7 @@ class SimplePreconditioner:
 def precondition_simple_static(M, alpha=4.0, epsilon=1e-20, gamma=None, rownorm2=None, stream=None):
     """ngsgd_precondition_simple_static: the simple method in place on M with the library's fixed scratch."""
     assert M.is_cuda and M.element_size() == 4 and M.stride(1) == 1
-    _check(load_library().ngsgd_precondition_simple_static(_ptr(M), M.shape[0], M.shape[1], M.stride(0), alpha,
+    _check(_library().ngsgd_precondition_simple_static(_ptr(M), M.shape[0], M.shape[1], M.stride(0), alpha,
                                                            epsilon, _ptr(gamma), _ptr(rownorm2),
                                                            _stream_ptr(stream)),
            "ngsgd_precondition_simple_static")
@@ -352,7 +365,7 @@ class LayerNorm:
 
     def __init__(self, max_rows, dim, epsilon=1e-5):
         import torch
-        self.lib = load_library()
+        self.lib = _library()
         self.max_rows, self.dim, self.epsilon = max_rows, dim, epsilon
         nbytes = c_size_t(0)
         _check(self.lib.ngsgd_layernorm_workspace_bytes(max_rows, dim, byref(nbytes)), "ngsgd_layernorm_workspace_bytes")
@@ -479,7 +492,7 @@ class Embedding:
 
     def __init__(self, max_tokens, vocabulary, dim, scale=1.0):
         import torch
-        self.lib = load_library()
+        self.lib = _library()
         self.max_tokens, self.vocabulary, self.dim, self.scale = max_tokens, vocabulary, dim, scale
         nbytes = c_size_t(0)
         _check(self.lib.ngsgd_embedding_workspace_bytes(max_tokens, vocabulary, dim, byref(nbytes)), "ngsgd_embedding_workspace_bytes")
@@ -567,7 +580,7 @@ class CrossEntropy:
 
     def __init__(self, max_rows, classes):
         import torch
-        self.lib = load_library()
+        self.lib = _library()
         self.max_rows, self.classes = max_rows, classes
         nbytes = c_size_t(0)
         _check(self.lib.ngsgd_cross_entropy_workspace_bytes(max_rows, classes, byref(nbytes)), "ngsgd_cross_entropy_workspace_bytes")
@@ -632,7 +645,8 @@ class GradientNorm:
 
     def __init__(self, like, grad_dtype=None):
         import torch
-        self.lib = load_library()
+        self.lib = _library()
+        _load_helper()
         like = list(like)
         n = len(like)
         if n == 0:
@@ -721,7 +735,7 @@ class AdamW:
                  master=False):
         import torch
         self.handle = None
-        self.lib = load_library()
+        self.lib = _library()
         self.params = list(params)
         n = len(self.params)
         if n == 0:
@@ -851,7 +865,7 @@ class Network:
                  num_samples_history=2000.0, epsilon=1e-10, update_period=4, always_update_first=10,
                  renorm=False, max_change_per_sample=0.0, method="online", simple_epsilon=1e-20, side_streams=0):
         import torch
-        self.lib = load_library()
+        self.lib = _library()
         self.handle = None
         self.method = {"online": NGSGD_METHOD_ONLINE, "simple": NGSGD_METHOD_SIMPLE, "adamw": NGSGD_METHOD_ADAMW,
                        "adamw8": NGSGD_METHOD_ADAMW8}[method]
@@ -989,7 +1003,7 @@ PROFILE_CATEGORIES = ["gemm_fwd", "gemm_bwd", "gemm_upd", "precond_h", "precond_
 
 
 def profile_enable(on: bool) -> None:
-    _check(load_library().ngsgd_profile_enable(1 if on else 0), "ngsgd_profile_enable")
+    _check(_library().ngsgd_profile_enable(1 if on else 0), "ngsgd_profile_enable")
 
 
 def profile_read():
@@ -997,18 +1011,18 @@ def profile_read():
     n = len(PROFILE_CATEGORIES)
     ms = (c_double * n)()
     cnt = (c_int64 * n)()
-    _check(load_library().ngsgd_profile_read(ms, cnt, n), "ngsgd_profile_read")
+    _check(_library().ngsgd_profile_read(ms, cnt, n), "ngsgd_profile_read")
     return {name: (ms[i], cnt[i]) for i, name in enumerate(PROFILE_CATEGORIES)}
 
 
 def set_wait_limit_us(microseconds: int) -> None:
     """ngsgd_set_wait_limit_us: bound of the waits between workgroups (fused apply kernel, first factors)."""
-    _check(load_library().ngsgd_set_wait_limit_us(int(microseconds)), "ngsgd_set_wait_limit_us")
+    _check(_library().ngsgd_set_wait_limit_us(int(microseconds)), "ngsgd_set_wait_limit_us")
 
 
 def average(networks, reset_preconditioners=True, stream=None):
     """ngsgd_average over replicas living on the same device."""
-    lib = load_library()
+    lib = _library()
     arr = (c_void_p * len(networks))(*[n.handle for n in networks])
     _check(lib.ngsgd_average(arr, len(networks), 1 if reset_preconditioners else 0, _stream_ptr(stream)),
            "ngsgd_average")

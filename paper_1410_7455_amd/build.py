@@ -1,10 +1,11 @@
-"""Builds libngsgd.so (HIP, gfx950) in-tree with hipcc, and the binding's helper _tensors.so (host code) with g++."""
+"""Builds libngsgd.so (HIP, gfx950) in-tree with hipcc alone, and where torch and g++ are there the binding's helper _tensors.so (host code)."""
 from __future__ import annotations
 
 import os
 import shutil
 import subprocess
 import sysconfig
+import warnings
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -30,10 +31,15 @@ def find_hipcc() -> str:
     raise RuntimeError("hipcc not found: the ngsgd library needs the ROCm toolchain to build")
 
 
-def binding_command() -> list:
-    """g++ on the binding's helper, against the Python and the torch that run this."""
-    import torch
-    from torch.utils import cpp_extension
+def binding_command():
+    """g++ on the binding's helper, against the Python and the torch that run this; None where there is no torch or no g++."""
+    try:
+        import torch
+        from torch.utils import cpp_extension
+    except ImportError:
+        return None
+    if shutil.which("g++") is None:
+        return None
     cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
            "-I", sysconfig.get_paths()["include"]]
     for path in cpp_extension.include_paths():
@@ -45,11 +51,12 @@ def binding_command() -> list:
 
 
 def build(verbose: bool = False) -> str:
-    """Compiles every source (side by side) and links them, and the binding's helper; raises with the compiler's output if one fails."""
+    """Compiles every source (side by side) and links them, and compiles the binding's helper; raises with the compiler's output if one fails."""
     hipcc = find_hipcc()
     objects = os.path.join(HERE, "_build")
     os.makedirs(objects, exist_ok=True)
     include = ["-I", os.path.join(ROOT, "include"), "-I", os.path.join(HERE, "csrc")]
+    binding = binding_command()
 
     def run(cmd):
         if verbose:
@@ -60,16 +67,20 @@ def build(verbose: bool = False) -> str:
         return run([hipcc, *HIPCC_FLAGS, *include, "-c", "-o", os.path.join(objects, os.path.basename(source) + ".o"), source])
 
     with ThreadPoolExecutor(max_workers=min(len(SOURCES) + 1, os.cpu_count() or 1)) as pool:
-        binding = pool.submit(lambda: run(binding_command()))
-        results = list(pool.map(compile_one, SOURCES)) + [binding.result()]
-    if all(r.returncode == 0 for r in results):
-        results.append(run([hipcc, "-shared", "-fPIC", "--offload-arch=gfx950", "-o", LIB_PATH,
-                            *(os.path.join(objects, os.path.basename(s) + ".o") for s in SOURCES)]))
+        helper = pool.submit(run, binding) if binding is not None else None
+        results = list(pool.map(compile_one, SOURCES))
+        if all(r.returncode == 0 for r in results):
+            results.append(run([hipcc, "-shared", "-fPIC", "--offload-arch=gfx950", "-o", LIB_PATH,
+                                *(os.path.join(objects, os.path.basename(s) + ".o") for s in SOURCES)]))
+    if helper is not None:
+        results.append(helper.result())
     for proc in results:
         if proc.returncode != 0:
             raise RuntimeError(f"{os.path.basename(proc.args[0])} failed:\n" + proc.stdout + proc.stderr)
         if verbose and proc.stderr.strip():
             print(proc.stderr)
+    if helper is None:
+        warnings.warn("no torch or no g++: built without _tensors.so, which GradientNorm needs")
     return LIB_PATH
 
 

@@ -205,3 +205,27 @@ def test_addresses_of_many_tensors():
     for bad in ((5, size(5), like, 0), ([None], [5], like, 0), ([None], size(5), torch.float32, 0), ([None], size(5), like, "0"), ([None], size(5), like)):
         with pytest.raises(TypeError):
             ng._tensors.addresses(*bad)
+
+
+@pytest.mark.parametrize("there", [False, True], ids=["missing", "of another torch"])
+def test_the_helper_is_needed_where_it_is_used(monkeypatch, there):
+    """Without it (built where there was no torch), or with one that does not load, everything but the norm of many gradients works."""
+    torch = pytest.importorskip("torch")
+    ng.load_library()
+    monkeypatch.setattr(ng, "_lib", None)
+    monkeypatch.delattr(ng, "_tensors")
+    monkeypatch.setitem(sys.modules, ng.__name__ + "._tensors", None)
+    if not there:
+        monkeypatch.setattr(ng, "HELPER_PATH", ng.HELPER_PATH + ".none")
+        assert ng.load_library().ngsgd_version() >= 100
+        monkeypatch.setattr(ng, "_lib", None)
+    monkeypatch.setattr(torch, "empty", lambda *_, **__: made(torch, Buffer))
+    monkeypatch.setattr(ng, "_raw_stream", lambda *_: 0)
+    for make in (lambda: ng.Embedding(4, 10, 8), lambda: ng.CrossEntropy(4, 10), lambda: ng.LayerNorm(4, 8)):
+        assert make().lib.ngsgd_version() >= 100
+    with pytest.raises(ImportError, match="_tensors.so"):
+        ng.GradientNorm([torch.zeros(4)])
+
+
+class Buffer:
+    """Stands for device memory."""
