@@ -289,8 +289,8 @@ def precondition_simple_static(M, alpha=4.0, epsilon=1e-20, gamma=None, rownorm2
     """ngsgd_precondition_simple_static: the simple method in place on M with the library's fixed scratch."""
     assert M.is_cuda and M.element_size() == 4 and M.stride(1) == 1
     _check(_library().ngsgd_precondition_simple_static(_ptr(M), M.shape[0], M.shape[1], M.stride(0), alpha,
-                                                           epsilon, _ptr(gamma), _ptr(rownorm2),
-                                                           _stream_ptr(stream)),
+                                                       epsilon, _ptr(gamma), _ptr(rownorm2),
+                                                       _stream_ptr(stream)),
            "ngsgd_precondition_simple_static")
 
 
