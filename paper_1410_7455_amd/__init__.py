@@ -711,7 +711,7 @@ class GradientNorm:
         """(norm, factor); every gradient is multiplied by the factor, in place or into `out` (a tensor for each gradient, which may be it)."""
         _current_device(self.device)
         if out is not None:
-            if len(out) != len(grads) or any(o is None and g is not None for o, g in zip(out, grads)):
+            if len(out) != len(grads) or any(o is None and g is not None and n != 0 for o, g, n in zip(out, grads, self.sizes)):
                 raise ValueError("out has no tensor for a gradient")
             out = self._addresses(out, "output")
         grads = self._addresses(grads, "gradient")

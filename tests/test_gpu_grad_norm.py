@@ -289,3 +289,13 @@ def test_refusals(ngsgd):
             g.norm(grads, bad)
         with pytest.raises(ngsgd.NgsgdError):
             g.clip(grads, bad)
+
+
+def test_no_output_for_an_empty_gradient(ngsgd):
+    import torch
+    rng = np.random.default_rng(20)
+    grads = make(torch, rng, [5, 0, 700], torch.float32, scale=1.0) + [None]
+    op = ngsgd.GradientNorm([*grads[:3], grads[0]])
+    out = [torch.full_like(grads[0], 9.0), None, torch.full_like(grads[2], 9.0), None]
+    norm, factor = op.clip(grads, 0.5, out=out)
+    check(torch, [grads[0], grads[2]], 0.5, norm, factor, out=[out[0], out[2]])

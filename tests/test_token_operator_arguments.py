@@ -229,3 +229,22 @@ def test_the_helper_is_needed_where_it_is_used(monkeypatch, there):
 
 class Buffer:
     """Stands for device memory."""
+
+
+def test_clip_needs_no_output_for_what_does_not_count(monkeypatch):
+    """out has to have a tensor only where a gradient with elements is."""
+    torch = pytest.importorskip("torch")
+    ng.load_library()
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(ng, "_raw_stream", lambda *_: None)
+    calls = []
+    taken = type("Library", (), {"ngsgd_grad_clip": lambda self, *a: calls.append(a) or ng.NGSGD_OK})()
+    some = torch.zeros(1)
+    g = made(torch, ng.GradientNorm, lib=taken, sizes=[0, 5], grad_dtype=torch.float32, _sizes=bytes(8) + (5).to_bytes(8, "little"), _like=torch.empty(0),
+             type=F32, workspace=some, workspace_bytes=4, _home=None, _results=lambda *_: (some, some))
+    for grads, out in (([torch.zeros(0), None], [None, None]), ([torch.zeros(0), None], [torch.zeros(0), None]), ([None, None], [None, None])):
+        g.clip(grads, 1.0, out=out)
+    assert len(calls) == 3 and all(a[2] == a[5] == bytes(16) for a in calls)
+    for grads, out in (([None, torch.zeros(5)], [None, None]), ([None, None], [None]), ([None, None], [None] * 3)):
+        with pytest.raises(ValueError, match="out has no tensor"):
+            g.clip(grads, 1.0, out=out)
