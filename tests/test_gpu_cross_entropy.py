@@ -492,3 +492,80 @@ def test_large_finite_logits(ngsgd, N, V, dtype):
         assert float(loss[i + 3]) == pytest.approx(np.log(V), rel=1e-6)
     ce.gradient(x, labels, scale=0.5, dlogits=x)
     assert torch.equal(x, d)
+
+
+def columns_at_borders(rng, V, E, parts):
+    """Both sides of the borders of pieces of E columns (the first one's, the last ones', those between a row's threads and rounds, between the rest and
+    what is held of a wide row, between parts), and some others."""
+    pieces = (V - 1) // E + 1 if V >= E else V
+    share = -(-pieces // parts)
+    at = {0, 1, 2, 3, E, V // 2, V // 3, V - E, V - 2 * E}
+    for threads in (16, 64, 256, 512, 1024):
+        at |= {threads * E * k for k in (1, 2, 3, 4, 7, 8, 15)}
+    at |= {share * E * k for k in range(1, parts)} | {(pieces - 12 * 1024) * E, (pieces - 1) * E, (pieces - 2) * E}
+    at = {b + s for b in at for s in (-1, 0)} | {V - 1 - k for k in range(2 * E)} | set(rng.integers(0, V, 20).tolist())
+    return np.array(sorted(c for c in at if 0 <= c < V))
+
+
+def count_columns(torch, ngsgd, V, dtype, at, N):
+    """Rows of zeros but for one column each.
+
+    16 at the label: its loss is log1p((V - 1) e^-16).  The others are 1 each in units of their own largest, whole numbers that fp32 adds exactly, so the loss counts the
+    columns: off by 16 u of itself (an exponential 3 u, a product, the label's power 2 u, a division 3 u, log1p 4 u; and 2^-40 of the argument), where one
+    column makes 1 / V.  16 elsewhere: a column that is left out makes the loss log V, one that is taken twice adds log 2 to it."""
+    p = np.exp(-16.0)
+    E, half = (4, 0.0) if dtype == torch.float32 else (8, torch.finfo(dtype).eps / 2)
+    tiny = torch.finfo(dtype).smallest_normal * torch.finfo(dtype).eps / 2
+    total = 1 + (V - 1) * p
+    ce = ngsgd.CrossEntropy(N, V)
+    for first in range(0, len(at), N):
+        c = np.resize(at[first:first + N], N)
+        rows, columns = torch.arange(N, device="cuda"), torch.from_numpy(c).cuda()
+        x = torch.zeros(N, V, dtype=dtype, device="cuda")
+        x[rows, columns] = 16.0
+        loss, d = ce.gradient(x, columns)
+        want = float(np.log1p((V - 1) * p))
+        assert bool(((loss.double() - want).abs() <= 16 * U * want).all()), (V, first, float(((loss.double() - want) / max(want, 1e-30)).abs().max()))
+        label, d[rows, columns] = d[rows, columns].double(), float("nan")
+        assert bool(((label + (V - 1) * p / total).abs() <= (32 * U + half) * (V - 1) * p + tiny).all())
+        there = d.isfinite().sum(1)
+        assert bool((there == V - 1).all())
+        assert bool((((d.double() - p / total).abs() <= (40 * U + half) * p + tiny) | d.isnan()).all())
+        if V == 1:
+            continue
+        labels = torch.from_numpy((c + 1 + V // 3) % V).cuda()
+        labels[labels == columns] = (columns[labels == columns] + 1) % V
+        loss, d = ce.gradient(x, labels)
+        # (K u of a sum of K additions, an eighth of log 2 at most here)
+        assert bool(((loss.double() - 16 - np.log(total)).abs() <= (V / 64 + 60) * U + 16 * 4 * U).all()), (V, first)
+        assert bool(((d[rows, columns].double() - 1 / total).abs() <= (V / 64 + 60) * U + half).all())
+        assert bool((d[rows, labels].double() + 1).abs().max() <= 2 * p + half)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("V", [*WIDTHS, 140001, 250001])
+def test_every_column_counts_once(ngsgd, V, dtype):
+    """Many rows, and few ones, which are cut into parts where they are wide."""
+    import torch
+    dtype = getattr(torch, dtype)
+    E = 4 if dtype == torch.float32 else 8
+    rng = np.random.default_rng(V)
+    for N in (130, 100, 5) if V > 4096 * E else (130,):
+        parts = 1 if N >= 128 else min(64, -(-1024 // N), -(-V // E) // 512)
+        count_columns(torch, ngsgd, V, dtype, columns_at_borders(rng, V, E, max(1, parts)), N)
+
+
+def test_every_column_of_narrow_rows(ngsgd):
+    import torch
+    for V, dtype in ((5, torch.float32), (37, torch.float16), (64, torch.bfloat16), (129, torch.bfloat16), (515, torch.float32), (1025, torch.float16)):
+        count_columns(torch, ngsgd, V, dtype, np.arange(V), V)
+
+
+@pytest.mark.parametrize("N,V", [(1, 3_000_001), (2, 2_500_000), (130, 2_000_003)])
+def test_columns_of_very_wide_rows(ngsgd, N, V):
+    """A piece of 8 columns that is left out or taken twice makes 8 / V = 2.7e-6 at least, where 16 u = 9.5e-7 are allowed."""
+    import torch
+    rng = np.random.default_rng(V)
+    pieces = -(-V // 8)
+    at = np.concatenate([[0, 7, 8, V - 1, V - 8, V - 9, V // 2, (pieces - 12288) * 8 - 1, (pieces - 12288) * 8], rng.integers(0, V, 3)])
+    count_columns(torch, ngsgd, V, torch.bfloat16, at, N)
