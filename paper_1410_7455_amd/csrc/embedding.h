@@ -257,42 +257,39 @@ __global__ __launch_bounds__(1024) void embedding_scan_kernel(const EmbeddingSor
 }
 
 // Places: digits in order, tiles in order within a digit, a tile's tokens in order within that.  A wavefront ranks 64 tokens at a time: lanes
-// with the same digit find each other by one ballot a bit.  Then the digits are dealt to the threads, neighbours to each.
+// with the same digit find each other by one ballot a bit.  Then every thread has one of the digits.
 template <typename I, bool FIRST>
 __global__ __launch_bounds__(kSortThreads) void embedding_scatter_kernel(const EmbeddingSort a) {
-  constexpr int kWaves = kSortThreads / 64, kOwn = kSortBins / kSortThreads;
+  static_assert(kSortBins == kSortThreads);
+  constexpr int kWaves = kSortThreads / 64;
   __shared__ uint32_t bins[kWaves * kSortBins];   // of each wavefront: its count, then where its next token with that digit goes
   __shared__ uint32_t waves[kWaves];
-  using Counts = Pack<uint32_t, kOwn>;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const bool owns = threadIdx.x * kOwn < (unsigned)a.bins;
+  const bool owns = threadIdx.x < (unsigned)a.bins;
   uint32_t* const mine = bins + wave * a.bins;
   const int64_t from = ((int64_t)blockIdx.x * kSortThreads + wave * 64) * kSortRounds + lane;
   SortedToken token[kSortRounds];
 #pragma unroll
   for (int r = 0; r < kSortRounds; ++r) token[r] = sort_input<I, FIRST>(a, min(from + r * 64, a.N - 1));
-  // tokens with this thread's digits: in all tiles, and in those in front
-  Counts total{}, before{};
+  // tokens with this thread's digit: in all tiles, and in those in front
+  uint32_t total = 0, before = 0;
   if (owns) {
-    const Counts* const counts = reinterpret_cast<const Counts*>(a.counts) + threadIdx.x;
-    const int stride = a.bins / kOwn;
+    const uint32_t* const counts = a.counts + threadIdx.x;
     if (a.totals != nullptr) {
-      before = counts[(int64_t)blockIdx.x * stride];
-      total = reinterpret_cast<const Counts*>(a.totals)[threadIdx.x];
+      before = counts[(int64_t)blockIdx.x * a.bins];
+      total = a.totals[threadIdx.x];
     } else {
       constexpr int kAhead = 16;
       for (int t = 0; t < a.tiles; t += kAhead) {
-        Counts of[kAhead];
+        uint32_t of[kAhead];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) of[u] = counts[min(t + u, a.tiles - 1) * stride];
+        for (int u = 0; u < kAhead; ++u) of[u] = counts[min(t + u, a.tiles - 1) * a.bins];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u)
-#pragma unroll
-          for (int k = 0; k < kOwn; ++k) {
-            const uint32_t here = t + u < a.tiles ? of[u].v[k] : 0u;
-            before.v[k] += t + u < (int)blockIdx.x ? here : 0u;
-            total.v[k] += here;
-          }
+        for (int u = 0; u < kAhead; ++u) {
+          const uint32_t here = t + u < a.tiles ? of[u] : 0u;
+          before += t + u < (int)blockIdx.x ? here : 0u;
+          total += here;
+        }
       }
     }
   }
@@ -320,10 +317,7 @@ __global__ __launch_bounds__(kSortThreads) void embedding_scatter_kernel(const E
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
   }
   // tokens with lower digits than this thread's
-  uint32_t sum = 0;
-#pragma unroll
-  for (int k = 0; k < kOwn; ++k) sum += total.v[k];
-  uint32_t below = sum;
+  uint32_t below = total;
 #pragma unroll
   for (int k = 1; k < 64; k *= 2) {
     const uint32_t o = __shfl_up(below, k);
@@ -331,21 +325,17 @@ __global__ __launch_bounds__(kSortThreads) void embedding_scatter_kernel(const E
   }
   if (lane == 63) waves[wave] = below;
   __syncthreads();
-  below -= sum;
+  below -= total;
   for (int k = 0; k < wave; ++k) below += waves[k];
   if (owns) {
+    uint32_t at = below + before, here[kWaves];
+    uint32_t* const bin = bins + threadIdx.x;
 #pragma unroll
-    for (int k = 0; k < kOwn; ++k) {
-      uint32_t at = below + before.v[k], here[kWaves];
-      below += total.v[k];
-      uint32_t* const bin = bins + threadIdx.x * kOwn + k;
+    for (int w = 0; w < kWaves; ++w) here[w] = bin[w * a.bins];
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) here[w] = bin[w * a.bins];
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
-        bin[w * a.bins] = at;
-        at += here[w];
-      }
+    for (int w = 0; w < kWaves; ++w) {
+      bin[w * a.bins] = at;
+      at += here[w];
     }
   }
   __syncthreads();
@@ -386,7 +376,7 @@ constexpr int kSumThreads = 256, kSumAhead = 8;   // rows that a thread has in f
 // The sums of a chunk of sorted tokens, of the columns of this thread's piece.  A token whose rows are all in the chunk is done; the first one's and the last
 // one's sums are parts if the chunks beside this one have rows of theirs.  Bound by memory: 262144 x 2048 bf16 over 131072 rows in fp32 (1.04 GB read, 1.07
 // GB written with the rows that are cleared) 450 us, 4.7 TB/s, what a copy reaches; 8192 wavefronts instead of 4096 480, 2048 585.
-template <typename T, typename W, int E, bool WAVE>
+template <typename T, typename W, int E>
 __device__ __forceinline__ void embedding_sum_chunk(const EmbeddingBackward& a, const int64_t chunk, const int piece) {
   const int64_t from = chunk * a.chunk, to = min(from + a.chunk, a.N);
   const int at = min(piece * E, a.D - E);
@@ -537,10 +527,10 @@ __global__ __launch_bounds__(kSumThreads) void embedding_sum_kernel(const Embedd
   if (WAVE) {   // (uniform)
     const int64_t unit = (int64_t)blockIdx.x * (kSumThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t chunk = unit / a.slabs;
-    if (chunk < a.chunks) embedding_sum_chunk<T, W, E, WAVE>(a, chunk, (int)(unit % a.slabs) * 64 + (threadIdx.x & 63));
+    if (chunk < a.chunks) embedding_sum_chunk<T, W, E>(a, chunk, (int)(unit % a.slabs) * 64 + (threadIdx.x & 63));
   } else {
     const int64_t chunk = ((int64_t)blockIdx.x * kSumThreads + threadIdx.x) / a.lanes;
-    if (chunk < a.chunks) embedding_sum_chunk<T, W, E, WAVE>(a, chunk, threadIdx.x & (a.lanes - 1));
+    if (chunk < a.chunks) embedding_sum_chunk<T, W, E>(a, chunk, threadIdx.x & (a.lanes - 1));
   }
 }
 
