@@ -88,7 +88,13 @@ struct RowPart {
       return __builtin_bit_cast(float, v[e]);
   }
 };
-// Both pieces that hold a column write the same number to it; with ONCE only the one where it counts.
+// A number that two threads write is not merged with its rounding to fp16.  (bf16 and fp32 have no instruction that does both.)
+template <typename T, bool TWICE>
+__device__ __forceinline__ float alone(const float x) {
+  if constexpr (__is_same(T, fp16) && TWICE) return as_f32(x);
+  return x;
+}
+// Both pieces that hold a column write the same number to it, so it is rounded alike in both; with ONCE only the one where it counts does.
 template <typename S, bool ONCE, typename T>
 __device__ __forceinline__ void store_row(const float (&v)[S::E], T* p, const RowColumns<S>& cols) {
 #pragma unroll
@@ -97,12 +103,12 @@ __device__ __forceinline__ void store_row(const float (&v)[S::E], T* p, const Ro
     if (!ONCE || cols.at[k] == S::column(k)) {
       Pack<T, S::VEC> o;
 #pragma unroll
-      for (int j = 0; j < S::VEC; ++j) o.v[j] = from_float<T>(v[k * S::VEC + j]);
+      for (int j = 0; j < S::VEC; ++j) o.v[j] = from_float<T>(alone<T, !ONCE>(v[k * S::VEC + j]));
       *reinterpret_cast<Pack<T, S::VEC>*>(p + cols.at[k]) = o;
     } else {
 #pragma unroll
       for (int j = 0; j < S::VEC; ++j)
-        if (cols.counts(k * S::VEC + j)) p[cols.at[k] + j] = from_float<T>(v[k * S::VEC + j]);
+        if (cols.counts(k * S::VEC + j)) p[cols.at[k] + j] = from_float<T>(alone<T, !ONCE>(v[k * S::VEC + j]));
     }
   }
 }

@@ -536,3 +536,25 @@ def test_rows_far_from_zero_among_others(ngsgd, N, D, dtype):
     bound = out[2][equal].double()[:, None] * (K * U * 100.5) * (K + 3) * U + (half_step(torch, x.dtype) + U) * B.abs()
     assert bool(((out[0][equal].double() - B).abs() <= bound).all())
     check_forward(torch, x[:64], None, b, 1e-5, *(t[:64] for t in out))
+
+
+@pytest.mark.parametrize("D", [6, 70, 514, 1030, 4098, 8202, 12000, 16382])
+def test_columns_are_rounded_alike(ngsgd, D):
+    """Equal numbers in all columns give equal gradients, also in those that two threads write: with x = mean = 0 and derivatives of +a and -a, dx is rstd (+-a).
+    The products of rstd and a are picked so that rounding them to fp16 by way of fp32 gives another number than rounding them at once."""
+    import torch
+    rng = np.random.default_rng(D)
+    a = (1.0 + rng.integers(1, 1024, 2 ** 20) / 1024.0)
+    r = (1.0 + rng.random(2 ** 20)).astype(np.float32).astype(np.float64)
+    exact = a * r                                       # (35 bits)
+    step = np.where(exact < 2, 2.0 ** -10, 2.0 ** -9)
+    fp32 = exact.astype(np.float32).astype(np.float64)
+    tie = ((fp32 / step) % 1.0 == 0.5) & (exact != fp32)
+    at_once = np.where(exact > fp32, np.ceil(fp32 / step), np.floor(fp32 / step)) * step
+    pick = np.flatnonzero(tie & (at_once != fp32.astype(np.float16)))[:24]
+    assert len(pick) == 24
+    dy = torch.from_numpy(np.outer(a[pick], np.resize([1.0, -1.0], D))).half().cuda()
+    rstd, zero = torch.from_numpy(r[pick]).float().cuda(), torch.zeros(24, device="cuda")
+    for w in (None, torch.ones(D, device="cuda"), torch.ones(D, device="cuda").half()):
+        dx = ngsgd.LayerNorm(24, D).backward(dy, torch.zeros_like(dy), zero, rstd, w)[0]
+        assert bool((dx.abs() == dx[:, :1].abs()).all())

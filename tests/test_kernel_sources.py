@@ -183,3 +183,15 @@ def test_wide_patches_leave_no_dies_idle():
     wide = {(n, d, r): r > 32 and -(-n // number["kFusedRows"]) * -(-d // number["kFusedChunk"]) > number["kFusedWideUnits"] and
             4 * busiest(n, d, number["kFusedWide"]) <= 3 * busiest(n, d, number["kFusedChunk"]) for n, d, r in WIDE + [(2048, 5000, 80), (512, 5000, 80)]}
     assert [k for k in wide if wide[k]] == [(4033, 2497, 41), (1990, 5001, 96), (4096, 2401, 80), (4090, 2560, 33), (2048, 5000, 80)]
+
+
+def test_columns_that_two_threads_write_are_rounded_alike():
+    """A row's last piece is moved back to end with the row, and some kernels write the columns that it shares with the piece before from both.  The compiler may
+    merge the last multiplication with the rounding to fp16 for some of a thread's elements only (one rounding, where the others have
+    two), and which of two such numbers stays is a matter of time: the conversion takes a number that is not merged with it."""
+    texts = dict(sources())
+    store_row = re.search(r"void store_row\(.*?\n}\n", texts["layer_norm.h"], re.S).group(0)
+    lookup = re.search(r"void embedding_forward_kernel\(.*?\n}\n", texts["embedding.h"], re.S).group(0)
+    store_piece = re.search(r"void store_piece\(.*?\n}\n", texts["embedding.h"], re.S).group(0)
+    for body, rounded in ((store_row, r"from_float<T>\(alone<T, !ONCE>\("), (lookup, r"from_float<T>\(named \? as_f32\("), (store_piece, r"from_float<W>\(as_f32\(")):
+        assert len(re.findall(r"from_float<", body)) == len(re.findall(rounded, body)) > 0
