@@ -288,7 +288,7 @@ int ngsgd_grad_norm_workspace_bytes(int32_t n_tensors, size_t* out_bytes);
  *   max_norm         not negative; infinity for the norm alone (factor 1)
  *   dev_norm, dev_factor (1 float each, either may be NULL)
  * Squares are summed in fp64, in an order that depends on the sizes alone, so no square overflows or vanishes; the norm is rounded to
- * fp32 and the factor formed before that.  An infinity among the elements gives the norm infinity and the factor 0 (max_norm
+ * fp32 and the factor formed before that (rounded to fp32 itself, with fewer digits below 2^-126).  An infinity among the elements gives the norm infinity and the factor 0 (max_norm
  * infinity: 1), a NaN gives NaN for both.  The factor is what ngsgd_adamw_step takes as dev_grad_scale.  At most 2^40 elements a tensor. */
 int ngsgd_grad_norm(int32_t n_tensors, const int64_t* sizes, const void* const* dev_grads, int32_t type, double max_norm,
                     float* dev_norm, float* dev_factor, void* dev_workspace, size_t workspace_bytes, void* hip_stream);

@@ -16,7 +16,10 @@ constexpr int64_t kLaunchRows = (int64_t)1 << 21;
 constexpr int kRegisterPieces = 16384;     // of 16 bytes: of wider rows some are read twice
 static_assert(kRegisterPieces >= kHeldPieces);
 constexpr int kPartPieces = 4096;          // rows of more are cut into parts
-constexpr int kPartRows = 128;             // if there are fewer than so many (127 x 128256 bf16 in parts 24 us, 128 without 24),
+// if there are fewer than so many.  127 rows in parts and 128 without, gradient, us: bf16 4100 pieces 11.5, 9.7; 8192 14.4, 14.4; 16384 26.2, 25.7; 25000 35.6, 39.7; 250000
+// 345, 416; fp32 4100 10.4, 7.5; 8192 12.4, 9.8; 16384 23.6, 18.2; 25000 32.9, 31.1; 250000 332, 352: the border is right for rows that a workgroup does not hold, and too
+// high for those that it does (64 rows in parts: 4100 pieces 10.5, 16384 13.6 bf16 and 12.0 fp32).
+constexpr int kPartRows = 128;
 constexpr int kPartGroups = 1024;          // into about so many workgroups' worth
 constexpr int kPartLeast = 512;            // of at least so many pieces
 

@@ -28,8 +28,11 @@ int with_types(const int type, const int table_type, const int index_type, F f) 
 }
 
 // Rows of the table from here on are cut into eight slabs, one for each die (workgroups go to them in turn), whose cache then holds eight times as many rows'
-// parts: 65536 x 8192 fp32 of a Zipf law 623 -> 535 us, 196613 x 4096 fp32 to bf16 543 -> 537 (1.37 -> 0.85 GB fetched); narrower rows lose (131072 x 4096
-// bf16 281 -> 300), and so do two or more slabs of a die one after the other (530 -> 550 and more: pieces of y that are written together get short).
+// parts (196613 x 4096 fp32 to bf16: 1.37 -> 0.85 GB fetched).  What a call takes without and with them, us, 131072 tokens (from 23 KB of y on so many that y has 3 GB) of
+// a Zipf law over 50021 rows: fp32 4096 columns 631, 598; 4104 592, 595; 5120 795, 765; 6152 868, 801; 8192 863, 745; 16384 841, 776; fp32 to bf16 4096 361, 357; 4104
+// 369, 408; 5120 461, 497; 6152 577, 578; 8192 719, 680; bf16 8192 623, 607; 8200 595, 616; 10240 783, 805; 12296 881, 825; 16384 849, 766.  Between 16 and 24 KB it
+// depends on how a slab's pieces fill a power of two of threads: up to 5 % are won, and up to 10 % lost.  Narrower rows lose (131072 x 4096 bf16 281 -> 300), and so
+// do two or more slabs of a die one after the other (530 -> 550 and more: pieces of y that are written together get short).
 constexpr size_t kSlabBytes = 16384;
 constexpr int kDies = 8;
 // What is larger than all dies' caches is written past them, which leaves them to the table (65536 x 1024 bf16 29 -> 26 us, 131072 x 4096 309 -> 281).
